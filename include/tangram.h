@@ -656,6 +656,204 @@ int32_t tg_concat_tables(const tg_geometry* geom, int32_t batch_a, const int64_t
 int32_t tg_read_probe(const tg_geometry* geom, int32_t dtype, const void* kv_pool, const int32_t* page_ids,
                       const int32_t* slots, int64_t n, int32_t n_workers, uint32_t* out, void* hip_stream);
 
+/* -------------------------- 10. queries and keys: norms, rotary positions
+ * What lies between a layer's projection and the cache: RMS norm of every query
+ * and key head, rotation by position, the value rows copied beside them.
+ *
+ * 10a. tg_rope_freqs (host): the rotation of pair j of rot_dim rotated dims,
+ * j < rot_dim / 2.  Radians per token, theta_j = base^(-2j / rot_dim), scaled
+ * for contexts longer than the model was trained on:
+ *   TG_ROPE_PLAIN   theta_j
+ *   TG_ROPE_LINEAR  theta_j / factor (positions interpolated)
+ *   TG_ROPE_NTK     theta_j with base * factor^(rot_dim / (rot_dim - 2)); rot_dim > 2
+ *   TG_ROPE_BANDS   by the turns n_j = original_len * theta_j / (2 pi) made in
+ *                   the original context: theta_j where n_j >= high, theta_j /
+ *                   factor where n_j <= low, between them
+ *                   (1 - w) theta_j / factor + w theta_j, w = (n_j - low) / (high - low)
+ *   TG_ROPE_YARN    the same, and cosine and sine times 0.1 ln(factor) + 1
+ * All arithmetic in fp64.  turns [rot_dim / 2] uint64 out: turns per token,
+ * theta_j / (2 pi) modulo 1, as a 64-bit binary fraction, which the kernels
+ * multiply by the position modulo 2^64: the angle of any int32 position is
+ * exact to 2^-52 of theta.  attn_factor out: 0.1 ln(factor) + 1 for TG_ROPE_YARN, else 1.
+ *   rot_dim even, >= 2; base > 1; factor >= 1; original_len >= 1 and 0 < low <
+ *   high (BANDS, YARN; not read otherwise).
+ * tg_rope_turns: the same conversion for n caller-made angular frequencies
+ * (finite, radians per token).
+ * Errors: TG_ERR_INVALID_ARG (nothing written). */
+enum { TG_ROPE_PLAIN = 0, TG_ROPE_LINEAR = 1, TG_ROPE_NTK = 2, TG_ROPE_BANDS = 3, TG_ROPE_YARN = 4 };
+/* which dims are a pair: j and j + rot_dim / 2, or 2j and 2j + 1 */
+enum { TG_ROPE_HALF = 0, TG_ROPE_INTERLEAVED = 1 };
+
+int32_t tg_rope_freqs(int32_t rot_dim, double base, int32_t scaling, double factor, int32_t original_len, double low,
+                      double high, uint64_t* turns, float* attn_factor);
+int32_t tg_rope_turns(int32_t n, const double* theta, uint64_t* turns);
+
+/* How a head is normalised and rotated: with x the head's d values,
+ *   y = norm ? x * (mean(x^2) + eps)^(-1/2) * w : x
+ *     (w = weight_offset + q_weight or k_weight, 1 where that is NULL),
+ *   (y_a, y_b) of every rotated pair becomes attn_factor * (y_a cos t - y_b sin t,
+ *     y_b cos t + y_a sin t), t = position * theta_j; dims at or past rot_dim
+ *     are left as y.
+ * Everything in fp32, rounded to the type once, at the end.
+ * rot_dim: 0 (no rotation, turns not read) or a multiple of 16 up to head_dim;
+ * attn_factor: 0 means 1; eps >= 0.  turns, q_weight [d] and k_weight [d]
+ * (dtype of the call) are DEVICE pointers, the weights 16-byte aligned. */
+typedef struct {
+  int32_t layout;
+  int32_t rot_dim;
+  const uint64_t* turns;
+  float attn_factor;
+  int32_t norm;            /* 0 or 1 */
+  float eps;
+  float weight_offset;
+  const void* q_weight;
+  const void* k_weight;
+} tg_rope_spec;
+
+/* 10b. tg_rope (device): the operands of a chunk's attention (tg_prefill,
+ * tg_compress; with chunk_len 1 tg_decode's q, append_k and append_v).
+ * DEVICE pointers:
+ *   q_in, k_in, v_in: token (b, i)'s heads are contiguous, [Hq or H][d], at
+ *     element (b*C + i) * stride of each (q_stride, k_stride, v_stride, in
+ *     elements), so the three may be parts of one projection's rows; a NULL
+ *     input with its NULL output is left out
+ *   q_out [B][C][Hq][d], k_out, v_out [B][C][H][d] dtype; v is copied as it is
+ *   positions [B][C] int32, or NULL: token (b, i) stands at start[b] + i (start
+ *     [B] int32, or NULL for 0); a position may be negative
+ *   chunk_tokens [B] int32 or NULL: tokens at or past chunk_tokens[b] are not
+ *     read and their outputs are left as they were (NULL: all C are valid)
+ * An output may be its own input when that input's stride is the dense one
+ * (Hq*d, H*d); otherwise outputs must not overlap inputs.
+ * Supported: dtype TG_F32 or TG_BF16, head_dim 64 or 128.  Pointers 16-byte
+ * aligned, strides multiples of 16 bytes and at least a token's heads.  No
+ * workspace. */
+typedef struct {
+  tg_geometry geom;
+  int32_t batch;
+  int32_t chunk_len;
+  int32_t dtype;
+  tg_rope_spec spec;
+  const void* q_in;
+  const void* k_in;
+  const void* v_in;
+  int64_t q_stride;
+  int64_t k_stride;
+  int64_t v_stride;
+  const int32_t* positions;
+  const int32_t* start;
+  const int32_t* chunk_tokens;
+  void* q_out;
+  void* k_out;
+  void* v_out;
+} tg_rope_args;
+
+int32_t tg_rope(const tg_rope_args* args, void* hip_stream);
+
+/* 10c. tg_rope_append (device): one decode step's new token of one layer from
+ * the projection's rows: the query heads to q_out, every KV head's key
+ * (normalised, rotated) and value to its next entry of the cache, as tg_rope
+ * with chunk_len 1 followed by tg_append, bit for bit, in one launch.
+ *   q_in (NULL with q_out NULL), k_in, v_in: rows of request b at b * stride
+ *   positions [B] int32: the token's position (with a compressed cache not the
+ *     head's number of entries)
+ *   the rest as tg_append's: a head whose table is full stores nothing and sets
+ *     *full to 1 (its query heads are written all the same).
+ * Supported: as tg_rope; any page_size. */
+typedef struct {
+  tg_geometry geom;
+  int32_t batch;
+  int32_t layer;
+  int32_t dtype;
+  tg_rope_spec spec;
+  const void* q_in;
+  const void* k_in;
+  const void* v_in;
+  int64_t q_stride;
+  int64_t k_stride;
+  int64_t v_stride;
+  const int32_t* positions;
+  void* q_out;
+  void* kv_pool;
+  const int32_t* pt_pages;
+  const int64_t* pt_offsets;
+  const int32_t* group_of;
+  const int32_t* slot_of;
+  int32_t* live_len;
+  int32_t* full;
+} tg_rope_append_args;
+
+int32_t tg_rope_append(const tg_rope_append_args* args, void* hip_stream);
+
+/* ------------------------------ 11. block tables and slot maps on the device
+ * 11a. tg_reserve_device: tg_reserve on DEVICE arrays, from context lengths
+ * that are on the device, without the host waiting: the same kv_len, group_len,
+ * pt_offsets and pt_pages, bit for bit.  Arguments as tg_reserve's, all DEVICE
+ * pointers except the counts (num_free, pool_pages, pt_capacity); pages_needed
+ * int64 and status int32 are one value each.
+ *   *status receives TG_OK, or what tg_reserve would have returned:
+ *     TG_ERR_INVALID_ARG for a context length < 1, a headroom < 0, a ratio
+ *     outside (0, 1], a group id outside [0, G) or a consumed page id outside
+ *     the pool; TG_ERR_OUT_OF_PAGES; TG_ERR_BUFFER_TOO_SMALL (in this order).
+ *   Unlike tg_reserve, distinctness of the consumed page ids is not checked.
+ *   Where *status is not TG_OK every table is empty (all of pt_offsets is 0), so
+ *     that calls already enqueued behind it touch no page; pages_needed is what
+ *     the lengths need (lengths that are invalid count as 0), and pt_pages past
+ *     the pages needed or taken is left as it was.
+ *   workspace: tg_reserve_device_workspace_bytes(geom, batch) bytes, no
+ *     initialisation needed; calls that share one must not overlap in time.
+ * Errors (host): TG_ERR_INVALID_ARG, TG_ERR_BUFFER_TOO_SMALL (workspace), TG_ERR_HIP. */
+typedef struct {
+  tg_geometry geom;
+  int32_t batch;
+  const int32_t* ctx_len;
+  const int32_t* headroom;
+  const double* ratio;
+  const double* budget;
+  const int32_t* group_of;
+  const int32_t* free_pages;
+  int64_t num_free;
+  int64_t pool_pages;
+  int32_t* kv_len;
+  int32_t* group_len;
+  int64_t* pt_offsets;
+  int32_t* pt_pages;
+  int64_t pt_capacity;
+  int64_t* pages_needed;
+  int32_t* status;
+  void* workspace;
+  size_t workspace_bytes;
+} tg_reserve_device_args;
+
+size_t  tg_reserve_device_workspace_bytes(const tg_geometry* geom, int32_t batch);
+int32_t tg_reserve_device(const tg_reserve_device_args* args, void* hip_stream);
+
+/* 11b. tg_slot_map (device): where entries of one layer's heads lie.  For j < n
+ * and e = begin[b][layer][h] + j (begin NULL: 0),
+ *   map[b][h][j] = ((page * 2) * H_p + slot) * P + e % P,
+ * the row (of d elements) of entry e's K in the pool, page = pt_pages[pt_offsets[t]
+ * + e / P]; its V is H_p * P rows further.  -1 where e < 0, e >= len[b][layer][h]
+ * (len NULL: no such limit) or e is past the head's table.  With begin = the live
+ * lengths these are the slots that the next n tokens take; with begin NULL and
+ * len = the live lengths, the whole head.
+ * DEVICE pointers: pt_offsets, pt_pages, group_of, slot_of as tg_append's; begin,
+ * len [B][L][H] int32 or NULL; map [B][H][n] int64.  n >= 1.  Any head_dim and
+ * page_size.  Errors: TG_ERR_INVALID_ARG, TG_ERR_HIP. */
+typedef struct {
+  tg_geometry geom;
+  int32_t batch;
+  int32_t layer;
+  const int64_t* pt_offsets;
+  const int32_t* pt_pages;
+  const int32_t* group_of;
+  const int32_t* slot_of;
+  const int32_t* begin;
+  const int32_t* len;
+  int32_t n;
+  int64_t* map;
+} tg_slot_map_args;
+
+int32_t tg_slot_map(const tg_slot_map_args* args, void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1026,3 +1026,54 @@ extern "C" int32_t tg_concat_tables(const tg_geometry* geom, int32_t batch_a, co
   if (nb) std::memcpy(pages + na, pages_b, (size_t)nb * sizeof(int32_t));
   return TG_OK;
 }
+
+// Turns per token modulo 1, as a 64-bit binary fraction.  The quotient by 2 pi
+// is taken in extended precision: 64 bits of fraction need more than fp64 holds.
+static uint64_t turn_fraction(double theta) {
+  constexpr long double kTwoPi = 6.283185307179586476925286766559L;
+  const long double turns = (long double)theta / kTwoPi;
+  const long double scaled = std::ldexp(turns - std::floor(turns), 64);
+  return scaled >= 18446744073709551615.5L ? 0 : (uint64_t)(scaled + 0.5L);
+}
+
+extern "C" int32_t tg_rope_turns(int32_t n, const double* theta, uint64_t* turns) {
+  if (n < 1) return fail(TG_ERR_INVALID_ARG, "n must be >= 1");
+  if (!theta || !turns) return fail(TG_ERR_INVALID_ARG, "NULL array");
+  for (int32_t j = 0; j < n; ++j)
+    if (!std::isfinite(theta[j])) return fail(TG_ERR_INVALID_ARG, "theta[%d] is not finite", j);
+  for (int32_t j = 0; j < n; ++j) turns[j] = turn_fraction(theta[j]);
+  return TG_OK;
+}
+
+// The rotation of every pair, scaled for long contexts.  Pairs that turn often
+// within the original context tell neighbours apart and are left as they are by
+// the two schemes that go by turns; pairs that make less than `low` turns would
+// see angles they were never trained on and are slowed down by the whole factor.
+extern "C" int32_t tg_rope_freqs(int32_t rot_dim, double base, int32_t scaling, double factor, int32_t original_len,
+                                 double low, double high, uint64_t* turns, float* attn_factor) {
+  if (!turns || !attn_factor) return fail(TG_ERR_INVALID_ARG, "NULL array");
+  if (rot_dim < 2 || rot_dim % 2) return fail(TG_ERR_INVALID_ARG, "rot_dim must be even and >= 2 (got %d)", rot_dim);
+  if (!(base > 1.0) || !std::isfinite(base)) return fail(TG_ERR_INVALID_ARG, "base must be finite and > 1");
+  if (scaling < TG_ROPE_PLAIN || scaling > TG_ROPE_YARN) return fail(TG_ERR_INVALID_ARG, "unknown scaling %d", scaling);
+  if (!(factor >= 1.0) || !std::isfinite(factor)) return fail(TG_ERR_INVALID_ARG, "factor must be finite and >= 1");
+  if (scaling == TG_ROPE_NTK && rot_dim < 4) return fail(TG_ERR_INVALID_ARG, "TG_ROPE_NTK needs rot_dim > 2");
+  const bool by_turns = scaling == TG_ROPE_BANDS || scaling == TG_ROPE_YARN;
+  if (by_turns && (original_len < 1 || !(low > 0.0) || !(high > low) || !std::isfinite(high)))
+    return fail(TG_ERR_INVALID_ARG, "scaling by turns needs original_len >= 1 and 0 < low < high");
+  const double r = rot_dim;
+  if (scaling == TG_ROPE_NTK) base *= std::pow(factor, r / (r - 2.0));
+  if (!std::isfinite(base)) return fail(TG_ERR_INVALID_ARG, "base * factor^(rot_dim / (rot_dim - 2)) is too large");
+  for (int32_t j = 0; j < rot_dim / 2; ++j) {
+    double theta = std::pow(base, -2.0 * j / r);
+    if (scaling == TG_ROPE_LINEAR) {
+      theta /= factor;
+    } else if (by_turns) {
+      const double n = original_len * theta / (2.0 * 3.14159265358979323846);
+      const double w = std::min(1.0, std::max(0.0, (n - low) / (high - low)));
+      theta = (1.0 - w) * (theta / factor) + w * theta;
+    }
+    turns[j] = turn_fraction(theta);
+  }
+  *attn_factor = scaling == TG_ROPE_YARN ? (float)(0.1 * std::log(factor) + 1.0) : 1.f;
+  return TG_OK;
+}

@@ -35,6 +35,10 @@ assert COMPRESS_ITEM_DTYPE.itemsize == 40
 TG_COMPRESS_MAX_CHUNK, TG_COMPRESS_MAX_ROWS, TG_COMPRESS_ONE_LAUNCH_MAX_CHUNK = 16384, 256, 1024
 
 
+TG_ROPE_PLAIN, TG_ROPE_LINEAR, TG_ROPE_NTK, TG_ROPE_BANDS, TG_ROPE_YARN = 0, 1, 2, 3, 4
+TG_ROPE_HALF, TG_ROPE_INTERLEAVED = 0, 1
+
+
 class TangramError(RuntimeError):
     def __init__(self, code, where, detail):
         super().__init__(f"{where}: {detail} (status {code})")
@@ -79,6 +83,43 @@ class tg_compress_args(C.Structure):
                 ("k_new", C.c_void_p), ("v_new", C.c_void_p), ("scores", C.c_void_p), ("kv_pool", C.c_void_p),
                 ("pt_pages", C.c_void_p), ("items", C.c_void_p), ("num_items", C.c_int32),
                 ("chunk_tokens", C.c_void_p), ("keep_count", C.c_void_p), ("kept", C.c_void_p)]
+
+
+class tg_rope_spec(C.Structure):
+    _fields_ = [("layout", C.c_int32), ("rot_dim", C.c_int32), ("turns", C.c_void_p), ("attn_factor", C.c_float),
+                ("norm", C.c_int32), ("eps", C.c_float), ("weight_offset", C.c_float), ("q_weight", C.c_void_p),
+                ("k_weight", C.c_void_p)]
+
+
+class tg_rope_args(C.Structure):
+    _fields_ = [("geom", tg_geometry), ("batch", C.c_int32), ("chunk_len", C.c_int32), ("dtype", C.c_int32),
+                ("spec", tg_rope_spec), ("q_in", C.c_void_p), ("k_in", C.c_void_p), ("v_in", C.c_void_p),
+                ("q_stride", C.c_int64), ("k_stride", C.c_int64), ("v_stride", C.c_int64), ("positions", C.c_void_p),
+                ("start", C.c_void_p), ("chunk_tokens", C.c_void_p), ("q_out", C.c_void_p), ("k_out", C.c_void_p),
+                ("v_out", C.c_void_p)]
+
+
+class tg_rope_append_args(C.Structure):
+    _fields_ = [("geom", tg_geometry), ("batch", C.c_int32), ("layer", C.c_int32), ("dtype", C.c_int32),
+                ("spec", tg_rope_spec), ("q_in", C.c_void_p), ("k_in", C.c_void_p), ("v_in", C.c_void_p),
+                ("q_stride", C.c_int64), ("k_stride", C.c_int64), ("v_stride", C.c_int64), ("positions", C.c_void_p),
+                ("q_out", C.c_void_p), ("kv_pool", C.c_void_p), ("pt_pages", C.c_void_p), ("pt_offsets", C.c_void_p),
+                ("group_of", C.c_void_p), ("slot_of", C.c_void_p), ("live_len", C.c_void_p), ("full", C.c_void_p)]
+
+
+class tg_reserve_device_args(C.Structure):
+    _fields_ = [("geom", tg_geometry), ("batch", C.c_int32), ("ctx_len", C.c_void_p), ("headroom", C.c_void_p),
+                ("ratio", C.c_void_p), ("budget", C.c_void_p), ("group_of", C.c_void_p), ("free_pages", C.c_void_p),
+                ("num_free", C.c_int64), ("pool_pages", C.c_int64), ("kv_len", C.c_void_p), ("group_len", C.c_void_p),
+                ("pt_offsets", C.c_void_p), ("pt_pages", C.c_void_p), ("pt_capacity", C.c_int64),
+                ("pages_needed", C.c_void_p), ("status", C.c_void_p), ("workspace", C.c_void_p),
+                ("workspace_bytes", C.c_size_t)]
+
+
+class tg_slot_map_args(C.Structure):
+    _fields_ = [("geom", tg_geometry), ("batch", C.c_int32), ("layer", C.c_int32), ("pt_offsets", C.c_void_p),
+                ("pt_pages", C.c_void_p), ("group_of", C.c_void_p), ("slot_of", C.c_void_p), ("begin", C.c_void_p),
+                ("len", C.c_void_p), ("n", C.c_int32), ("map", C.c_void_p)]
 
 
 class tg_footprint(C.Structure):
@@ -131,6 +172,13 @@ _SIGS = {
     "tg_calibrate_budget": (_i32, [_i32, _i32, _i32, _P, C.c_double, C.c_double, _P]),
     "tg_release_requests": (_i32, [_G, _i32, _P, _P, _P, _P, _i64, _P, _P, _i64, _P, _P, _P]),
     "tg_concat_tables": (_i32, [_G, _i32, _P, _P, _i32, _P, _P, _P, _P]),
+    "tg_rope_freqs": (_i32, [_i32, C.c_double, _i32, C.c_double, _i32, C.c_double, C.c_double, _P, _P]),
+    "tg_rope_turns": (_i32, [_i32, _P, _P]),
+    "tg_rope": (_i32, [C.POINTER(tg_rope_args), _P]),
+    "tg_rope_append": (_i32, [C.POINTER(tg_rope_append_args), _P]),
+    "tg_reserve_device_workspace_bytes": (_sz, [_G, _i32]),
+    "tg_reserve_device": (_i32, [C.POINTER(tg_reserve_device_args), _P]),
+    "tg_slot_map": (_i32, [C.POINTER(tg_slot_map_args), _P]),
     "tg_read_probe": (_i32, [_G, _i32, _P, _P, _P, _i64, _i32, _P, _P]),
 }
 for _name, (_res, _args) in _SIGS.items():
@@ -470,3 +518,95 @@ def tg_read_probe(geom, dtype, kv_pool, page_ids, slots, n_workers, out, stream=
     uint32/int32 tensor of n_workers checksums."""
     _check(_lib.tg_read_probe(C.byref(_geom(geom)), int(dtype), _dptr(kv_pool), _dptr(page_ids), _dptr(slots),
                               int(page_ids.numel()), int(n_workers), _dptr(out), _stream(stream)), "tg_read_probe")
+
+
+def tg_rope_freqs(rot_dim, base, scaling=TG_ROPE_PLAIN, factor=1.0, original_len=0, low=0.0, high=0.0):
+    """-> (turns [rot_dim / 2] uint64, attn_factor)."""
+    turns = np.zeros(max(1, int(rot_dim) // 2), np.uint64)
+    f = C.c_float(0)
+    _check(_lib.tg_rope_freqs(int(rot_dim), float(base), int(scaling), float(factor), int(original_len), float(low),
+                              float(high), _ptr(turns), C.byref(f)), "tg_rope_freqs")
+    return turns, f.value
+
+
+def tg_rope_turns(theta):
+    """theta float64 (radians per token) -> turns uint64."""
+    t = _host(theta, np.float64).reshape(-1)
+    turns = np.zeros(len(t), np.uint64)
+    _check(_lib.tg_rope_turns(len(t), _ptr(t), _ptr(turns)), "tg_rope_turns")
+    return turns
+
+
+def make_rope_spec(layout=TG_ROPE_HALF, rot_dim=0, turns=None, attn_factor=1.0, norm=False, eps=1e-6,
+                   weight_offset=0.0, q_weight=None, k_weight=None) -> tg_rope_spec:
+    """Packs a tg_rope_spec; turns is the device copy (8 bytes per pair) of tg_rope_freqs' result, the weights
+    [head_dim] device tensors of the call's type, or None."""
+    return tg_rope_spec(int(layout), int(rot_dim), _dptr(turns), float(attn_factor), int(norm), float(eps),
+                        float(weight_offset), _dptr(q_weight), _dptr(k_weight))
+
+
+def _token_stride(t):
+    """Elements between consecutive tokens of a [tokens][heads * d] tensor (a view of wider rows, say)."""
+    if t is None:
+        return 0
+    assert t.dim() == 2 and t.stride(1) == 1, "projection rows are [tokens][heads * d] with contiguous heads"
+    # a single row may report any stride
+    return int(t.stride(0)) if t.shape[0] > 1 else max(int(t.stride(0)), int(t.shape[1]))
+
+
+def make_rope_args(geom, batch, chunk_len, dtype, spec, q_in, k_in, v_in, q_out, k_out, v_out, positions=None,
+                   start=None, chunk_tokens=None) -> tg_rope_args:
+    """Packs a tg_rope_args from device tensors (kept alive by the caller); q_in, k_in, v_in are [B*C][heads * d],
+    views of one projection's rows or tensors of their own."""
+    return tg_rope_args(_geom(geom), int(batch), int(chunk_len), int(dtype), spec, _dptr(q_in), _dptr(k_in), _dptr(v_in),
+                        _token_stride(q_in), _token_stride(k_in), _token_stride(v_in), _dptr(positions), _dptr(start),
+                        _dptr(chunk_tokens), _dptr(q_out), _dptr(k_out), _dptr(v_out))
+
+
+def tg_rope(args: tg_rope_args, stream=None):
+    _check(_lib.tg_rope(C.byref(args), _stream(stream)), "tg_rope")
+
+
+def make_rope_append_args(geom, batch, layer, dtype, spec, q_in, k_in, v_in, positions, q_out, kv_pool, pt_pages,
+                          pt_offsets, group_of, slot_of, live_len, full=None) -> tg_rope_append_args:
+    """Packs a tg_rope_append_args from device tensors (kept alive by the caller); q_in, k_in, v_in are
+    [B][heads * d] as in make_rope_args."""
+    return tg_rope_append_args(_geom(geom), int(batch), int(layer), int(dtype), spec, _dptr(q_in), _dptr(k_in),
+                               _dptr(v_in), _token_stride(q_in), _token_stride(k_in), _token_stride(v_in),
+                               _dptr(positions), _dptr(q_out), _dptr(kv_pool), _dptr(pt_pages), _dptr(pt_offsets),
+                               _dptr(group_of), _dptr(slot_of), _dptr(live_len), _dptr(full))
+
+
+def tg_rope_append(args: tg_rope_append_args, stream=None):
+    _check(_lib.tg_rope_append(C.byref(args), _stream(stream)), "tg_rope_append")
+
+
+def tg_reserve_device_workspace_bytes(geom, batch) -> int:
+    return int(_lib.tg_reserve_device_workspace_bytes(C.byref(_geom(geom)), int(batch)))
+
+
+def make_reserve_device_args(geom, batch, ctx_len, ratio, budget, group_of, free_pages, pool_pages, kv_len, group_len,
+                             pt_offsets, pt_pages, pages_needed, status, workspace, headroom=None) -> tg_reserve_device_args:
+    """Packs a tg_reserve_device_args from device tensors (kept alive by the caller): ctx_len, headroom int32 [B];
+    ratio float64 [B][L][H] or budget float64 [L][H]; free_pages, pt_pages int32 (their lengths are num_free and
+    pt_capacity); pages_needed int64 [1], status int32 [1]."""
+    return tg_reserve_device_args(_geom(geom), int(batch), _dptr(ctx_len), _dptr(headroom), _dptr(ratio), _dptr(budget),
+                                  _dptr(group_of), _dptr(free_pages), int(free_pages.numel()), int(pool_pages),
+                                  _dptr(kv_len), _dptr(group_len), _dptr(pt_offsets), _dptr(pt_pages),
+                                  int(pt_pages.numel()), _dptr(pages_needed), _dptr(status), _dptr(workspace),
+                                  0 if workspace is None else workspace.numel() * workspace.element_size())
+
+
+def tg_reserve_device(args: tg_reserve_device_args, stream=None):
+    _check(_lib.tg_reserve_device(C.byref(args), _stream(stream)), "tg_reserve_device")
+
+
+def make_slot_map_args(geom, batch, layer, pt_offsets, pt_pages, group_of, slot_of, n, map, begin=None,
+                       len=None) -> tg_slot_map_args:
+    """Packs a tg_slot_map_args from device tensors (kept alive by the caller); map is int64 [B][H][n]."""
+    return tg_slot_map_args(_geom(geom), int(batch), int(layer), _dptr(pt_offsets), _dptr(pt_pages), _dptr(group_of),
+                            _dptr(slot_of), _dptr(begin), _dptr(len), int(n), _dptr(map))
+
+
+def tg_slot_map(args: tg_slot_map_args, stream=None):
+    _check(_lib.tg_slot_map(C.byref(args), _stream(stream)), "tg_slot_map")

@@ -1,0 +1,205 @@
+"""Rotary frequencies and the refusals of the rotary and table calls (CPU only: nothing reaches the GPU)."""
+import ctypes as C
+import math
+from fractions import Fraction
+
+import numpy as np
+import pytest
+
+from paper_2606_06302_amd import tangram as tg
+
+# 2 pi to 40 digits, as a ratio
+TWO_PI = Fraction(62831853071795864769252867665590057683943, 10 ** 40)
+
+
+def fraction_of(turns):
+    return Fraction(int(turns), 1 << 64)
+
+
+@pytest.mark.parametrize("theta", [1.0, 0.5, 1e-6, 3.3e-4, 2 * math.pi, 6.0, 7.5, 1e3, -0.25, -1e-7, 0.0, 5e-324])
+def test_turns_are_theta_over_two_pi_modulo_one(theta):
+    got = fraction_of(tg.tg_rope_turns([theta])[0])
+    want = Fraction(theta) / TWO_PI
+    want -= math.floor(want)
+    # one rounding of the quotient to 64 bits (of theta's size), one to 2^-64
+    off = abs(got - want)
+    assert min(off, 1 - off) <= Fraction(1, 1 << 64) * (1 + int(abs(theta) / 6))
+
+
+def wanted_theta(r, base, scaling, s, n0, low, high):
+    out = []
+    for j in range(r // 2):
+        if scaling == tg.TG_ROPE_NTK:
+            t = (base * s ** (r / (r - 2))) ** (-2 * j / r)
+        else:
+            t = base ** (-2 * j / r)
+        if scaling == tg.TG_ROPE_LINEAR:
+            t /= s
+        elif scaling in (tg.TG_ROPE_BANDS, tg.TG_ROPE_YARN):
+            turns = n0 * t / (2 * math.pi)
+            if turns <= low:
+                t /= s
+            elif turns < high:
+                w = (turns - low) / (high - low)
+                t = (1 - w) * t / s + w * t
+        out.append(t)
+    return np.array(out)
+
+
+@pytest.mark.parametrize("scaling", [tg.TG_ROPE_PLAIN, tg.TG_ROPE_LINEAR, tg.TG_ROPE_NTK, tg.TG_ROPE_BANDS, tg.TG_ROPE_YARN])
+@pytest.mark.parametrize("r,base,s", [(128, 500000.0, 8.0), (64, 10000.0, 1.0), (16, 1e6, 40.0), (4, 1.5, 2.0)])
+def test_frequencies(scaling, r, base, s):
+    turns, factor = tg.tg_rope_freqs(r, base, scaling, s, 8192, 1.0, 32.0 if scaling == tg.TG_ROPE_YARN else 4.0)
+    theta = wanted_theta(r, base, scaling, s, 8192, 1.0, 32.0 if scaling == tg.TG_ROPE_YARN else 4.0)
+    got = turns.astype(np.float64) / 2.0 ** 64 * 2 * math.pi
+    # fp64 powers and quotients: a few roundings of 2^-53 each, the NTK base's exponent times log(base)
+    assert np.allclose(got, theta, rtol=2e-14, atol=1e-18)
+    assert factor == pytest.approx(0.1 * math.log(s) + 1 if scaling == tg.TG_ROPE_YARN else 1.0, rel=2.0 ** -24)
+
+
+@pytest.mark.parametrize("kw", [dict(rot_dim=0), dict(rot_dim=7), dict(base=1.0), dict(base=float("nan")),
+                                dict(base=float("inf")), dict(scaling=5), dict(scaling=-1), dict(factor=0.5),
+                                dict(factor=float("nan")), dict(scaling=2, rot_dim=2),
+                                dict(scaling=3, original_len=0), dict(scaling=3, low=0.0), dict(scaling=4, low=4.0),
+                                dict(scaling=4, high=float("inf")), dict(scaling=2, base=1e300, factor=1e300)])
+def test_frequency_refusals(kw):
+    a = dict(rot_dim=64, base=10000.0, scaling=0, factor=2.0, original_len=4096, low=1.0, high=4.0)
+    a.update(kw)
+    with pytest.raises(tg.TangramError) as e:
+        tg.tg_rope_freqs(**a)
+    assert e.value.code == tg.TG_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("theta", [[], [float("nan")], [1.0, float("inf")]])
+def test_turns_refusals(theta):
+    with pytest.raises(tg.TangramError):
+        tg.tg_rope_turns(theta)
+
+
+# ------------------------------------------------- refusals of the device calls (before anything is enqueued)
+G = tg.tg_geometry(2, 4, 8, 64, 16, 2)
+FAKE = 1 << 20                     # an aligned address that is never read: every call below is refused on the host
+
+
+def spec(**kw):
+    s = dict(layout=0, rot_dim=64, turns=FAKE, attn_factor=1.0, norm=1, eps=1e-6, weight_offset=0.0, q_weight=FAKE,
+             k_weight=FAKE)
+    s.update(kw)
+    return tg.tg_rope_spec(**s)
+
+
+def rope_args(spec_kw=None, **kw):
+    a = dict(geom=G, batch=1, chunk_len=4, dtype=tg.TG_BF16, spec=spec(**(spec_kw or {})), q_in=FAKE, k_in=FAKE,
+             v_in=FAKE, q_stride=1024, k_stride=1024, v_stride=1024, q_out=FAKE, k_out=FAKE, v_out=FAKE)
+    a.update(kw)
+    return tg.tg_rope_args(**a)
+
+
+def append_args(spec_kw=None, **kw):
+    a = dict(geom=G, batch=1, layer=0, dtype=tg.TG_BF16, spec=spec(**(spec_kw or {})), q_in=FAKE, k_in=FAKE, v_in=FAKE,
+             q_stride=1024, k_stride=1024, v_stride=1024, positions=FAKE, q_out=FAKE, kv_pool=FAKE, pt_pages=FAKE,
+             pt_offsets=FAKE, group_of=FAKE, slot_of=FAKE, live_len=FAKE)
+    a.update(kw)
+    return tg.tg_rope_append_args(**a)
+
+
+INVALID, UNSUPPORTED, SMALL = tg.TG_ERR_INVALID_ARG, tg.TG_ERR_UNSUPPORTED, tg.TG_ERR_BUFFER_TOO_SMALL
+
+SPEC_REFUSALS = [(dict(layout=2), INVALID), (dict(rot_dim=-16), INVALID), (dict(rot_dim=80), INVALID),
+                 (dict(rot_dim=24), UNSUPPORTED), (dict(turns=None), INVALID), (dict(turns=FAKE + 4), INVALID),
+                 (dict(norm=2), INVALID), (dict(eps=-1.0), INVALID), (dict(eps=float("nan")), INVALID),
+                 (dict(attn_factor=float("inf")), INVALID), (dict(weight_offset=float("nan")), INVALID),
+                 (dict(q_weight=FAKE + 8), INVALID), (dict(k_weight=FAKE + 2), INVALID)]
+
+
+@pytest.mark.parametrize("kw,code", SPEC_REFUSALS)
+def test_spec_refusals(kw, code):
+    for call, args in ((tg.tg_rope, rope_args(kw)), (tg.tg_rope_append, append_args(kw))):
+        with pytest.raises(tg.TangramError) as e:
+            call(args)
+        assert e.value.code == code and tg.tg_last_error()
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(batch=0), INVALID), (dict(chunk_len=0), INVALID), (dict(dtype=7), UNSUPPORTED),
+    (dict(geom=tg.tg_geometry(2, 4, 8, 96, 16, 2)), UNSUPPORTED), (dict(geom=tg.tg_geometry(2, 4, 6, 64, 16, 2)), INVALID),
+    (dict(q_out=None), INVALID), (dict(k_in=None), INVALID), (dict(v_out=None), INVALID),
+    (dict(q_in=None, q_out=None, k_in=None, k_out=None, v_in=None, v_out=None), INVALID),
+    (dict(q_in=FAKE + 8), INVALID), (dict(k_out=FAKE + 4), INVALID), (dict(q_stride=511), INVALID),
+    (dict(k_stride=255), INVALID), (dict(v_stride=1028), INVALID), (dict(q_stride=-1024), INVALID),
+    (dict(q_stride=1 << 62), INVALID)])
+def test_rope_refusals(kw, code):
+    with pytest.raises(tg.TangramError) as e:
+        tg.tg_rope(rope_args(**kw))
+    assert e.value.code == code
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(batch=0), INVALID), (dict(layer=2), INVALID), (dict(layer=-1), INVALID), (dict(dtype=3), UNSUPPORTED),
+    (dict(q_in=None), INVALID), (dict(positions=None), INVALID), (dict(v_in=None), INVALID), (dict(kv_pool=None), INVALID),
+    (dict(live_len=None), INVALID), (dict(kv_pool=FAKE + 8), INVALID), (dict(k_stride=250), INVALID)])
+def test_rope_append_refusals(kw, code):
+    with pytest.raises(tg.TangramError) as e:
+        tg.tg_rope_append(append_args(**kw))
+    assert e.value.code == code
+
+
+def reserve_args(**kw):
+    a = dict(geom=G, batch=3, ctx_len=FAKE, ratio=FAKE, group_of=FAKE, free_pages=FAKE, num_free=100, pool_pages=100,
+             kv_len=FAKE, group_len=FAKE, pt_offsets=FAKE, pt_pages=FAKE, pt_capacity=100, pages_needed=FAKE, status=FAKE,
+             workspace=FAKE, workspace_bytes=1 << 20)
+    a.update(kw)
+    return tg.tg_reserve_device_args(**a)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(batch=0), INVALID), (dict(geom=tg.tg_geometry(2, 4, 8, 64, 16, 3)), INVALID), (dict(ctx_len=None), INVALID),
+    (dict(ratio=None), INVALID), (dict(status=None), INVALID), (dict(num_free=-1), INVALID),
+    (dict(pool_pages=-1), INVALID), (dict(pt_capacity=-1), INVALID), (dict(free_pages=None), INVALID),
+    (dict(pt_pages=None), INVALID), (dict(workspace=None), SMALL), (dict(workspace_bytes=16), SMALL),
+    (dict(workspace=FAKE + 8), INVALID)])
+def test_reserve_device_refusals(kw, code):
+    with pytest.raises(tg.TangramError) as e:
+        tg.tg_reserve_device(reserve_args(**kw))
+    assert e.value.code == code
+
+
+@pytest.mark.parametrize("kw", [dict(batch=0), dict(n=0), dict(layer=2), dict(map=None), dict(pt_pages=None),
+                                dict(batch=1 << 20)])
+def test_slot_map_refusals(kw):
+    a = dict(geom=G, batch=1, layer=0, pt_offsets=FAKE, pt_pages=FAKE, group_of=FAKE, slot_of=FAKE, n=4, map=FAKE)
+    a.update(kw)
+    with pytest.raises(tg.TangramError) as e:
+        tg.tg_slot_map(tg.tg_slot_map_args(**a))
+    assert e.value.code == INVALID
+
+
+def test_null_argument_blocks():
+    for name in ("tg_rope", "tg_rope_append", "tg_reserve_device", "tg_slot_map"):
+        assert getattr(tg._lib, name)(None, None) == INVALID
+    assert tg._lib.tg_reserve_device_workspace_bytes(None, 1) == 0
+    assert tg.tg_reserve_device_workspace_bytes(G, 0) == 0
+    assert tg._lib.tg_rope_turns(1, None, None) == INVALID
+
+
+def test_struct_layouts_match_the_header(tmp_path):
+    """sizeof / offsetof of the argument structs, by the host C compiler, against the binding's."""
+    import os
+    import shutil
+    import subprocess
+    cc = shutil.which("gcc") or shutil.which("cc")
+    if cc is None:
+        pytest.skip("no host C compiler")
+    structs = [tg.tg_rope_spec, tg.tg_rope_args, tg.tg_rope_append_args, tg.tg_reserve_device_args, tg.tg_slot_map_args]
+    lines = ['#include <stdio.h>', '#include <stddef.h>', '#include "tangram.h"', "int main(void) {"]
+    for s in structs:
+        lines.append(f'printf("%zu\\n", sizeof({s.__name__}));')
+        lines += [f'printf("%zu\\n", offsetof({s.__name__}, {f[0]}));' for f in s._fields_]
+    (tmp_path / "l.c").write_text("\n".join(lines + ["return 0; }"]))
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    subprocess.run([cc, "-std=c99", f"-I{root}/include", str(tmp_path / "l.c"), "-o", str(tmp_path / "l")], check=True)
+    got = iter(int(x) for x in subprocess.run([str(tmp_path / "l")], capture_output=True, text=True, check=True).stdout.split())
+    for s in structs:
+        assert next(got) == C.sizeof(s), s.__name__
+        for f in s._fields_:
+            assert next(got) == getattr(s, f[0]).offset, (s.__name__, f[0])
