@@ -854,6 +854,40 @@ typedef struct {
 
 int32_t tg_slot_map(const tg_slot_map_args* args, void* hip_stream);
 
+/* ------------------------------- 12. attention with modified scores and masks
+ * 12a. tg_prefill_mod: tg_prefill with
+ *   softcap: 0, or in [1e-3, 1e6]: the scores s = sm_scale * q.k become
+ *     softcap * tanh(s / softcap);
+ *   key_begin, key_end [B][C] int32 DEVICE pointers or NULL: row i of request b
+ *     sees the chunk keys j with key_begin[b][i] <= j < key_end[b][i] (clamped to
+ *     the valid tokens; the row's own index is no limit), and the whole history
+ *     where key_begin[b][i] < 0.  key_begin NULL: -1 everywhere (history and
+ *     chunk from its first key); key_end NULL: i + 1 (causal).  A prefix mask is
+ *     key_end = max(i + 1, prefix), documents packed into a chunk key_begin = the
+ *     first token of the row's document (-1 for the one that continues the
+ *     history), a window inside the chunk key_begin = i + 1 - window;
+ *   chunk_tokens [B] int32 DEVICE pointer or NULL (all C): tokens at or past
+ *     chunk_tokens[b] are no keys, and their output rows are left as they were.
+ * A row that sees no key gives zeros (so does one whose visible scores are all
+ * -inf).  What keys that a row does not see hold, NaN and infinities included,
+ * does not reach its output.
+ * The other arguments, the workspace, the schedule (whose costs count the causal
+ * tiles) and the supported shapes are tg_prefill's; sm_scale must be >= 0. */
+typedef struct {
+  float softcap;
+  const int32_t* chunk_tokens;
+  const int32_t* key_begin;
+  const int32_t* key_end;
+} tg_score_mod;
+
+int32_t tg_prefill_mod(const tg_prefill_args* args, const tg_score_mod* mod, void* hip_stream);
+
+/* 12b. tg_decode_capped: tg_decode with the scores s = sm_scale * q.k replaced
+ * by softcap * tanh(s / softcap), softcap in [1e-3, 1e6] (out, lse and the
+ * partials are those of the capped scores).  Everything else, the in-launch
+ * merge and append included, is tg_decode's; sm_scale must be >= 0. */
+int32_t tg_decode_capped(const tg_decode_args* args, float softcap, void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -135,8 +135,9 @@ struct DecodeParams {
   uint64_t* timestamps;      // [n_bins][2] start / end stamps, or NULL
   const int32_t* live;       // live lengths of this layer: live[b * live_stride + h], or NULL
   int32_t live_stride;
-  float scale_log2;          // sm_scale * log2(e)
-  float scale;               // sm_scale
+  // the kernels without / with capped scores
+  float scale_log2;          // sm_scale * log2(e)   / sm_scale / softcap
+  float scale;               // sm_scale             / softcap * log2(e)
   int32_t* merge_counters;   // [B*H] arrival counters of the in-launch merge, or NULL
   // in-launch decode-token append (open items only), or append_k == NULL
   const u4* append_k;        // [B][H] token rows, 16-byte chunks
@@ -169,16 +170,24 @@ __device__ __forceinline__ int resolve_end(int tok_begin, int tok_end, int b, in
   return resolve_open(tok_begin, tok_end, n, p.append_k != nullptr, arow);
 }
 
+// softcap * tanh(sm_scale * s / softcap) in log2 units
+__device__ __forceinline__ float cap_score(float s, const DecodeParams& p) { return p.scale * tanh_f32(s * p.scale_log2); }
+// log2 units and natural units per unit of score: capped scores are in log2 units
+template <bool kCap>
+__device__ __forceinline__ float score_log2(const DecodeParams& p) { return kCap ? 1.f : p.scale_log2; }
+template <bool kCap>
+__device__ __forceinline__ float score_nat(const DecodeParams& p) { return kCap ? kLn2 : p.scale; }
+
 __device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
 
 // End of an item: combine the per-wave states (m, l in LDS [kWaves][G],
 // accumulators at acc + w*acc_stride + g*D + e) and write the final output or
 // this chunk's fp32 partial (normalised o and its lse).  Called by the whole
 // workgroup after a barrier.
-template <typename T, int G, int D>
+template <typename T, int G, int D, bool kCap>
 __device__ __forceinline__ void finish_item(const DecodeParams& p, const tg_work_item& item, const float (*sm_m)[G],
                                             const float (*sm_l)[G], const float* acc, int acc_stride) {
-  const float cs = p.scale_log2;
+  const float cs = score_log2<kCap>(p);
   const int qh0 = item.kv_head * G;
   for (int o = threadIdx.x; o < G * D; o += kBlock) {
     const int g = o / D, e = o % D;
@@ -193,7 +202,7 @@ __device__ __forceinline__ void finish_item(const DecodeParams& p, const tg_work
       A = fmaf(acc[w * acc_stride + g * D + e], f, A);
     }
     const float O = A / L;
-    const float lse_nat = M * p.scale + logf(L);
+    const float lse_nat = M * score_nat<kCap>(p) + logf(L);
     if (item.out_idx < 0) {
       store_out<T>(static_cast<T*>(p.out) + ((int64_t)item.b * p.num_q_heads + qh0 + g) * D + e, O);
       if (p.lse && e == 0) p.lse[(int64_t)item.b * p.num_q_heads + qh0 + g] = lse_nat;
@@ -223,7 +232,7 @@ struct Tile {
   static_assert(kCPR == 8 || kCPR == 16 || kCPR == 32, "unsupported row size");
 };
 
-template <typename T, int D, int GQA>
+template <typename T, int D, int GQA, bool kCap>
 __global__ void __launch_bounds__(kBlock) tg_decode_kernel(DecodeParams p, const tg_work_item* __restrict__ items,
                                                           const int32_t* __restrict__ pt_pages,
                                                           const int32_t* __restrict__ bin_offsets,
@@ -240,7 +249,7 @@ __global__ void __launch_bounds__(kBlock) tg_decode_kernel(DecodeParams p, const
   const int c = lane % CPR;
   const int r = lane / CPR;
   const int it_begin = bin_offsets[blockIdx.x], it_end = bin_offsets[blockIdx.x + 1];
-  const float cs = p.scale_log2;
+  const float cs = score_log2<kCap>(p);
   const uint64_t t_start = __builtin_amdgcn_s_memrealtime();
 
   for (int it = it_begin; it < it_end; ++it) {
@@ -298,6 +307,7 @@ __global__ void __launch_bounds__(kBlock) tg_decode_kernel(DecodeParams p, const
           float d = chunk_dot<T>(kc[j], qv[g], 0.f);
           if constexpr (CPR == 32) d = swap16_sum(group_sum<16>(d));
           else d = group_sum<CPR>(d);
+          if constexpr (kCap) d = cap_score(d, p);
           s[j][g] = d;
         }
       }
@@ -357,7 +367,7 @@ __global__ void __launch_bounds__(kBlock) tg_decode_kernel(DecodeParams p, const
         for (int e = 0; e < EPC; ++e) sm_acc[wave][g][c * EPC + e] = acc[g][e];
     }
     __syncthreads();
-    finish_item<T, GQA, D>(p, item, sm_m, sm_l, &sm_acc[0][0][0], GQA * D);
+    finish_item<T, GQA, D, kCap>(p, item, sm_m, sm_l, &sm_acc[0][0][0], GQA * D);
     if (arow >= 0) {   // the token becomes entry arow of the cache; every thread read the length above
       if (threadIdx.x < 2 * CPR) {
         const bool is_k = threadIdx.x < CPR;
@@ -509,7 +519,7 @@ __device__ __forceinline__ s16x4 lds_read_tr16(const void* ptr) {
 // This file is built with -mllvm -amdgpu-mfma-vgpr-form: the accumulators stay
 // in VGPRs, where the rescale multiplies them in place, instead of being
 // copied between AGPRs and VGPRs on every page.
-template <int D, int QMAX>   // QMAX 8 or 16: the q slots hold up to QMAX query heads
+template <int D, int QMAX, bool kCap>   // QMAX 8 or 16: the q slots hold up to QMAX query heads
 __global__ void __launch_bounds__(kBlock) tg_decode_mfma_kernel(DecodeParams p, const tg_work_item* __restrict__ items_g,
                                                                const int32_t* __restrict__ pt_g,
                                                                const int32_t* __restrict__ bin_offsets_g,
@@ -552,7 +562,7 @@ __global__ void __launch_bounds__(kBlock) tg_decode_mfma_kernel(DecodeParams p, 
   const int col = lane & 15;            // head column of the MFMA tiles
   const int rb = lane >> 4;             // row block: tokens / dims 4rb..4rb+3
   const int hq = col < G ? col : col % G;
-  const float cs = p.scale_log2;
+  const float cs = score_log2<kCap>(p);
   const uint32_t ring_lds = lds_address(&sm_ring[wave][0][0]);
   const uint32_t q_lds = lds_address(&sm_q[wave][0][0]);
   const u4* const qsrc = static_cast<const u4*>(p.q);
@@ -708,7 +718,10 @@ __global__ void __launch_bounds__(kBlock) tg_decode_mfma_kernel(DecodeParams p, 
 #pragma unroll
       for (int c = 0; c < D / 32; ++c) s = mfma_qk(kbuf[t * kSlab + k_off + ((4 * c + rb) ^ k_swz(col))], qv[c], s);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) sv[4 * t + i] = t * kPage + 4 * rb + i < nvalid ? s[i] : -INFINITY;
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (kCap) s[i] = cap_score(s[i], p);
+        sv[4 * t + i] = t * kPage + 4 * rb + i < nvalid ? s[i] : -INFINITY;
+      }
     }
     float mx = sv[0];
 #pragma unroll
@@ -799,7 +812,7 @@ __global__ void __launch_bounds__(kBlock) tg_decode_mfma_kernel(DecodeParams p, 
     // item end: the head's sum over all 16 token rows, then normalise and store
     l = swap32_sum(swap16_sum(l));
     if (col < G) {
-      const float lse_nat = m * p.scale + logf(l);
+      const float lse_nat = m * score_nat<kCap>(p) + logf(l);
       const float inv = 1.f / l;
       if constexpr (KP == 2) {
 #pragma unroll
@@ -975,7 +988,7 @@ __global__ void __launch_bounds__(kBlock) tg_decode_mfma_kernel(DecodeParams p, 
 // passes over less (198 MB: 42, plain 38; after the caches were replaced both
 // 45).  Loading an item's queries while the item before runs, into a second
 // buffer, measured slower at 64 (14.2 -> 15.8 us at 31 MB) and level at 128.
-template <int D>
+template <int D, bool kCap>
 __global__ void __launch_bounds__(kBlock, 2) tg_decode_f32_kernel(DecodeParams p, const tg_work_item* __restrict__ items_g,
                                                                  const int32_t* __restrict__ pt_g,
                                                                  const int32_t* __restrict__ bin_offsets_g,
@@ -1004,7 +1017,7 @@ __global__ void __launch_bounds__(kBlock, 2) tg_decode_f32_kernel(DecodeParams p
   const int rb = lane >> 4;
   const int hq = col < G ? col : col % G;   // columns past G repeat a real head and are never stored
   const int it_begin = bin_offsets[blockIdx.x], it_end = bin_offsets[blockIdx.x + 1];
-  const float cs = p.scale_log2;
+  const float cs = score_log2<kCap>(p);
   const uint64_t t_start = __builtin_amdgcn_s_memrealtime();
 
   // load cursor over the pages of the bin that are this wave's
@@ -1124,7 +1137,10 @@ __global__ void __launch_bounds__(kBlock, 2) tg_decode_f32_kernel(DecodeParams p
       load_k(d, d_id);
       float sv[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) sv[i] = 4 * rb + i < nvalid ? s[0][i] : -INFINITY;
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (kCap) s[0][i] = cap_score(s[0][i], p);
+        sv[i] = 4 * rb + i < nvalid ? s[0][i] : -INFINITY;
+      }
       float mx = fmaxf(fmaxf(sv[0], sv[1]), fmaxf(sv[2], sv[3]));
       mx = swap32_max(swap16_max(mx));
       const bool raise = (mx - m) * cs > kSlack;   // rescale only when it matters: p <= 2^8
@@ -1209,7 +1225,7 @@ __global__ void __launch_bounds__(kBlock, 2) tg_decode_f32_kernel(DecodeParams p
                                            : (int64_t)item.out_idx * G + g;
       reinterpret_cast<f32x4*>(item.out_idx < 0 ? static_cast<float*>(p.out) : p.part_o)[row * CPR + c] = O;
       float* lse = item.out_idx < 0 ? p.lse : p.part_lse;
-      if (lse && c == 0) lse[row] = M * p.scale + logf(L);
+      if (lse && c == 0) lse[row] = M * score_nat<kCap>(p) + logf(L);
     }
     if (arow >= 0) {   // the token becomes entry arow of the cache; every wave read the length above
       if (threadIdx.x < 2 * CPR) {
@@ -1429,27 +1445,35 @@ bool vector_kernel_pays(int dtype, int d, int gqa, int n_bins) {
   return d == 64 && (gqa == 1 || (gqa <= 4 && n_bins <= 384));
 }
 
-template <typename T, int D>
+template <typename T, int D, bool kCap>
 DecodeFn pick_vector(int gqa) {
-  if (gqa == 1) return &tg_decode_kernel<T, D, 1>;
-  if (gqa == 2) return &tg_decode_kernel<T, D, 2>;
+  if (gqa == 1) return &tg_decode_kernel<T, D, 1, kCap>;
+  if (gqa == 2) return &tg_decode_kernel<T, D, 2, kCap>;
   if constexpr (sizeof(T) == 2) {
-    if (gqa == 4) return &tg_decode_kernel<T, D, 4>;
+    if (gqa == 4) return &tg_decode_kernel<T, D, 4, kCap>;
   }
-  return &tg_decode_kernel<T, D, 3>;
+  return &tg_decode_kernel<T, D, 3, kCap>;
 }
 
-DecodeFn pick_decode(int dtype, int d, int gqa, int n_bins) {
+template <bool kCap>
+DecodeFn pick_kernel(int dtype, int d, int gqa, int n_bins) {
   if (gqa < 1 || gqa > kMaxGqa) return nullptr;
   if (vector_kernel_pays(dtype, d, gqa, n_bins)) {
-    if (dtype == TG_BF16) return pick_vector<uint16_t, 64>(gqa);
-    return d == 64 ? pick_vector<float, 64>(gqa) : pick_vector<float, 128>(gqa);
+    if (dtype == TG_BF16) return pick_vector<uint16_t, 64, kCap>(gqa);
+    return d == 64 ? pick_vector<float, 64, kCap>(gqa) : pick_vector<float, 128, kCap>(gqa);
   }
-  if (dtype == TG_BF16 && d == 128) return gqa <= 8 ? &tg_decode_mfma_kernel<128, 8> : &tg_decode_mfma_kernel<128, 16>;
-  if (dtype == TG_BF16 && d == 64) return gqa <= 8 ? &tg_decode_mfma_kernel<64, 8> : &tg_decode_mfma_kernel<64, 16>;
-  if (dtype == TG_F32 && d == 64) return &tg_decode_f32_kernel<64>;
-  if (dtype == TG_F32 && d == 128) return &tg_decode_f32_kernel<128>;
+  if (dtype == TG_BF16 && d == 128)
+    return gqa <= 8 ? &tg_decode_mfma_kernel<128, 8, kCap> : &tg_decode_mfma_kernel<128, 16, kCap>;
+  if (dtype == TG_BF16 && d == 64)
+    return gqa <= 8 ? &tg_decode_mfma_kernel<64, 8, kCap> : &tg_decode_mfma_kernel<64, 16, kCap>;
+  if (dtype == TG_F32 && d == 64) return &tg_decode_f32_kernel<64, kCap>;
+  if (dtype == TG_F32 && d == 128) return &tg_decode_f32_kernel<128, kCap>;
   return nullptr;
+}
+
+// softcap > 0: the kernels that cap the scores
+DecodeFn pick_decode(int dtype, int d, int gqa, int n_bins, float softcap) {
+  return softcap > 0.f ? pick_kernel<true>(dtype, d, gqa, n_bins) : pick_kernel<false>(dtype, d, gqa, n_bins);
 }
 
 // whether every wave runs a bin of its own (the bf16 matrix kernel)
@@ -1523,8 +1547,8 @@ int32_t scratch_address(void** out) {
 }
 
 // tg_decode with the partials' memory passed in: ws (ws_bytes bytes) stands for
-// the caller's workspace.
-int32_t decode_impl(const tg_decode_args* a, void* ws_ptr, size_t ws_bytes, void* hip_stream) {
+// the caller's workspace; softcap > 0 caps the scores.
+int32_t decode_impl(const tg_decode_args* a, void* ws_ptr, size_t ws_bytes, float softcap, void* hip_stream) {
   if (!a) return tg::fail(TG_ERR_INVALID_ARG, "args is NULL");
   if (int32_t rc = check_decode_shape(&a->geom, a->dtype)) return rc;
   const tg_geometry& g = a->geom;
@@ -1586,9 +1610,13 @@ int32_t decode_impl(const tg_decode_args* a, void* ws_ptr, size_t ws_bytes, void
   p.merge_counters = fused_merge ? a->merge_counters : nullptr;
   p.scale = a->sm_scale != 0.f ? a->sm_scale : 1.0f / std::sqrt((float)g.head_dim);
   p.scale_log2 = p.scale * kLog2e;
+  if (softcap > 0.f) {
+    p.scale_log2 = p.scale / softcap;
+    p.scale = softcap * kLog2e;
+  }
   if (a->num_items == 0) return TG_OK;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
-  DecodeFn fn = pick_decode(a->dtype, g.head_dim, gqa, a->n_bins);
+  DecodeFn fn = pick_decode(a->dtype, g.head_dim, gqa, a->n_bins, softcap);
   const int bins = bins_per_wg(a->dtype, g.head_dim, gqa, a->n_bins);   // bins per workgroup
   const int waves = wave_per_bin(a->dtype, g.head_dim, gqa, a->n_bins) ? bins : kWaves;
   hipLaunchKernelGGL(fn, dim3((a->n_bins + bins - 1) / bins), dim3(64 * waves), 0, st, p, a->items, a->pt_pages,
@@ -1636,7 +1664,7 @@ int32_t tg_decode_max_ctas(const tg_geometry* geom, int32_t dtype, int32_t devic
   if (int32_t rc = check_decode_shape(geom, dtype)) return rc;
   // the kernel that a plan of as many bins as fit runs on
   const int gqa = geom->num_q_heads / geom->num_kv_heads;
-  DecodeFn fn = pick_decode(dtype, geom->head_dim, gqa, INT32_MAX);
+  DecodeFn fn = pick_decode(dtype, geom->head_dim, gqa, INT32_MAX, 0.f);
   int cus = 0, per_cu = 0;
   if (hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, device) != hipSuccess)
     return tg::fail(TG_ERR_HIP, "hipDeviceGetAttribute failed for device %d", device);
@@ -1652,7 +1680,13 @@ int32_t tg_decode_max_ctas(const tg_geometry* geom, int32_t dtype, int32_t devic
 
 int32_t tg_decode(const tg_decode_args* a, void* hip_stream) {
   if (!a) return tg::fail(TG_ERR_INVALID_ARG, "args is NULL");
-  return decode_impl(a, a->workspace, a->workspace_bytes, hip_stream);
+  return decode_impl(a, a->workspace, a->workspace_bytes, 0.f, hip_stream);
+}
+
+int32_t tg_decode_capped(const tg_decode_args* a, float softcap, void* hip_stream) {
+  if (!a) return tg::fail(TG_ERR_INVALID_ARG, "args is NULL");
+  if (int32_t rc = tg::check_softcap(softcap, a->sm_scale)) return rc;
+  return decode_impl(a, a->workspace, a->workspace_bytes, softcap, hip_stream);
 }
 
 int32_t tg_decode_noalloc(const tg_decode_args* a, void* hip_stream) {
@@ -1672,7 +1706,8 @@ int32_t tg_decode_noalloc(const tg_decode_args* a, void* hip_stream) {
   char* base = static_cast<char*>(ws);
   const bool counters_fit = (size_t)a->batch * a->geom.num_kv_heads * sizeof(int32_t) <= kScratchCounters;
   b.merge_counters = a->merge_counters && counters_fit ? reinterpret_cast<int32_t*>(base) : nullptr;
-  return decode_impl(&b, base + kScratchCounters, (size_t)TG_DECODE_NOALLOC_MAX_BYTES - kScratchCounters, hip_stream);
+  return decode_impl(&b, base + kScratchCounters, (size_t)TG_DECODE_NOALLOC_MAX_BYTES - kScratchCounters, 0.f,
+                     hip_stream);
 }
 
 }  // extern "C"

@@ -17,6 +17,10 @@ int32_t fail(int32_t code, const char* fmt, ...);
 // message and returns TG_ERR_INVALID_ARG.
 int32_t check_geometry(const tg_geometry* g);
 
+// Validates the score cap of the calls that take one, and their softmax scale
+// (a negative one would turn the running maximum into a minimum).
+int32_t check_softcap(float softcap, float sm_scale);
+
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // True when every pointer given is 16-byte aligned (NULL counts as aligned):

@@ -120,7 +120,31 @@ struct PrefillParams {
   int2* pieces;             // [units * row_tiles]: first partial slot and piece count of every block
   int32_t part_waves;       // waves of a block that own rows: min(8, ceil(chunk*gqa / 32))
   int32_t last_tiles;       // key tiles of the chunk that a unit's last row tile sees
+  // masked kernels only
+  const int32_t* tokens;    // [B] valid tokens of the chunk, or NULL
+  const int32_t* key_begin; // [B][C] or NULL
+  const int32_t* key_end;   // [B][C] or NULL
+  // capped kernels only: s becomes cap_log2 * tanh(s * cap_in), in log2 units, so that scale_log2 is 1 there
+  float cap_in;             // sm_scale / softcap
+  float cap_log2;           // softcap * log2(e)
+  float cap_split;          // |s| up to which the polynomial is used: kCapSplit / cap_in
 };
+
+// Masked launches (kMask).  Row i of request b sees the chunk keys [lo, hi) and
+// all of the history or none of it; the bounds of a lane's row sit in two
+// registers.  A workgroup walks the tiles that any of its rows sees, a wave
+// computes the 32-key blocks that any of its rows sees and masks those that not
+// all of them see entirely.  Keys that a row does not see get probability 0,
+// but 0 * infinity is NaN: where a masked block holds an infinite or NaN V, the
+// products take V without them, and two more sets of products count for every
+// output the visible positive and negative ones (NaN counts as both), which are
+// then added as infinities.  Rows of tokens that are no keys are cleared in LDS.
+//
+// Capped launches (kCap).  tanh costs two transcendental instructions, twice
+// what exp2 does, so the blocks whose largest |score| lets them (all, with the
+// scores of a trained model well below the cap) take an odd polynomial with
+// full-rate instructions only.
+constexpr float kCapSplit = 0.75f;
 
 // Key-split launch.  The longest block bounds a launch of few or very unequal
 // blocks: one request of 8 KV heads, chunk 512, is 64 blocks on 256 CUs, and
@@ -193,12 +217,83 @@ __device__ __forceinline__ int wave_inclusive_sum(int x) {
   return x;
 }
 
+// Least of a wave's values, in scalar registers.
+__device__ __forceinline__ int wave_min(int x) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) x = min(x, __shfl_xor(x, o));
+  return __builtin_amdgcn_readfirstlane(x);
+}
+
+// The scores of a block capped, in log2 units.
+__device__ __forceinline__ void cap_scores(f32x16& s, const PrefillParams& p) {
+  float big = 0.f;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) big = fmaxf(big, fabsf(s[r]));
+  if (!__any(big > p.cap_split)) {
+    // tanh up to kCapSplit, fitted for the smallest relative error: 5.7e-7
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const float x = s[r] * p.cap_in, u = x * x;
+      float q = fmaf(u, 0.012929632f, -0.0500563022f);
+      q = fmaf(u, q, 0.132589832f);
+      q = fmaf(u, q, -0.333282515f);
+      q = fmaf(u, q, 0.999999435f);
+      s[r] = x * p.cap_log2 * q;
+    }
+  } else {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] = p.cap_log2 * tanh_f32(s[r] * p.cap_in);
+  }
+}
+
+// Bits 15 and 31: whether the bf16 of a word's lower and upper half are infinite or NaN.
+__device__ __forceinline__ uint32_t not_finite(uint32_t w) { return ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
+// 0xffff in the halves whose bit 15 or 31 is set
+__device__ __forceinline__ uint32_t halves(uint32_t bits) { return (bits >> 15) * 0xffffu; }
+
+// One 32-dim block of a masked key block whose V holds infinities or NaN: clears
+// them in the operands and adds what the visible ones make of every output.
+__device__ __forceinline__ void add_infinities(f32x16& acc, u4& v0, u4& v1, u4& p0, u4& p1) {
+#pragma unroll
+  for (int sign = 0; sign < 2; ++sign) {
+    f32x16 n = f32x16(0.f);
+    // nothing is kept from one use for the next: registers
+    asm volatile("" : "+v"(v0), "+v"(v1), "+v"(p0), "+v"(p1));
+#pragma unroll
+    for (int q16 = 0; q16 < 2; ++q16) {
+      u4 found, seen;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const uint32_t v = q16 ? v1[w] : v0[w], pw = q16 ? p1[w] : p0[w];
+        const uint32_t odd = halves(not_finite(v));
+        const uint32_t nan = halves((((v & 0x007f007fu) + 0x007f007fu) << 8) & 0x80008000u);
+        const uint32_t neg = halves(v & 0x80008000u);
+        found[w] = 0x3f803f80u & odd & (nan | (sign ? neg : ~neg));
+        // probabilities are not negative, 0 where a key is not seen
+        seen[w] = 0x3f803f80u & halves(((pw & 0x7fff7fffu) + 0x7fff7fffu) & 0x80008000u);
+      }
+      n = mfma(found, seen, n);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[r] += n[r] > 0.f ? (sign ? -INFINITY : INFINITY) : 0.f;
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  asm volatile("" : "+v"(v0), "+v"(v1));
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    v0[w] &= ~halves(not_finite(v0[w]));
+    v1[w] &= ~halves(not_finite(v1[w]));
+  }
+  __builtin_amdgcn_sched_barrier(0);
+}
+
 // Registers: 222 and 226 (key-split) at head_dim 128, 128 at 64, none in scratch.
 // A reload from scratch would wait for every DMA in flight: with 64-bit lane
 // addresses for the DMA, six reloads a tile at head_dim 64 drained the ring
 // (five requests, chunk 333, 49.4 us against 45.1; the blocks of one request,
 // chunk 512 over 16384 tokens, 58 against 54).
-template <int D, bool kSplit, int kWavesPerSimd>
+template <int D, bool kSplit, int kWavesPerSimd, bool kMask, bool kCap>
 __global__ void __launch_bounds__(kBlock, kWavesPerSimd) tg_prefill_kernel(PrefillParams p) {
   using S = Shape<D>;
   constexpr int kChunks = S::kChunks, kDmaInst = S::kDmaInst, kDmaPerTile = S::kDmaPerTile;
@@ -208,6 +303,7 @@ __global__ void __launch_bounds__(kBlock, kWavesPerSimd) tg_prefill_kernel(Prefi
   __shared__ int64_t wave_sum[kSplit ? kWaves : 1];
   __shared__ int32_t class_groups[kSplit ? 64 : 1];
   __shared__ int32_t mine[kSplit ? 3 : 1];
+  __shared__ int32_t bounds[kMask ? kWaves : 1][3];
 
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -308,10 +404,57 @@ __global__ void __launch_bounds__(kBlock, kWavesPerSimd) tg_prefill_kernel(Prefi
   const int n_hist_tiles = (hist + kTile - 1) / kTile;
   const int row0 = rt * kRows;
   const int i_last = min(C - 1, (min(row0 + kRows, rows_total) - 1) / gqa);   // last chunk row of the block
-  const int n_tiles = n_hist_tiles + (i_last + kTile) / kTile;
+  int nh = n_hist_tiles;                          // history tiles the block walks, then chunk tiles ct0, ct0 + 1, ...
+  int ct0 = 0;
+  int n_tiles = n_hist_tiles + (i_last + kTile) / kTile;
+  // masked launch: this lane's row, and what the rows of this wave see
+  int lo = 0, hi = 0, n_valid = C;
+  bool see_hist = true, seen_row = true;
+  int w_min_lo = 0, w_max_lo = 0, w_min_hi = 0, w_max_hi = 0;
+  bool w_hist_any = true, w_hist_all = true;
+  if constexpr (kMask) {
+    static_assert(kCB == 1, "one row per lane pair");
+    if (p.tokens) n_valid = max(0, min(p.tokens[b], C));
+    const int r = row0 + wave * kRowsPerWave + (lane & 31);
+    const int i = min(r / gqa, C - 1);
+    seen_row = r < rows_total && i < n_valid;
+    lo = p.key_begin ? p.key_begin[(int64_t)b * C + i] : -1;
+    hi = min(p.key_end ? p.key_end[(int64_t)b * C + i] : i + 1, n_valid);
+    see_hist = lo < 0;
+    lo = max(lo, 0);
+    if (hi <= lo) {   // no key of the chunk: neutral for the least lo and the greatest hi
+      lo = INT32_MAX;
+      hi = 0;
+    }
+    w_min_lo = wave_min(seen_row ? lo : INT32_MAX);
+    w_max_lo = -wave_min(seen_row ? -lo : 0);
+    w_min_hi = wave_min(seen_row ? hi : INT32_MAX);
+    w_max_hi = -wave_min(seen_row ? -hi : 0);
+    w_hist_any = __any(seen_row && see_hist);
+    w_hist_all = !__any(seen_row && !see_hist);
+    if (lane == 0) {
+      bounds[wave][0] = w_min_lo;
+      bounds[wave][1] = w_max_hi;
+      bounds[wave][2] = w_hist_any;
+    }
+    __syncthreads();
+    int first = INT32_MAX, last = 0, any = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      first = min(first, bounds[w][0]);
+      last = max(last, bounds[w][1]);
+      any |= bounds[w][2];
+    }
+    first = __builtin_amdgcn_readfirstlane(first);
+    last = __builtin_amdgcn_readfirstlane(last);
+    nh = __builtin_amdgcn_readfirstlane(any) ? n_hist_tiles : 0;
+    ct0 = last > 0 ? first / kTile : 0;
+    n_tiles = nh + (last > 0 ? (last + kTile - 1) / kTile - ct0 : 0);
+  }
   int t_begin = 0, t_end = n_tiles, np = 1;
   if constexpr (kSplit) {
     np = (n_tiles + piece_tiles - 1) / piece_tiles;   // fewer than the unit's where the row tile sees less of the chunk
+    if constexpr (kMask) np = max(np, 1);             // rows that see nothing are written too
     if (piece == 0 && threadIdx.x == 0) p.pieces[unit * p.row_tiles + rt] = make_int2(first_slot * p.row_tiles + rt, np);
     if (piece >= np) return;
     t_begin = (int)((int64_t)piece * n_tiles / np);
@@ -330,7 +473,7 @@ __global__ void __launch_bounds__(kBlock, kWavesPerSimd) tg_prefill_kernel(Prefi
   const int rb0 = (wave * kDmaRows) % kPage;   // first row of the share within its page
   auto issue = [&](int t, int s) {
     const uint32_t dst = ring_lds + (uint32_t)s * kTileBytes + (uint32_t)wave * (kDmaRows * kChunks * 16);
-    if (t < n_hist_tiles) {
+    if (t < nh) {
       // past the history: any valid page, masked later
       const int pg = min(t * (kTile / kPage) + wave * kDmaRows / kPage, npages - 1);
       const int64_t id = pt_pages[tbase + pg];
@@ -343,7 +486,7 @@ __global__ void __launch_bounds__(kBlock, kWavesPerSimd) tg_prefill_kernel(Prefi
         lds_dma16(vb, r * kChunks + (pos ^ S::v_swz(r)), dst + kTile * kChunks * 16 + j * 1024);
       }
     } else {
-      const int c0 = min((t - n_hist_tiles) * kTile + wave * kDmaRows, C - 1);   // first chunk key of the share
+      const int c0 = min((kMask ? t - nh + ct0 : t - nh) * kTile + wave * kDmaRows, C - 1);   // first chunk key of the share
       const int64_t first = (((int64_t)b * C + c0) * p.num_kv_heads + h) * kChunks;
       const u4* kb = p.k_new + first;
       const u4* vb = p.v_new + first;
@@ -367,7 +510,7 @@ __global__ void __launch_bounds__(kBlock, kWavesPerSimd) tg_prefill_kernel(Prefi
     m[cb] = -INFINITY;
     l[cb] = 0.f;
   }
-  const float cs = p.scale_log2;
+  const float cs = kCap ? 1.f : p.scale_log2;
 
   // lane-constant parts of the LDS operand addresses
   const int k_row = lane & 31;                                  // A of S^T: key row kb*32 + k_row
@@ -382,7 +525,7 @@ __global__ void __launch_bounds__(kBlock, kWavesPerSimd) tg_prefill_kernel(Prefi
 #pragma unroll
   for (int cb = 0; cb < kCB; ++cb) {
     const int r = row0 + wave * kRowsPerWave + cb * 32 + (lane & 31);
-    row_ok[cb] = r < rows_total;
+    row_ok[cb] = kMask ? seen_row : r < rows_total;
     my_i[cb] = row_ok[cb] ? r / gqa : 0;
     const int j = row_ok[cb] ? r % gqa : 0;
     const u4* qp = reinterpret_cast<const u4*>(p.q + (((int64_t)b * C + my_i[cb]) * Hq + h * gqa + j) * D);
@@ -413,14 +556,26 @@ __global__ void __launch_bounds__(kBlock, kWavesPerSimd) tg_prefill_kernel(Prefi
       wait_vmcnt<kDmaPerTile>();
     else
       wait_vmcnt<0>();
-    if (t < n_hist_tiles && t * kTile + wave * kDmaRows + kDmaRows > hist) {
-      // this wave's share holds V rows past the retained history: they may
-      // hold anything (NaN included) and p = 0 does not cancel NaN, so zero them
-      u4* vq = &ring[(t - t_begin) % kRing][1][wave * kDmaRows * kChunks];
+    if constexpr (!kMask) {
+      if (t < nh && t * kTile + wave * kDmaRows + kDmaRows > hist) {
+        // this wave's share holds V rows past the retained history: they may
+        // hold anything (NaN included) and p = 0 does not cancel NaN, so zero them
+        u4* vq = &ring[(t - t_begin) % kRing][1][wave * kDmaRows * kChunks];
 #pragma unroll
-      for (int j = 0; j < kDmaInst; ++j)
-        if (t * kTile + wave * kDmaRows + j * kRowsPerDma + rl >= hist) vq[j * 64 + lane] = u4(0u);
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        for (int j = 0; j < kDmaInst; ++j)
+          if (t * kTile + wave * kDmaRows + j * kRowsPerDma + rl >= hist) vq[j * 64 + lane] = u4(0u);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      }
+    } else {   // the same, and for tokens that are no keys
+      const int first = (t < nh ? t : t - nh + ct0) * kTile + wave * kDmaRows;
+      const int end = t < nh ? hist : n_valid;
+      if (first + kDmaRows > end) {
+        u4* vq = &ring[(t - t_begin) % kRing][1][wave * kDmaRows * kChunks];
+#pragma unroll
+        for (int j = 0; j < kDmaInst; ++j)
+          if (first + j * kRowsPerDma + rl >= end) vq[j * 64 + lane] = u4(0u);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      }
     }
     barrier();   // tile t complete in LDS; every wave is done with tile t-1
     if (t + kRing - 1 < t_end) issue(t + kRing - 1, (t - t_begin + kRing - 1) % kRing);
@@ -428,15 +583,23 @@ __global__ void __launch_bounds__(kBlock, kWavesPerSimd) tg_prefill_kernel(Prefi
     const int s = (t - t_begin) % kRing;
     const unsigned char* kt = reinterpret_cast<const unsigned char*>(&ring[s][0][0]);
     const unsigned char* vt = reinterpret_cast<const unsigned char*>(&ring[s][1][0]);
-    const bool is_chunk = t >= n_hist_tiles;
-    const int key0 = is_chunk ? (t - n_hist_tiles) * kTile : t * kTile;   // first key of the tile
-    const int key_end = is_chunk ? C : hist;                                 // keys >= this are invalid
-    if (is_chunk && key0 > wave_i_max) continue;   // tile entirely in the future of this wave's rows
+    const bool is_chunk = t >= nh;
+    const int key0 = is_chunk ? (kMask ? t - nh + ct0 : t - nh) * kTile : t * kTile;   // first key of the tile
+    const int key_end = is_chunk ? C : hist;                          // keys >= this are invalid
+    if constexpr (kMask) {
+      if (is_chunk ? key0 >= w_max_hi || key0 + kTile <= w_min_lo : !w_hist_any) continue;   // no row of this wave sees it
+    } else {
+      if (is_chunk && key0 > wave_i_max) continue;   // tile entirely in the future of this wave's rows
+    }
 
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
       const int kbase = key0 + kb * 32;
-      if (is_chunk && kbase > wave_i_max) break;
+      if constexpr (kMask) {
+        if (is_chunk && (kbase >= w_max_hi || kbase + 32 <= w_min_lo)) continue;
+      } else {
+        if (is_chunk && kbase > wave_i_max) break;
+      }
       // S^T for both column blocks; the K operand is read once
       f32x16 sc[kCB];
 #pragma unroll
@@ -467,9 +630,17 @@ __global__ void __launch_bounds__(kBlock, kWavesPerSimd) tg_prefill_kernel(Prefi
       for (int kk = 0; kk < S::kK; ++kk)
 #pragma unroll
         for (int cb = 0; cb < kCB; ++cb) sc[cb] = mfma(ka[kk], qb[cb][kk], sc[cb]);
+      if constexpr (kCap) {
+#pragma unroll
+        for (int cb = 0; cb < kCB; ++cb) cap_scores(sc[cb], p);
+      }
       // only the block holding the end of the history and the chunk blocks
       // that reach past the wave's first row need a mask
-      const bool masked = is_chunk ? kbase + 31 > wave_i_min : kbase + 32 > hist;
+      bool masked;
+      if constexpr (kMask)
+        masked = is_chunk ? kbase < w_max_lo || kbase + 32 > w_min_hi : kbase + 32 > hist || !w_hist_all;
+      else
+        masked = is_chunk ? kbase + 31 > wave_i_min : kbase + 32 > hist;
       if (masked) {
 #pragma unroll
         for (int cb = 0; cb < kCB; ++cb)
@@ -477,8 +648,13 @@ __global__ void __launch_bounds__(kBlock, kWavesPerSimd) tg_prefill_kernel(Prefi
           for (int r = 0; r < 16; ++r) {
             // lane holds keys n(r) = 8*(r/4) + 4*hf + r%4 of its row
             const int key = kbase + 8 * (r >> 2) + 4 * hf + (r & 3);
-            const bool ok = key < key_end && (!is_chunk || key <= my_i[cb]);
-            sc[cb][r] = ok ? sc[cb][r] : -INFINITY;
+            if constexpr (kMask) {
+              const bool ok = is_chunk ? key >= lo && key < hi : key < hist && see_hist;
+              sc[cb][r] = ok ? sc[cb][r] : -INFINITY;
+            } else {
+              const bool ok = key < key_end && (!is_chunk || key <= my_i[cb]);
+              sc[cb][r] = ok ? sc[cb][r] : -INFINITY;
+            }
           }
       }
       u4 pb[kCB][2];
@@ -492,16 +668,16 @@ __global__ void __launch_bounds__(kBlock, kWavesPerSimd) tg_prefill_kernel(Prefi
         if (__any(raise)) {   // raise the running max (rare after the first block)
           const float m_new = raise ? mx : m[cb];
           // 0 when m was -inf, and 1, not NaN, where it still is beside a row that raises
-          const float alpha = kSplit && !raise ? 1.f : fast_exp2((m[cb] - m_new) * cs);
+          const float alpha = (kSplit || kMask) && !raise ? 1.f : fast_exp2((m[cb] - m_new) * cs);
           m[cb] = m_new;
           l[cb] *= alpha;
 #pragma unroll
           for (int d = 0; d < S::kDB; ++d) acc[cb][d] *= alpha;
         }
-        // key-split launch: a row whose scores so far are all -inf has no
+        // key-split and masked launches: a row whose scores so far are all -inf has no
         // probabilities yet, not NaN (rows past the chunk's end are such, and
         // rows that meet infinite scores first)
-        const float mcs = (kSplit && m[cb] == -INFINITY ? 0.f : m[cb]) * cs;
+        const float mcs = ((kSplit || kMask) && m[cb] == -INFINITY ? 0.f : m[cb]) * cs;
         uint32_t pw[8];
 #pragma unroll
         for (int r = 0; r < 16; r += 2) {
@@ -512,6 +688,21 @@ __global__ void __launch_bounds__(kBlock, kWavesPerSimd) tg_prefill_kernel(Prefi
         }
         pb[cb][0] = u4{pw[0], pw[1], pw[2], pw[3]};
         pb[cb][1] = u4{pw[4], pw[5], pw[6], pw[7]};
+      }
+      if constexpr (kMask) {
+        if (masked) {
+          uint32_t odd = 0;
+#pragma unroll
+          for (int q16 = 0; q16 < 2; ++q16)
+#pragma unroll
+            for (int db = 0; db < S::kDB; ++db)
+#pragma unroll
+              for (int w = 0; w < 4; ++w) odd |= not_finite(va[q16][db][w]);
+          if (__any(odd != 0)) {   // an infinite or NaN V that some row may not see
+#pragma unroll
+            for (int db = 0; db < S::kDB; ++db) add_infinities(acc[0][db], va[0][db], va[1][db], pb[0][0], pb[0][1]);
+          }
+        }
       }
       // O^T += V^T P^T over the two 16-key halves of the block
 #pragma unroll
@@ -547,7 +738,7 @@ __global__ void __launch_bounds__(kBlock, kWavesPerSimd) tg_prefill_kernel(Prefi
     if (!row_ok[cb]) continue;
     const int r = row0 + wave * kRowsPerWave + cb * 32 + (lane & 31);
     const int i = r / gqa, j = r % gqa;
-    const float inv = 1.f / lt;
+    const float inv = kMask && lt == 0.f ? 0.f : 1.f / lt;   // zeros where no key is seen
     uint16_t* orow = p.out + (((int64_t)b * C + i) * Hq + h * gqa + j) * D;
 #pragma unroll
     for (int db = 0; db < S::kDB; ++db)
@@ -567,7 +758,7 @@ __global__ void __launch_bounds__(kBlock, kWavesPerSimd) tg_prefill_kernel(Prefi
 // four consecutive dims), so partial loads are contiguous over a wave's 32
 // rows.  Bound by reading the partials back: 9 us for 220 pieces of 256 rows
 // (29 MB).
-template <int D>
+template <int D, bool kMask>
 __global__ void __launch_bounds__(256) tg_prefill_merge_kernel(PrefillParams p) {
   const int2 k = p.pieces[blockIdx.x];
   const int n = k.y;
@@ -580,6 +771,7 @@ __global__ void __launch_bounds__(256) tg_prefill_merge_kernel(PrefillParams p) 
   const int row = threadIdx.x & 31;
   const int r = rt * kRows + wave * kRowsPerWave + row;
   if (r >= p.chunk * p.gqa) return;
+  if (kMask && p.tokens && r / p.gqa >= p.tokens[b]) return;
   auto part = [&](int i) { return ((int64_t)k.x + (int64_t)i * p.row_tiles) * p.part_waves + wave; };
   constexpr int kBatch = 4;
   float M = -INFINITY, L = 0.f;
@@ -615,7 +807,7 @@ __global__ void __launch_bounds__(256) tg_prefill_merge_kernel(PrefillParams p) 
     }
     M = Mn;
   }
-  const float inv = 1.f / L;
+  const float inv = kMask && L == 0.f ? 0.f : 1.f / L;
   const int Hq = p.num_kv_heads * p.gqa;
   uint16_t* orow = p.out + (((int64_t)b * p.chunk + r / p.gqa) * Hq + h * p.gqa + r % p.gqa) * D;
   *reinterpret_cast<uint2*>(orow + 4 * chunk) =
@@ -661,16 +853,27 @@ int32_t check_prefill(const tg_prefill_args* a) {
   return TG_OK;
 }
 
-}  // namespace
+using PrefillFn = void (*)(PrefillParams);
 
-extern "C" {
-
-size_t tg_prefill_workspace_bytes(const tg_prefill_args* args) {
-  if (check_prefill(args) != TG_OK) return 0;
-  return split_layout(args->geom, args->batch, args->chunk_len).bytes;
+template <bool kSplit, bool kMask, bool kCap>
+PrefillFn pick_dim(int d) {
+  if (d == 128) return &tg_prefill_kernel<128, kSplit, 2, kMask, kCap>;
+  return &tg_prefill_kernel<64, kSplit, kSplit && !kMask ? 4 : 2, kMask, kCap>;
 }
 
-int32_t tg_prefill(const tg_prefill_args* a, void* hip_stream) {
+template <bool kSplit>
+PrefillFn pick_prefill(int d, bool mask, bool cap) {
+  if (!mask) return pick_dim<kSplit, false, false>(d);
+  return cap ? pick_dim<kSplit, true, true>(d) : pick_dim<kSplit, true, false>(d);
+}
+
+PrefillFn pick_merge(int d, bool mask) {
+  if (d == 128) return mask ? &tg_prefill_merge_kernel<128, true> : &tg_prefill_merge_kernel<128, false>;
+  return mask ? &tg_prefill_merge_kernel<64, true> : &tg_prefill_merge_kernel<64, false>;
+}
+
+// tg_prefill, or with mod tg_prefill_mod.
+int32_t prefill_impl(const tg_prefill_args* a, const tg_score_mod* mod, void* hip_stream) {
   if (int32_t rc = check_prefill(a)) return rc;
   const tg_geometry& g = a->geom;
   const int gqa = g.num_q_heads / g.num_kv_heads;
@@ -702,6 +905,20 @@ int32_t tg_prefill(const tg_prefill_args* a, void* hip_stream) {
   p.row_tiles = (a->chunk_len * gqa + kRows - 1) / kRows;
   const float scale = a->sm_scale != 0.f ? a->sm_scale : 1.0f / std::sqrt((float)g.head_dim);
   p.scale_log2 = scale * kLog2e;
+  const bool cap = mod && mod->softcap > 0.f;
+  p.tokens = p.key_begin = p.key_end = nullptr;
+  p.cap_in = p.cap_log2 = p.cap_split = 0.f;
+  if (mod) {
+    p.tokens = mod->chunk_tokens;
+    p.key_begin = mod->key_begin;
+    p.key_end = mod->key_end;
+  }
+  if (cap) {
+    p.cap_in = scale / mod->softcap;
+    p.cap_log2 = mod->softcap * kLog2e;
+    p.cap_split = kCapSplit / p.cap_in;
+    p.scale_log2 = 1.f;
+  }
   const int units = a->batch * g.num_kv_heads;
   if (a->block_order && a->num_blocks < 1) return tg::fail(TG_ERR_INVALID_ARG, "block_order needs num_blocks >= 1");
   const int blocks = a->block_order ? a->num_blocks : 8 * ((units + 7) / 8) * p.row_tiles;
@@ -714,8 +931,8 @@ int32_t tg_prefill(const tg_prefill_args* a, void* hip_stream) {
     p.pieces = reinterpret_cast<int2*>(ws + sl.o_bytes + sl.ml_bytes);
     p.part_waves = sl.part_waves;
     p.last_tiles = (a->chunk_len - 1 + kTile) / kTile;
-    auto split = g.head_dim == 128 ? tg_prefill_kernel<128, true, 2> : tg_prefill_kernel<64, true, 4>;
-    auto merge = g.head_dim == 128 ? tg_prefill_merge_kernel<128> : tg_prefill_merge_kernel<64>;
+    const PrefillFn split = pick_prefill<true>(g.head_dim, mod != nullptr, cap);
+    const PrefillFn merge = pick_merge(g.head_dim, mod != nullptr);
     hipLaunchKernelGGL(split, dim3((sl.groups + 7) / 8 * 8 * sl.row_tiles), dim3(kBlock), 0, st, p);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return tg::fail(TG_ERR_HIP, "prefill launch failed: %s", hipGetErrorString(e));
@@ -731,11 +948,30 @@ int32_t tg_prefill(const tg_prefill_args* a, void* hip_stream) {
   // requests 63 us against 65, 336 of 14 37 against 38): LDS that is not used
   // keeps the second workgroup off.
   const size_t one_per_cu = g.head_dim == 64 && blocks <= tg::kPrefillOnePerCuBlocks ? 24 << 10 : 0;
-  auto kernel = g.head_dim == 128 ? tg_prefill_kernel<128, false, 2> : tg_prefill_kernel<64, false, 2>;
+  const PrefillFn kernel = pick_prefill<false>(g.head_dim, mod != nullptr, cap);
   hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kBlock), one_per_cu, st, p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return tg::fail(TG_ERR_HIP, "prefill launch failed: %s", hipGetErrorString(e));
   return TG_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t tg_prefill_workspace_bytes(const tg_prefill_args* args) {
+  if (check_prefill(args) != TG_OK) return 0;
+  return split_layout(args->geom, args->batch, args->chunk_len).bytes;
+}
+
+int32_t tg_prefill(const tg_prefill_args* a, void* hip_stream) { return prefill_impl(a, nullptr, hip_stream); }
+
+int32_t tg_prefill_mod(const tg_prefill_args* a, const tg_score_mod* mod, void* hip_stream) {
+  if (!a) return tg::fail(TG_ERR_INVALID_ARG, "args is NULL");
+  if (!mod) return tg::fail(TG_ERR_INVALID_ARG, "mod is NULL");
+  // without a cap the check is the scale's alone
+  if (int32_t rc = tg::check_softcap(mod->softcap == 0.f ? 1.f : mod->softcap, a->sm_scale)) return rc;
+  return prefill_impl(a, mod, hip_stream);
 }
 
 }  // extern "C"

@@ -55,12 +55,55 @@ class Tables:
         return int(kv.sum()) * 2 * g.head_dim * esz
 
 
+class DeviceTables:
+    """The reservation of one workload with the block tables built on the GPU (tg_reserve_device): context lengths,
+    ratios and the free list are device tensors, and nothing comes back to the host unless asked for.
+
+    ctx_len, headroom int32 [B]; ratio float64 [B][L][H]; group_of, slot_of int32 [L][H]; free_pages int32, ids below
+    pool_pages; capacity: entries of the page array, at least what the lengths can need."""
+
+    def __init__(self, geom, ctx_len, ratio, group_of, slot_of, free_pages, pool_pages, capacity, headroom=None):
+        B, L, H, G = ctx_len.numel(), geom.num_layers, geom.num_kv_heads, geom.num_kv_heads // geom.heads_per_group
+        dev = ctx_len.device
+        self.geom, self.batch, self.device = geom, B, dev
+        self.d_group_of, self.d_slot_of = group_of, slot_of
+        self.d_kv_len = torch.zeros(B, L, H, dtype=torch.int32, device=dev)
+        self.d_group_len = torch.zeros(B, L, G, dtype=torch.int32, device=dev)
+        self.d_offsets = torch.zeros(B * L * G + 1, dtype=torch.int64, device=dev)
+        self.d_pt_pages = torch.zeros(max(1, int(capacity)), dtype=torch.int32, device=dev)
+        self.d_needed = torch.zeros(1, dtype=torch.int64, device=dev)
+        self.d_status = torch.zeros(1, dtype=torch.int32, device=dev)
+        self.workspace = torch.empty(tg.tg_reserve_device_workspace_bytes(geom, B), dtype=torch.uint8, device=dev)
+        self.inputs = (ctx_len, ratio, free_pages, headroom)
+        self.args = tg.make_reserve_device_args(geom, B, ctx_len, ratio, None, group_of, free_pages, pool_pages,
+                                                self.d_kv_len, self.d_group_len, self.d_offsets, self.d_pt_pages,
+                                                self.d_needed, self.d_status, self.workspace, headroom=headroom)
+
+    def run(self, stream=None):
+        tg.tg_reserve_device(self.args, stream)
+
+    def check(self):
+        """Waits for the tables; raises TangramError where the reservation failed."""
+        code = int(self.d_status)
+        if code != tg.TG_OK:
+            raise tg.TangramError(code, "tg_reserve_device", tg.tg_status_string(code))
+
+    def slot_map(self, layer, n, begin=None, length=None, out=None, stream=None):
+        """Pool rows of n entries per head of the layer (tg_slot_map): int64 [B][H][n]."""
+        if out is None:
+            out = torch.empty(self.batch, self.geom.num_kv_heads, n, dtype=torch.int64, device=self.device)
+        tg.tg_slot_map(tg.make_slot_map_args(self.geom, self.batch, layer, self.d_offsets, self.d_pt_pages, self.d_group_of,
+                                             self.d_slot_of, n, out, begin=begin, len=length), stream)
+        return out
+
+
 class DecodeSession:
-    """Pool, queries, outputs and per-layer plans of one decode workload."""
+    """Pool, queries, outputs and per-layer plans of one decode workload.  softcap > 0: the scores are capped
+    (tg_decode_capped)."""
 
     def __init__(self, wl, tables: Tables = None, mode=tg.TG_PLAN_AOT, n_bins=None, split_target=None,
                  fill="device", pool=None, q=None, want_lse=True, device="cuda", layers=None, open_end=False,
-                 fused_merge=False):
+                 fused_merge=False, softcap=0.0):
         from workloads import S_POOL, S_Q, device_normal_, host_pool, host_q_decode, page_elems
         g = wl.geom
         self.wl, self.device = wl, device
@@ -72,6 +115,7 @@ class DecodeSession:
         if split_target is None:
             split_target = 2 * n_bins   # measured best on the 64-layer step (bins x {1,2,4,8})
         self.mode, self.n_bins, self.split_target = mode, n_bins, split_target
+        self.softcap = float(softcap)
         # open-ended plans: every unit's last chunk runs to the live length, so that the
         # plans built here serve every later decode step (tokens appended with append_layer)
         self.open_end = open_end
@@ -211,21 +255,49 @@ class DecodeSession:
     def append_layer(self, l, stream=None):
         tg.tg_append(self.append_args[l], stream)
 
+    def enable_projection(self, spec, rows, positions):
+        """The step's queries, keys and values come as projection rows ([L][B][(Hq + 2H) * d], queries first, then keys,
+        then values) with the tokens' positions [B] int32: run_projected_step normalises, rotates and stores them
+        (tg_rope_append into self.q and the cache), then attends."""
+        assert self.open_end, "appending needs open-ended plans and live lengths"
+        g, B, dev = self.wl.geom, self.wl.batch, self.device
+        self.rows, self.positions, self.spec = rows, positions, spec
+        self.full = torch.zeros(1, dtype=torch.int32, device=dev)
+        self.d_offsets = to_device(self.t.pt_offsets, dev)
+        self.d_group_of = to_device(self.t.group_of, dev)
+        self.d_slot_of = to_device(self.t.slot_of, dev)
+        q, k = g.num_q_heads * g.head_dim, g.num_kv_heads * g.head_dim
+        self.rope_append_args = {l: tg.make_rope_append_args(
+            g, B, l, self.tg_dtype, spec, rows[l][:, :q], rows[l][:, q:q + k], rows[l][:, q + k:], positions, self.q[l],
+            self.pool, self.t.d_pt_pages, self.d_offsets, self.d_group_of, self.d_slot_of, self.live_len, self.full)
+            for l in self.layers}
+
+    def run_projected_step(self, stream=None):
+        for l in self.layers:
+            tg.tg_rope_append(self.rope_append_args[l], stream)
+            self._decode(self.dplans[l].args, stream)
+
+    def _decode(self, args, stream):
+        if self.softcap > 0:
+            tg.tg_decode_capped(args, self.softcap, stream)
+        else:
+            tg.tg_decode(args, stream)
+
     def run_decode_step(self, stream=None):
         """One decode step: per layer, the new token's K/V appended, then attention over the cache."""
         for l in self.layers:
             if self.fused_append:
-                tg.tg_decode(self.append_decode_args[l], stream)
+                self._decode(self.append_decode_args[l], stream)
             else:
                 tg.tg_append(self.append_args[l], stream)
-                tg.tg_decode(self.dplans[l].args, stream)
+                self._decode(self.dplans[l].args, stream)
 
     def run_layer(self, l, stream=None):
-        tg.tg_decode(self.dplans[l].args, stream)
+        self._decode(self.dplans[l].args, stream)
 
     def run_step(self, stream=None):
         for l in self.layers:
-            tg.tg_decode(self.dplans[l].args, stream)
+            self._decode(self.dplans[l].args, stream)
 
     def capture_step(self, stream):
         """Captures one step (every layer's decode and merge launches) into a HIP graph on
@@ -243,7 +315,7 @@ class DecodeSession:
         ts = torch.zeros(2 * dp.host["num_bins"], dtype=torch.int64, device=self.device)
         args = tg.tg_decode_args.from_buffer_copy(dp.args)
         args.timestamps = ts.data_ptr()
-        tg.tg_decode(args, stream)
+        self._decode(args, stream)
         torch.cuda.synchronize()
         return ts.view(-1, 2).cpu().numpy().astype(np.float64)
 
@@ -321,14 +393,15 @@ class PrefillSession:
     """Pool, chunk inputs and output of one chunked-prefill workload (one layer).  workspace: scratch of the key-split
     launch (a uint8 tensor of at least tg_prefill_workspace_bytes, up to 60 MB), shared by sessions whose calls run
     one after another on a stream, as a model's layers do; the session allocates its own where none, or too small a
-    one, is given."""
+    one, is given.  mod: a tg_score_mod (make_score_mod) of capped scores, masks and short chunks, whose tensors the
+    caller keeps."""
 
     def __init__(self, wl, tables: Tables = None, layer=0, fill="device", pool=None, device="cuda", schedule=True,
-                 hist_len=None, workspace=None):
+                 hist_len=None, workspace=None, mod=None):
         from workloads import S_K, S_POOL, S_Q, S_V, device_normal_, host_pool, host_prefill_inputs, page_elems
         g = wl.geom
         assert wl.chunk_len >= 1, "prefill workloads need a chunk length"
-        self.wl, self.layer, self.device = wl, layer, device
+        self.wl, self.layer, self.device, self.mod = wl, layer, device, mod
         self.t = tables if tables is not None else Tables(wl, device=device)
         # retained history rows per (b, l, h): the reserved lengths, or fewer when the
         # tables also reserve room for entries of this and later chunks
@@ -374,7 +447,10 @@ class PrefillSession:
             self.args.workspace, self.args.workspace_bytes = self.workspace.data_ptr(), ws_bytes
 
     def run(self, stream=None):
-        tg.tg_prefill(self.args, stream)
+        if self.mod is not None:
+            tg.tg_prefill_mod(self.args, self.mod, stream)
+        else:
+            tg.tg_prefill(self.args, stream)
 
     def min_hbm_bytes(self) -> int:
         """Bytes one launch must move at least: Q, each KV head's retained history and chunk K/V read once,

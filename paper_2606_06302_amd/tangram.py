@@ -122,6 +122,10 @@ class tg_slot_map_args(C.Structure):
                 ("len", C.c_void_p), ("n", C.c_int32), ("map", C.c_void_p)]
 
 
+class tg_score_mod(C.Structure):
+    _fields_ = [("softcap", C.c_float), ("chunk_tokens", C.c_void_p), ("key_begin", C.c_void_p), ("key_end", C.c_void_p)]
+
+
 class tg_footprint(C.Structure):
     _fields_ = [("full_slots", C.c_int64), ("retained_slots", C.c_int64), ("monolithic_slots", C.c_int64),
                 ("ragged_slots", C.c_int64), ("ragged_pages", C.c_int64), ("page_tables", C.c_int64)]
@@ -179,6 +183,8 @@ _SIGS = {
     "tg_reserve_device_workspace_bytes": (_sz, [_G, _i32]),
     "tg_reserve_device": (_i32, [C.POINTER(tg_reserve_device_args), _P]),
     "tg_slot_map": (_i32, [C.POINTER(tg_slot_map_args), _P]),
+    "tg_prefill_mod": (_i32, [C.POINTER(tg_prefill_args), C.POINTER(tg_score_mod), _P]),
+    "tg_decode_capped": (_i32, [C.POINTER(tg_decode_args), _f32, _P]),
     "tg_read_probe": (_i32, [_G, _i32, _P, _P, _P, _i64, _i32, _P, _P]),
 }
 for _name, (_res, _args) in _SIGS.items():
@@ -610,3 +616,17 @@ def make_slot_map_args(geom, batch, layer, pt_offsets, pt_pages, group_of, slot_
 
 def tg_slot_map(args: tg_slot_map_args, stream=None):
     _check(_lib.tg_slot_map(C.byref(args), _stream(stream)), "tg_slot_map")
+
+
+def make_score_mod(softcap=0.0, chunk_tokens=None, key_begin=None, key_end=None) -> tg_score_mod:
+    """Packs a tg_score_mod from int32 device tensors (kept alive by the caller): chunk_tokens [B], key_begin and
+    key_end [B][C]."""
+    return tg_score_mod(float(softcap), _dptr(chunk_tokens), _dptr(key_begin), _dptr(key_end))
+
+
+def tg_prefill_mod(args: tg_prefill_args, mod: tg_score_mod, stream=None):
+    _check(_lib.tg_prefill_mod(C.byref(args), C.byref(mod), _stream(stream)), "tg_prefill_mod")
+
+
+def tg_decode_capped(args: tg_decode_args, softcap, stream=None):
+    _check(_lib.tg_decode_capped(C.byref(args), float(softcap), _stream(stream)), "tg_decode_capped")
