@@ -23,7 +23,7 @@ ARCH = "gfx950"
 
 HOST_SOURCES = ["tg_host.cpp"]
 HIP_SOURCES = ["tg_decode.hip", "tg_prefill.hip", "tg_compress.hip", "tg_append.hip", "tg_probe.hip",
-               "tg_rope.hip", "tg_tables.hip"]
+               "tg_rope.hip", "tg_tables.hip", "tg_prefill_mod.hip"]
 
 HIP_FLAGS = [
     f"--offload-arch={ARCH}", "-O3", "-fPIC", "-std=c++17",
@@ -38,7 +38,8 @@ HIP_FLAGS = [
 # the online-softmax rescale multiplies them in place (AGPR accumulators are
 # copied to VGPRs and back around every rescale branch)
 HIP_EXTRA = {"tg_decode.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
-             "tg_prefill.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+             "tg_prefill.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+             "tg_prefill_mod.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 HOST_FLAGS = ["-O2", "-fPIC", "-std=c++17", "-ffp-contract=off", "-Wall", "-Wextra",
               f"-I{INCLUDE}", f"-I{CSRC}"]
 

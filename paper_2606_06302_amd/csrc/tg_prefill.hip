@@ -47,57 +47,9 @@
 
 #include <cmath>
 
-#include "tg_device.h"
-#include "tg_internal.h"
+#include "tg_prefill.h"
 
 namespace {
-
-using namespace tgd;
-
-typedef uint32_t u4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u2v __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x4_vs __attribute__((__vector_size__(4 * sizeof(__bf16))));
-typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef float f32x2 __attribute__((ext_vector_type(2)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef __bf16 bf16x2v __attribute__((ext_vector_type(2)));
-
-#define TG_CONST __attribute__((address_space(4)))
-#define TG_LDS __attribute__((address_space(3)))
-
-constexpr int kPage = 16;
-constexpr int kWaves = 8;
-constexpr int kBlock = 64 * kWaves;
-constexpr int kCB = 1;                         // 32-row MFMA column blocks per wave
-constexpr int kRowsPerWave = 32 * kCB;
-constexpr int kRows = kRowsPerWave * kWaves;   // query rows per workgroup
-constexpr int kTile = 64;                      // keys per tile = 4 pages
-static_assert(kRows == TG_PREFILL_ROWS && kTile == TG_PREFILL_TILE, "tg_prefill_schedule costs these tiles");
-constexpr int kRing = 4;                       // LDS tile buffers
-static_assert(kRing >= 2 && kRing <= 4, "the wait below covers up to two tiles in flight after the current one");
-constexpr int kDmaRows = kTile / kWaves;       // key rows each wave fetches per tile
-constexpr float kSlack = 8.0f;
-
-// Shape constants of the kernel for head_dim D (64 or 128).  A key row is
-// 2*D bytes = kChunks 16-byte chunks; one 1 KiB DMA instruction (64 lanes x
-// 16 bytes) moves kRowsPerDma rows.  LDS swizzles: chunk c of key row r of a
-// tile sits at position c ^ k_swz(r) in the K tile and c ^ v_swz(r) in the V
-// tile (r taken mod 16, which is also the row within its page), chosen so
-// that the q.k operand reads and the transposed V reads are bank-conflict free.
-template <int D>
-struct Shape {
-  static_assert(D == 64 || D == 128, "head_dim 64 or 128");
-  static constexpr int kChunks = D / 8;
-  static constexpr int kRowsPerDma = 64 / kChunks;
-  static constexpr int kDmaInst = kDmaRows / kRowsPerDma;   // 1 KiB instructions per K or V slab and wave
-  static constexpr int kDmaPerTile = 2 * kDmaInst;
-  static constexpr int kTileBytes = 2 * kTile * D * 2;      // K + V
-  static constexpr int kK = D / 16;                         // 16-deep k steps of q.k
-  static constexpr int kDB = D / 32;                        // 32-dim blocks of the output
-  __device__ static constexpr int k_swz(int r) { return D == 128 ? (r & 15) : ((r >> 1) & 7); }
-  __device__ static constexpr int v_swz(int r) { return D == 128 ? 4 * (r & 3) : 2 * (r & 3); }
-};
 
 struct PrefillParams {
   const uint16_t* q;        // [B][C][Hq][d]
@@ -120,31 +72,7 @@ struct PrefillParams {
   int2* pieces;             // [units * row_tiles]: first partial slot and piece count of every block
   int32_t part_waves;       // waves of a block that own rows: min(8, ceil(chunk*gqa / 32))
   int32_t last_tiles;       // key tiles of the chunk that a unit's last row tile sees
-  // masked kernels only
-  const int32_t* tokens;    // [B] valid tokens of the chunk, or NULL
-  const int32_t* key_begin; // [B][C] or NULL
-  const int32_t* key_end;   // [B][C] or NULL
-  // capped kernels only: s becomes cap_log2 * tanh(s * cap_in), in log2 units, so that scale_log2 is 1 there
-  float cap_in;             // sm_scale / softcap
-  float cap_log2;           // softcap * log2(e)
-  float cap_split;          // |s| up to which the polynomial is used: kCapSplit / cap_in
 };
-
-// Masked launches (kMask).  Row i of request b sees the chunk keys [lo, hi) and
-// all of the history or none of it; the bounds of a lane's row sit in two
-// registers.  A workgroup walks the tiles that any of its rows sees, a wave
-// computes the 32-key blocks that any of its rows sees and masks those that not
-// all of them see entirely.  Keys that a row does not see get probability 0,
-// but 0 * infinity is NaN: where a masked block holds an infinite or NaN V, the
-// products take V without them, and two more sets of products count for every
-// output the visible positive and negative ones (NaN counts as both), which are
-// then added as infinities.  Rows of tokens that are no keys are cleared in LDS.
-//
-// Capped launches (kCap).  tanh costs two transcendental instructions, twice
-// what exp2 does, so the blocks whose largest |score| lets them (all, with the
-// scores of a trained model well below the cap) take an odd polynomial with
-// full-rate instructions only.
-constexpr float kCapSplit = 0.75f;
 
 // Key-split launch.  The longest block bounds a launch of few or very unequal
 // blocks: one request of 8 KV heads, chunk 512, is 64 blocks on 256 CUs, and
@@ -168,44 +96,6 @@ constexpr float kCapSplit = 0.75f;
 // (tg_prefill_split_pays).
 constexpr int kSplitMinTiles = tg::kPrefillSplitMinTiles;
 static_assert(tg::kPrefillSplitMaxUnits == kBlock, "one thread per unit");
-constexpr int split_target(int d) { return tg::prefill_split_target(d); }
-// a cut unit of n tiles has at most n / T + 1 <= 2n / T pieces
-constexpr int split_slots(int d) { return 2 * split_target(d); }
-
-__device__ __forceinline__ f32x16 mfma(const u4& a, const u4& b, const f32x16& c) {
-  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0,
-                                                 0);
-}
-
-__device__ __forceinline__ uint32_t lds_address(const void* ptr) {
-  return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((const TG_LDS void*)ptr));
-}
-
-// 16 bytes per lane from global memory (a wave-uniform base plus 16 * chunk
-// bytes per lane) into LDS at m0_base + 16 * lane.  The scalar base keeps
-// 64-bit addresses out of the vector registers.
-__device__ __forceinline__ void lds_dma16(const u4* base, uint32_t chunk, uint32_t m0_base) {
-  asm volatile("global_load_lds_dwordx4 %0, %1" ::"v"(chunk * 16), "s"(base), "{m0}"(m0_base) : "memory");
-}
-
-template <int N>
-__device__ __forceinline__ void wait_vmcnt() {
-  static_assert(N >= 0 && N < 64, "vmcnt is 6 bits");
-  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
-}
-
-__device__ __forceinline__ void barrier() { asm volatile("s_barrier" ::: "memory"); }
-
-// (lo, hi) rounded to bf16 and packed into one dword (one v_cvt_pk_bf16_f32)
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{lo, hi}, bf16x2v));
-}
-
-// Lane l of each 16-lane block receives element l % 4 of the 8-byte rows
-// addressed by lanes l/4, l/4 + 4, l/4 + 8, l/4 + 12 of the block.
-__device__ __forceinline__ u2v lds_read_tr16(const void* ptr) {
-  return __builtin_bit_cast(u2v, __builtin_amdgcn_ds_read_tr16_b64_v4bf16((TG_LDS bf16x4_vs*)ptr));
-}
 
 // Inclusive sum over the lanes of a wave.
 __device__ __forceinline__ int wave_inclusive_sum(int x) {
@@ -217,83 +107,12 @@ __device__ __forceinline__ int wave_inclusive_sum(int x) {
   return x;
 }
 
-// Least of a wave's values, in scalar registers.
-__device__ __forceinline__ int wave_min(int x) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) x = min(x, __shfl_xor(x, o));
-  return __builtin_amdgcn_readfirstlane(x);
-}
-
-// The scores of a block capped, in log2 units.
-__device__ __forceinline__ void cap_scores(f32x16& s, const PrefillParams& p) {
-  float big = 0.f;
-#pragma unroll
-  for (int r = 0; r < 16; ++r) big = fmaxf(big, fabsf(s[r]));
-  if (!__any(big > p.cap_split)) {
-    // tanh up to kCapSplit, fitted for the smallest relative error: 5.7e-7
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const float x = s[r] * p.cap_in, u = x * x;
-      float q = fmaf(u, 0.012929632f, -0.0500563022f);
-      q = fmaf(u, q, 0.132589832f);
-      q = fmaf(u, q, -0.333282515f);
-      q = fmaf(u, q, 0.999999435f);
-      s[r] = x * p.cap_log2 * q;
-    }
-  } else {
-#pragma unroll
-    for (int r = 0; r < 16; ++r) s[r] = p.cap_log2 * tanh_f32(s[r] * p.cap_in);
-  }
-}
-
-// Bits 15 and 31: whether the bf16 of a word's lower and upper half are infinite or NaN.
-__device__ __forceinline__ uint32_t not_finite(uint32_t w) { return ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
-// 0xffff in the halves whose bit 15 or 31 is set
-__device__ __forceinline__ uint32_t halves(uint32_t bits) { return (bits >> 15) * 0xffffu; }
-
-// One 32-dim block of a masked key block whose V holds infinities or NaN: clears
-// them in the operands and adds what the visible ones make of every output.
-__device__ __forceinline__ void add_infinities(f32x16& acc, u4& v0, u4& v1, u4& p0, u4& p1) {
-#pragma unroll
-  for (int sign = 0; sign < 2; ++sign) {
-    f32x16 n = f32x16(0.f);
-    // nothing is kept from one use for the next: registers
-    asm volatile("" : "+v"(v0), "+v"(v1), "+v"(p0), "+v"(p1));
-#pragma unroll
-    for (int q16 = 0; q16 < 2; ++q16) {
-      u4 found, seen;
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        const uint32_t v = q16 ? v1[w] : v0[w], pw = q16 ? p1[w] : p0[w];
-        const uint32_t odd = halves(not_finite(v));
-        const uint32_t nan = halves((((v & 0x007f007fu) + 0x007f007fu) << 8) & 0x80008000u);
-        const uint32_t neg = halves(v & 0x80008000u);
-        found[w] = 0x3f803f80u & odd & (nan | (sign ? neg : ~neg));
-        // probabilities are not negative, 0 where a key is not seen
-        seen[w] = 0x3f803f80u & halves(((pw & 0x7fff7fffu) + 0x7fff7fffu) & 0x80008000u);
-      }
-      n = mfma(found, seen, n);
-      __builtin_amdgcn_sched_barrier(0);
-    }
-#pragma unroll
-    for (int r = 0; r < 16; ++r) acc[r] += n[r] > 0.f ? (sign ? -INFINITY : INFINITY) : 0.f;
-    __builtin_amdgcn_sched_barrier(0);
-  }
-  asm volatile("" : "+v"(v0), "+v"(v1));
-#pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    v0[w] &= ~halves(not_finite(v0[w]));
-    v1[w] &= ~halves(not_finite(v1[w]));
-  }
-  __builtin_amdgcn_sched_barrier(0);
-}
-
 // Registers: 222 and 226 (key-split) at head_dim 128, 128 at 64, none in scratch.
 // A reload from scratch would wait for every DMA in flight: with 64-bit lane
 // addresses for the DMA, six reloads a tile at head_dim 64 drained the ring
 // (five requests, chunk 333, 49.4 us against 45.1; the blocks of one request,
 // chunk 512 over 16384 tokens, 58 against 54).
-template <int D, bool kSplit, int kWavesPerSimd, bool kMask, bool kCap>
+template <int D, bool kSplit, int kWavesPerSimd>
 __global__ void __launch_bounds__(kBlock, kWavesPerSimd) tg_prefill_kernel(PrefillParams p) {
   using S = Shape<D>;
   constexpr int kChunks = S::kChunks, kDmaInst = S::kDmaInst, kDmaPerTile = S::kDmaPerTile;
@@ -303,7 +122,6 @@ __global__ void __launch_bounds__(kBlock, kWavesPerSimd) tg_prefill_kernel(Prefi
   __shared__ int64_t wave_sum[kSplit ? kWaves : 1];
   __shared__ int32_t class_groups[kSplit ? 64 : 1];
   __shared__ int32_t mine[kSplit ? 3 : 1];
-  __shared__ int32_t bounds[kMask ? kWaves : 1][3];
 
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -404,57 +222,10 @@ __global__ void __launch_bounds__(kBlock, kWavesPerSimd) tg_prefill_kernel(Prefi
   const int n_hist_tiles = (hist + kTile - 1) / kTile;
   const int row0 = rt * kRows;
   const int i_last = min(C - 1, (min(row0 + kRows, rows_total) - 1) / gqa);   // last chunk row of the block
-  int nh = n_hist_tiles;                          // history tiles the block walks, then chunk tiles ct0, ct0 + 1, ...
-  int ct0 = 0;
-  int n_tiles = n_hist_tiles + (i_last + kTile) / kTile;
-  // masked launch: this lane's row, and what the rows of this wave see
-  int lo = 0, hi = 0, n_valid = C;
-  bool see_hist = true, seen_row = true;
-  int w_min_lo = 0, w_max_lo = 0, w_min_hi = 0, w_max_hi = 0;
-  bool w_hist_any = true, w_hist_all = true;
-  if constexpr (kMask) {
-    static_assert(kCB == 1, "one row per lane pair");
-    if (p.tokens) n_valid = max(0, min(p.tokens[b], C));
-    const int r = row0 + wave * kRowsPerWave + (lane & 31);
-    const int i = min(r / gqa, C - 1);
-    seen_row = r < rows_total && i < n_valid;
-    lo = p.key_begin ? p.key_begin[(int64_t)b * C + i] : -1;
-    hi = min(p.key_end ? p.key_end[(int64_t)b * C + i] : i + 1, n_valid);
-    see_hist = lo < 0;
-    lo = max(lo, 0);
-    if (hi <= lo) {   // no key of the chunk: neutral for the least lo and the greatest hi
-      lo = INT32_MAX;
-      hi = 0;
-    }
-    w_min_lo = wave_min(seen_row ? lo : INT32_MAX);
-    w_max_lo = -wave_min(seen_row ? -lo : 0);
-    w_min_hi = wave_min(seen_row ? hi : INT32_MAX);
-    w_max_hi = -wave_min(seen_row ? -hi : 0);
-    w_hist_any = __any(seen_row && see_hist);
-    w_hist_all = !__any(seen_row && !see_hist);
-    if (lane == 0) {
-      bounds[wave][0] = w_min_lo;
-      bounds[wave][1] = w_max_hi;
-      bounds[wave][2] = w_hist_any;
-    }
-    __syncthreads();
-    int first = INT32_MAX, last = 0, any = 0;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      first = min(first, bounds[w][0]);
-      last = max(last, bounds[w][1]);
-      any |= bounds[w][2];
-    }
-    first = __builtin_amdgcn_readfirstlane(first);
-    last = __builtin_amdgcn_readfirstlane(last);
-    nh = __builtin_amdgcn_readfirstlane(any) ? n_hist_tiles : 0;
-    ct0 = last > 0 ? first / kTile : 0;
-    n_tiles = nh + (last > 0 ? (last + kTile - 1) / kTile - ct0 : 0);
-  }
+  const int n_tiles = n_hist_tiles + (i_last + kTile) / kTile;
   int t_begin = 0, t_end = n_tiles, np = 1;
   if constexpr (kSplit) {
     np = (n_tiles + piece_tiles - 1) / piece_tiles;   // fewer than the unit's where the row tile sees less of the chunk
-    if constexpr (kMask) np = max(np, 1);             // rows that see nothing are written too
     if (piece == 0 && threadIdx.x == 0) p.pieces[unit * p.row_tiles + rt] = make_int2(first_slot * p.row_tiles + rt, np);
     if (piece >= np) return;
     t_begin = (int)((int64_t)piece * n_tiles / np);
@@ -473,7 +244,7 @@ __global__ void __launch_bounds__(kBlock, kWavesPerSimd) tg_prefill_kernel(Prefi
   const int rb0 = (wave * kDmaRows) % kPage;   // first row of the share within its page
   auto issue = [&](int t, int s) {
     const uint32_t dst = ring_lds + (uint32_t)s * kTileBytes + (uint32_t)wave * (kDmaRows * kChunks * 16);
-    if (t < nh) {
+    if (t < n_hist_tiles) {
       // past the history: any valid page, masked later
       const int pg = min(t * (kTile / kPage) + wave * kDmaRows / kPage, npages - 1);
       const int64_t id = pt_pages[tbase + pg];
@@ -486,7 +257,7 @@ __global__ void __launch_bounds__(kBlock, kWavesPerSimd) tg_prefill_kernel(Prefi
         lds_dma16(vb, r * kChunks + (pos ^ S::v_swz(r)), dst + kTile * kChunks * 16 + j * 1024);
       }
     } else {
-      const int c0 = min((kMask ? t - nh + ct0 : t - nh) * kTile + wave * kDmaRows, C - 1);   // first chunk key of the share
+      const int c0 = min((t - n_hist_tiles) * kTile + wave * kDmaRows, C - 1);   // first chunk key of the share
       const int64_t first = (((int64_t)b * C + c0) * p.num_kv_heads + h) * kChunks;
       const u4* kb = p.k_new + first;
       const u4* vb = p.v_new + first;
@@ -510,7 +281,7 @@ __global__ void __launch_bounds__(kBlock, kWavesPerSimd) tg_prefill_kernel(Prefi
     m[cb] = -INFINITY;
     l[cb] = 0.f;
   }
-  const float cs = kCap ? 1.f : p.scale_log2;
+  const float cs = p.scale_log2;
 
   // lane-constant parts of the LDS operand addresses
   const int k_row = lane & 31;                                  // A of S^T: key row kb*32 + k_row
@@ -525,7 +296,7 @@ __global__ void __launch_bounds__(kBlock, kWavesPerSimd) tg_prefill_kernel(Prefi
 #pragma unroll
   for (int cb = 0; cb < kCB; ++cb) {
     const int r = row0 + wave * kRowsPerWave + cb * 32 + (lane & 31);
-    row_ok[cb] = kMask ? seen_row : r < rows_total;
+    row_ok[cb] = r < rows_total;
     my_i[cb] = row_ok[cb] ? r / gqa : 0;
     const int j = row_ok[cb] ? r % gqa : 0;
     const u4* qp = reinterpret_cast<const u4*>(p.q + (((int64_t)b * C + my_i[cb]) * Hq + h * gqa + j) * D);
@@ -556,26 +327,14 @@ __global__ void __launch_bounds__(kBlock, kWavesPerSimd) tg_prefill_kernel(Prefi
       wait_vmcnt<kDmaPerTile>();
     else
       wait_vmcnt<0>();
-    if constexpr (!kMask) {
-      if (t < nh && t * kTile + wave * kDmaRows + kDmaRows > hist) {
-        // this wave's share holds V rows past the retained history: they may
-        // hold anything (NaN included) and p = 0 does not cancel NaN, so zero them
-        u4* vq = &ring[(t - t_begin) % kRing][1][wave * kDmaRows * kChunks];
+    if (t < n_hist_tiles && t * kTile + wave * kDmaRows + kDmaRows > hist) {
+      // this wave's share holds V rows past the retained history: they may
+      // hold anything (NaN included) and p = 0 does not cancel NaN, so zero them
+      u4* vq = &ring[(t - t_begin) % kRing][1][wave * kDmaRows * kChunks];
 #pragma unroll
-        for (int j = 0; j < kDmaInst; ++j)
-          if (t * kTile + wave * kDmaRows + j * kRowsPerDma + rl >= hist) vq[j * 64 + lane] = u4(0u);
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      }
-    } else {   // the same, and for tokens that are no keys
-      const int first = (t < nh ? t : t - nh + ct0) * kTile + wave * kDmaRows;
-      const int end = t < nh ? hist : n_valid;
-      if (first + kDmaRows > end) {
-        u4* vq = &ring[(t - t_begin) % kRing][1][wave * kDmaRows * kChunks];
-#pragma unroll
-        for (int j = 0; j < kDmaInst; ++j)
-          if (first + j * kRowsPerDma + rl >= end) vq[j * 64 + lane] = u4(0u);
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      }
+      for (int j = 0; j < kDmaInst; ++j)
+        if (t * kTile + wave * kDmaRows + j * kRowsPerDma + rl >= hist) vq[j * 64 + lane] = u4(0u);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
     barrier();   // tile t complete in LDS; every wave is done with tile t-1
     if (t + kRing - 1 < t_end) issue(t + kRing - 1, (t - t_begin + kRing - 1) % kRing);
@@ -583,23 +342,15 @@ __global__ void __launch_bounds__(kBlock, kWavesPerSimd) tg_prefill_kernel(Prefi
     const int s = (t - t_begin) % kRing;
     const unsigned char* kt = reinterpret_cast<const unsigned char*>(&ring[s][0][0]);
     const unsigned char* vt = reinterpret_cast<const unsigned char*>(&ring[s][1][0]);
-    const bool is_chunk = t >= nh;
-    const int key0 = is_chunk ? (kMask ? t - nh + ct0 : t - nh) * kTile : t * kTile;   // first key of the tile
-    const int key_end = is_chunk ? C : hist;                          // keys >= this are invalid
-    if constexpr (kMask) {
-      if (is_chunk ? key0 >= w_max_hi || key0 + kTile <= w_min_lo : !w_hist_any) continue;   // no row of this wave sees it
-    } else {
-      if (is_chunk && key0 > wave_i_max) continue;   // tile entirely in the future of this wave's rows
-    }
+    const bool is_chunk = t >= n_hist_tiles;
+    const int key0 = is_chunk ? (t - n_hist_tiles) * kTile : t * kTile;   // first key of the tile
+    const int key_end = is_chunk ? C : hist;                                 // keys >= this are invalid
+    if (is_chunk && key0 > wave_i_max) continue;   // tile entirely in the future of this wave's rows
 
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
       const int kbase = key0 + kb * 32;
-      if constexpr (kMask) {
-        if (is_chunk && (kbase >= w_max_hi || kbase + 32 <= w_min_lo)) continue;
-      } else {
-        if (is_chunk && kbase > wave_i_max) break;
-      }
+      if (is_chunk && kbase > wave_i_max) break;
       // S^T for both column blocks; the K operand is read once
       f32x16 sc[kCB];
 #pragma unroll
@@ -630,17 +381,9 @@ __global__ void __launch_bounds__(kBlock, kWavesPerSimd) tg_prefill_kernel(Prefi
       for (int kk = 0; kk < S::kK; ++kk)
 #pragma unroll
         for (int cb = 0; cb < kCB; ++cb) sc[cb] = mfma(ka[kk], qb[cb][kk], sc[cb]);
-      if constexpr (kCap) {
-#pragma unroll
-        for (int cb = 0; cb < kCB; ++cb) cap_scores(sc[cb], p);
-      }
       // only the block holding the end of the history and the chunk blocks
       // that reach past the wave's first row need a mask
-      bool masked;
-      if constexpr (kMask)
-        masked = is_chunk ? kbase < w_max_lo || kbase + 32 > w_min_hi : kbase + 32 > hist || !w_hist_all;
-      else
-        masked = is_chunk ? kbase + 31 > wave_i_min : kbase + 32 > hist;
+      const bool masked = is_chunk ? kbase + 31 > wave_i_min : kbase + 32 > hist;
       if (masked) {
 #pragma unroll
         for (int cb = 0; cb < kCB; ++cb)
@@ -648,13 +391,8 @@ __global__ void __launch_bounds__(kBlock, kWavesPerSimd) tg_prefill_kernel(Prefi
           for (int r = 0; r < 16; ++r) {
             // lane holds keys n(r) = 8*(r/4) + 4*hf + r%4 of its row
             const int key = kbase + 8 * (r >> 2) + 4 * hf + (r & 3);
-            if constexpr (kMask) {
-              const bool ok = is_chunk ? key >= lo && key < hi : key < hist && see_hist;
-              sc[cb][r] = ok ? sc[cb][r] : -INFINITY;
-            } else {
-              const bool ok = key < key_end && (!is_chunk || key <= my_i[cb]);
-              sc[cb][r] = ok ? sc[cb][r] : -INFINITY;
-            }
+            const bool ok = key < key_end && (!is_chunk || key <= my_i[cb]);
+            sc[cb][r] = ok ? sc[cb][r] : -INFINITY;
           }
       }
       u4 pb[kCB][2];
@@ -668,16 +406,16 @@ __global__ void __launch_bounds__(kBlock, kWavesPerSimd) tg_prefill_kernel(Prefi
         if (__any(raise)) {   // raise the running max (rare after the first block)
           const float m_new = raise ? mx : m[cb];
           // 0 when m was -inf, and 1, not NaN, where it still is beside a row that raises
-          const float alpha = (kSplit || kMask) && !raise ? 1.f : fast_exp2((m[cb] - m_new) * cs);
+          const float alpha = kSplit && !raise ? 1.f : fast_exp2((m[cb] - m_new) * cs);
           m[cb] = m_new;
           l[cb] *= alpha;
 #pragma unroll
           for (int d = 0; d < S::kDB; ++d) acc[cb][d] *= alpha;
         }
-        // key-split and masked launches: a row whose scores so far are all -inf has no
+        // key-split launch: a row whose scores so far are all -inf has no
         // probabilities yet, not NaN (rows past the chunk's end are such, and
         // rows that meet infinite scores first)
-        const float mcs = ((kSplit || kMask) && m[cb] == -INFINITY ? 0.f : m[cb]) * cs;
+        const float mcs = (kSplit && m[cb] == -INFINITY ? 0.f : m[cb]) * cs;
         uint32_t pw[8];
 #pragma unroll
         for (int r = 0; r < 16; r += 2) {
@@ -688,21 +426,6 @@ __global__ void __launch_bounds__(kBlock, kWavesPerSimd) tg_prefill_kernel(Prefi
         }
         pb[cb][0] = u4{pw[0], pw[1], pw[2], pw[3]};
         pb[cb][1] = u4{pw[4], pw[5], pw[6], pw[7]};
-      }
-      if constexpr (kMask) {
-        if (masked) {
-          uint32_t odd = 0;
-#pragma unroll
-          for (int q16 = 0; q16 < 2; ++q16)
-#pragma unroll
-            for (int db = 0; db < S::kDB; ++db)
-#pragma unroll
-              for (int w = 0; w < 4; ++w) odd |= not_finite(va[q16][db][w]);
-          if (__any(odd != 0)) {   // an infinite or NaN V that some row may not see
-#pragma unroll
-            for (int db = 0; db < S::kDB; ++db) add_infinities(acc[0][db], va[0][db], va[1][db], pb[0][0], pb[0][1]);
-          }
-        }
       }
       // O^T += V^T P^T over the two 16-key halves of the block
 #pragma unroll
@@ -738,7 +461,7 @@ __global__ void __launch_bounds__(kBlock, kWavesPerSimd) tg_prefill_kernel(Prefi
     if (!row_ok[cb]) continue;
     const int r = row0 + wave * kRowsPerWave + cb * 32 + (lane & 31);
     const int i = r / gqa, j = r % gqa;
-    const float inv = kMask && lt == 0.f ? 0.f : 1.f / lt;   // zeros where no key is seen
+    const float inv = 1.f / lt;
     uint16_t* orow = p.out + (((int64_t)b * C + i) * Hq + h * gqa + j) * D;
 #pragma unroll
     for (int db = 0; db < S::kDB; ++db)
@@ -758,7 +481,7 @@ __global__ void __launch_bounds__(kBlock, kWavesPerSimd) tg_prefill_kernel(Prefi
 // four consecutive dims), so partial loads are contiguous over a wave's 32
 // rows.  Bound by reading the partials back: 9 us for 220 pieces of 256 rows
 // (29 MB).
-template <int D, bool kMask>
+template <int D>
 __global__ void __launch_bounds__(256) tg_prefill_merge_kernel(PrefillParams p) {
   const int2 k = p.pieces[blockIdx.x];
   const int n = k.y;
@@ -771,7 +494,6 @@ __global__ void __launch_bounds__(256) tg_prefill_merge_kernel(PrefillParams p) 
   const int row = threadIdx.x & 31;
   const int r = rt * kRows + wave * kRowsPerWave + row;
   if (r >= p.chunk * p.gqa) return;
-  if (kMask && p.tokens && r / p.gqa >= p.tokens[b]) return;
   auto part = [&](int i) { return ((int64_t)k.x + (int64_t)i * p.row_tiles) * p.part_waves + wave; };
   constexpr int kBatch = 4;
   float M = -INFINITY, L = 0.f;
@@ -807,73 +529,23 @@ __global__ void __launch_bounds__(256) tg_prefill_merge_kernel(PrefillParams p) 
     }
     M = Mn;
   }
-  const float inv = kMask && L == 0.f ? 0.f : 1.f / L;
+  const float inv = 1.f / L;
   const int Hq = p.num_kv_heads * p.gqa;
   uint16_t* orow = p.out + (((int64_t)b * p.chunk + r / p.gqa) * Hq + h * p.gqa + r % p.gqa) * D;
   *reinterpret_cast<uint2*>(orow + 4 * chunk) =
       make_uint2(pack_bf16(A[0] * inv, A[1] * inv), pack_bf16(A[2] * inv, A[3] * inv));
 }
 
-size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
+}  // namespace
 
-// Workspace of the key-split launch for this shape, 0 where it is not taken.
-struct SplitLayout {
-  int row_tiles, part_waves, groups;
-  size_t o_bytes, ml_bytes, bytes;
-};
+extern "C" {
 
-SplitLayout split_layout(const tg_geometry& g, int batch, int chunk_len) {
-  SplitLayout s = {};
-  const int64_t rows = (int64_t)chunk_len * (g.num_q_heads / g.num_kv_heads);
-  const int64_t row_tiles = (rows + kRows - 1) / kRows;
-  const int64_t units = (int64_t)batch * g.num_kv_heads;
-  if (units > tg::kPrefillSplitMaxUnits || units * row_tiles > tg::kPrefillSplitMaxBlocks) return s;
-  s.row_tiles = (int)row_tiles;
-  s.part_waves = (int)((rows < kRows ? rows : kRows) + 31) / 32;
-  s.groups = split_target(g.head_dim) / s.row_tiles + (int)units;   // sum over units of ceil(n / T)
-  const size_t parts = (size_t)split_slots(g.head_dim) * s.part_waves;
-  s.o_bytes = align256(parts * 32 * g.head_dim * sizeof(float));
-  s.ml_bytes = align256(parts * 64 * sizeof(float));
-  s.bytes = s.o_bytes + s.ml_bytes + align256((size_t)(units * row_tiles) * sizeof(int2));
-  return s;
+size_t tg_prefill_workspace_bytes(const tg_prefill_args* args) {
+  if (check_prefill(args) != TG_OK) return 0;
+  return split_layout(args->geom, args->batch, args->chunk_len).bytes;
 }
 
-int32_t check_prefill(const tg_prefill_args* a) {
-  if (!a) return tg::fail(TG_ERR_INVALID_ARG, "args is NULL");
-  const tg_geometry& g = a->geom;
-  if (int32_t rc = tg::check_geometry(&g)) return rc;
-  if (a->dtype != TG_BF16) return tg::fail(TG_ERR_UNSUPPORTED, "prefill supports bf16 only");
-  if (g.head_dim != 64 && g.head_dim != 128)
-    return tg::fail(TG_ERR_UNSUPPORTED, "prefill supports head_dim 64 or 128 (got %d)", g.head_dim);
-  if (g.page_size != kPage) return tg::fail(TG_ERR_UNSUPPORTED, "prefill supports page_size 16 only");
-  const int gqa = g.num_q_heads / g.num_kv_heads;
-  if (gqa < 1 || gqa > 16) return tg::fail(TG_ERR_UNSUPPORTED, "prefill supports 1..16 query heads per KV head");
-  if (a->batch < 1 || a->chunk_len < 1 || a->layer < 0 || a->layer >= g.num_layers)
-    return tg::fail(TG_ERR_INVALID_ARG, "batch and chunk_len must be >= 1, layer in range");
-  return TG_OK;
-}
-
-using PrefillFn = void (*)(PrefillParams);
-
-template <bool kSplit, bool kMask, bool kCap>
-PrefillFn pick_dim(int d) {
-  if (d == 128) return &tg_prefill_kernel<128, kSplit, 2, kMask, kCap>;
-  return &tg_prefill_kernel<64, kSplit, kSplit && !kMask ? 4 : 2, kMask, kCap>;
-}
-
-template <bool kSplit>
-PrefillFn pick_prefill(int d, bool mask, bool cap) {
-  if (!mask) return pick_dim<kSplit, false, false>(d);
-  return cap ? pick_dim<kSplit, true, true>(d) : pick_dim<kSplit, true, false>(d);
-}
-
-PrefillFn pick_merge(int d, bool mask) {
-  if (d == 128) return mask ? &tg_prefill_merge_kernel<128, true> : &tg_prefill_merge_kernel<128, false>;
-  return mask ? &tg_prefill_merge_kernel<64, true> : &tg_prefill_merge_kernel<64, false>;
-}
-
-// tg_prefill, or with mod tg_prefill_mod.
-int32_t prefill_impl(const tg_prefill_args* a, const tg_score_mod* mod, void* hip_stream) {
+int32_t tg_prefill(const tg_prefill_args* a, void* hip_stream) {
   if (int32_t rc = check_prefill(a)) return rc;
   const tg_geometry& g = a->geom;
   const int gqa = g.num_q_heads / g.num_kv_heads;
@@ -905,20 +577,6 @@ int32_t prefill_impl(const tg_prefill_args* a, const tg_score_mod* mod, void* hi
   p.row_tiles = (a->chunk_len * gqa + kRows - 1) / kRows;
   const float scale = a->sm_scale != 0.f ? a->sm_scale : 1.0f / std::sqrt((float)g.head_dim);
   p.scale_log2 = scale * kLog2e;
-  const bool cap = mod && mod->softcap > 0.f;
-  p.tokens = p.key_begin = p.key_end = nullptr;
-  p.cap_in = p.cap_log2 = p.cap_split = 0.f;
-  if (mod) {
-    p.tokens = mod->chunk_tokens;
-    p.key_begin = mod->key_begin;
-    p.key_end = mod->key_end;
-  }
-  if (cap) {
-    p.cap_in = scale / mod->softcap;
-    p.cap_log2 = mod->softcap * kLog2e;
-    p.cap_split = kCapSplit / p.cap_in;
-    p.scale_log2 = 1.f;
-  }
   const int units = a->batch * g.num_kv_heads;
   if (a->block_order && a->num_blocks < 1) return tg::fail(TG_ERR_INVALID_ARG, "block_order needs num_blocks >= 1");
   const int blocks = a->block_order ? a->num_blocks : 8 * ((units + 7) / 8) * p.row_tiles;
@@ -931,8 +589,8 @@ int32_t prefill_impl(const tg_prefill_args* a, const tg_score_mod* mod, void* hi
     p.pieces = reinterpret_cast<int2*>(ws + sl.o_bytes + sl.ml_bytes);
     p.part_waves = sl.part_waves;
     p.last_tiles = (a->chunk_len - 1 + kTile) / kTile;
-    const PrefillFn split = pick_prefill<true>(g.head_dim, mod != nullptr, cap);
-    const PrefillFn merge = pick_merge(g.head_dim, mod != nullptr);
+    auto split = g.head_dim == 128 ? tg_prefill_kernel<128, true, 2> : tg_prefill_kernel<64, true, 4>;
+    auto merge = g.head_dim == 128 ? tg_prefill_merge_kernel<128> : tg_prefill_merge_kernel<64>;
     hipLaunchKernelGGL(split, dim3((sl.groups + 7) / 8 * 8 * sl.row_tiles), dim3(kBlock), 0, st, p);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return tg::fail(TG_ERR_HIP, "prefill launch failed: %s", hipGetErrorString(e));
@@ -948,30 +606,11 @@ int32_t prefill_impl(const tg_prefill_args* a, const tg_score_mod* mod, void* hi
   // requests 63 us against 65, 336 of 14 37 against 38): LDS that is not used
   // keeps the second workgroup off.
   const size_t one_per_cu = g.head_dim == 64 && blocks <= tg::kPrefillOnePerCuBlocks ? 24 << 10 : 0;
-  const PrefillFn kernel = pick_prefill<false>(g.head_dim, mod != nullptr, cap);
+  auto kernel = g.head_dim == 128 ? tg_prefill_kernel<128, false, 2> : tg_prefill_kernel<64, false, 2>;
   hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kBlock), one_per_cu, st, p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return tg::fail(TG_ERR_HIP, "prefill launch failed: %s", hipGetErrorString(e));
   return TG_OK;
-}
-
-}  // namespace
-
-extern "C" {
-
-size_t tg_prefill_workspace_bytes(const tg_prefill_args* args) {
-  if (check_prefill(args) != TG_OK) return 0;
-  return split_layout(args->geom, args->batch, args->chunk_len).bytes;
-}
-
-int32_t tg_prefill(const tg_prefill_args* a, void* hip_stream) { return prefill_impl(a, nullptr, hip_stream); }
-
-int32_t tg_prefill_mod(const tg_prefill_args* a, const tg_score_mod* mod, void* hip_stream) {
-  if (!a) return tg::fail(TG_ERR_INVALID_ARG, "args is NULL");
-  if (!mod) return tg::fail(TG_ERR_INVALID_ARG, "mod is NULL");
-  // without a cap the check is the scale's alone
-  if (int32_t rc = tg::check_softcap(mod->softcap == 0.f ? 1.f : mod->softcap, a->sm_scale)) return rc;
-  return prefill_impl(a, mod, hip_stream);
 }
 
 }  // extern "C"

@@ -205,11 +205,11 @@ def test_prefill_longer_history_with_the_pieces_of_few_blocks(d):
 
 
 @pytest.mark.parametrize("d,gqa", [(128, 4), (64, 5)])
-@pytest.mark.parametrize("split", [False, True])
-def test_no_mask_no_cap_is_tg_prefill(d, gqa, split):
-    """Neither a cap nor a mask: tg_prefill's output bit for bit."""
+def test_no_mask_no_cap_is_tg_prefill(d, gqa):
+    """Neither a cap nor a mask: tg_prefill's output bit for bit, whatever the block order (whole blocks; the key-split
+    launches cut in different places)."""
     _gpu()
-    p = Prefill(10, 4, gqa, d, 2, 3, 200, (300, 3000), "causal", 0.0, split=split)
+    p = Prefill(10, 4, gqa, d, 2, 3, 200, (300, 3000), "causal", 0.0, split=False)
     p.s.run()
     got = p.s.out.clone()
     p.s.out.fill_(float("nan"))
