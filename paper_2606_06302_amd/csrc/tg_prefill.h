@@ -94,6 +94,8 @@ __device__ __forceinline__ u2v lds_read_tr16(const void* ptr) {
 constexpr int split_target(int d) { return tg::prefill_split_target(d); }
 // a cut unit of n tiles has at most n / T + 1 <= 2n / T pieces
 constexpr int split_slots(int d) { return 2 * split_target(d); }
+// workgroups that run at once: one per CU at head_dim 128, two at 64
+constexpr int split_at_once(int d) { return d == 128 ? 256 : 512; }
 
 size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 
@@ -119,7 +121,8 @@ SplitLayout split_layout(const tg_geometry& g, int batch, int chunk_len) {
   s.ml_bytes = align256(parts * 64 * sizeof(float));
   s.pieces_bytes = align256((size_t)(units * row_tiles) * sizeof(int2));
   // sum over blocks of ceil(n / T) entries in eight classes, each class dealt to the 8 XCDs
-  s.list_per_xcd = (split_target(g.head_dim) + (int)(units * row_tiles)) / 8 + 9;
+  const int entries = split_target(g.head_dim) + (int)(units * row_tiles);
+  s.list_per_xcd = (entries > split_at_once(g.head_dim) ? entries : split_at_once(g.head_dim)) / 8 + 9;
   s.blocks_bytes = align256((size_t)(units * row_tiles) * sizeof(int4));
   s.bytes = s.o_bytes + s.ml_bytes + s.pieces_bytes + s.blocks_bytes + align256((size_t)s.list_per_xcd * 8 * sizeof(int));
   return s;

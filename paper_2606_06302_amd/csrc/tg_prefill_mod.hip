@@ -576,6 +576,7 @@ __global__ void __launch_bounds__(kBlock, kWavesPerSimd) tg_prefill_mod_kernel(M
 // of rows.
 constexpr int kPlanBlock = 1024;
 constexpr int kPlanWaves = kPlanBlock / 64;
+constexpr int kPairLanes = 16;
 constexpr int kClasses = 8;   // 0: the pieces of cut blocks; 1..7 the other blocks by descending length
 
 __device__ __forceinline__ int wave_inclusive_sum(int x) {
@@ -587,12 +588,13 @@ __device__ __forceinline__ int wave_inclusive_sum(int x) {
   return x;
 }
 
-__global__ void __launch_bounds__(kPlanBlock) tg_prefill_mod_plan_kernel(ModParams p, int target) {
+__global__ void __launch_bounds__(kPlanBlock) tg_prefill_mod_plan_kernel(ModParams p, int target, int slots) {
   // per (request, row tile): least lo, greatest hi, whether a row sees the history
   __shared__ int32_t min_lo[tg::kPrefillSplitMaxBlocks], max_hi[tg::kPrefillSplitMaxBlocks];
   __shared__ int32_t any_hist[tg::kPrefillSplitMaxBlocks];
   __shared__ int32_t starts[tg::kPrefillSplitMaxBlocks];   // first entry (and partial slot) of every cut block
   __shared__ int64_t sums[kPlanWaves];
+  __shared__ int32_t fits[kPlanWaves];
   __shared__ int32_t counts[kClasses][kPlanWaves], in_class[kClasses];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int pairs = p.batch * p.row_tiles, blocks = pairs * p.num_kv_heads;
@@ -609,25 +611,30 @@ __global__ void __launch_bounds__(kPlanBlock) tg_prefill_mod_plan_kernel(ModPara
     hist = (int)max<int64_t>(0, min<int64_t>(len, room));
   }
   for (int i = threadIdx.x; i < p.list_len; i += kPlanBlock) p.list[i] = -1;
-  for (int i = threadIdx.x; i < pairs; i += kPlanBlock) {
-    min_lo[i] = INT32_MAX;
-    max_hi[i] = any_hist[i] = 0;
-  }
-  __syncthreads();
-  const int rows = p.batch * p.chunk;   // at most kRows * kPrefillSplitMaxBlocks
-  for (int at = threadIdx.x; at < rows; at += kPlanBlock) {
-    const int b = at / p.chunk, i = at % p.chunk;
+  // kPairLanes lanes per (request, row tile)
+  const int sub = lane % kPairLanes;
+  for (int at = threadIdx.x / kPairLanes; at < pairs; at += kPlanBlock / kPairLanes) {
+    const int b = at / p.row_tiles, rt = at % p.row_tiles;
     const int n_valid = valid_tokens(p, b);
-    const Seen s = row_sees(p, b, i, n_valid);
-    if (i >= n_valid) continue;
-    const int first = i * p.gqa / kRows, last = ((i + 1) * p.gqa - 1) / kRows;   // the row tiles of its query heads
-    for (int rt = first; rt <= last; ++rt) {
-      const int at_pair = b * p.row_tiles + rt;
-      if (s.hi > 0) {
-        atomicMin(&min_lo[at_pair], s.lo);
-        atomicMax(&max_hi[at_pair], s.hi);
-      }
-      if (s.hist) any_hist[at_pair] = 1;
+    const int last = min(n_valid - 1, ((rt + 1) * kRows - 1) / p.gqa);
+    int lo = INT32_MAX, hi = 0, seen = 0;
+#pragma unroll 4
+    for (int i = rt * kRows / p.gqa + sub; i <= last; i += kPairLanes) {
+      const Seen s = row_sees(p, b, i, n_valid);
+      lo = min(lo, s.lo);
+      hi = max(hi, s.hi);
+      seen |= s.hist;
+    }
+#pragma unroll
+    for (int o = kPairLanes / 2; o > 0; o >>= 1) {
+      lo = min(lo, __shfl_xor(lo, o));
+      hi = max(hi, __shfl_xor(hi, o));
+      seen |= __shfl_xor(seen, o);
+    }
+    if (sub == 0) {
+      min_lo[at] = lo;
+      max_hi[at] = hi;
+      any_hist[at] = seen;
     }
   }
   __syncthreads();
@@ -640,11 +647,26 @@ __global__ void __launch_bounds__(kPlanBlock) tg_prefill_mod_plan_kernel(ModPara
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) total += __shfl_xor((long long)total, o);
   if (lane == 0) sums[wave] = total;
+  if (k < blocks) starts[k] = w.n_tiles;
   __syncthreads();
   total = sums[lane % kPlanWaves];
 #pragma unroll
   for (int o = kPlanWaves / 2; o > 0; o >>= 1) total += __shfl_xor((long long)total, o);
-  const int T = (int)max<int64_t>(tg::kPrefillSplitMinTiles, (total + target - 1) / target);
+  // T: the shortest of a few that give no more pieces than run at once, so that
+  // all end together, or total / target where that is shorter: many short
+  // blocks leave their places early
+  const int fair = (int)((total + slots - 1) / slots);
+  const int try_T = max(tg::kPrefillSplitMinTiles, fair + (fair * wave + 31) / 32);   // this wave's
+  int tried = 0;
+  for (int i = lane; i < blocks; i += 64) tried += max(1, (starts[i] + try_T - 1) / try_T);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) tried += __shfl_xor(tried, o);
+  if (lane == 0) fits[wave] = tried <= slots ? try_T : INT32_MAX;
+  __syncthreads();
+  int T = fits[lane % kPlanWaves];
+#pragma unroll
+  for (int o = kPlanWaves / 2; o > 0; o >>= 1) T = min(T, __shfl_xor(T, o));
+  T = min(T, (int)max<int64_t>(tg::kPrefillSplitMinTiles, (total + target - 1) / target));
   const int np = k < blocks ? max(1, (w.n_tiles + T - 1) / T) : 0;
   const int cls = np == 0 ? -1 : np > 1 ? 0 : 7 - w.n_tiles * 6 / T;   // n_tiles <= T there
   // place of the block's first entry in its class: within the wave, then over the waves
@@ -839,7 +861,8 @@ extern "C" int32_t tg_prefill_mod(const tg_prefill_args* a, const tg_score_mod* 
     p.list = reinterpret_cast<int32_t*>(ws + sl.o_bytes + sl.ml_bytes + sl.pieces_bytes + sl.blocks_bytes);
     p.part_waves = sl.part_waves;
     p.list_len = 8 * sl.list_per_xcd;
-    hipLaunchKernelGGL(tg_prefill_mod_plan_kernel, dim3(1), dim3(kPlanBlock), 0, st, p, split_target(g.head_dim));
+    hipLaunchKernelGGL(tg_prefill_mod_plan_kernel, dim3(1), dim3(kPlanBlock), 0, st, p, split_target(g.head_dim),
+                       split_at_once(g.head_dim));
     e = hipGetLastError();
     if (e != hipSuccess) return tg::fail(TG_ERR_HIP, "prefill plan launch failed: %s", hipGetErrorString(e));
     hipLaunchKernelGGL(pick_mod<true>(g.head_dim, cap), dim3(p.list_len), dim3(kBlock), 0, st, p);
