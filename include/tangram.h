@@ -801,7 +801,8 @@ int32_t tg_rope_append(const tg_rope_append_args* args, void* hip_stream);
  *     the pages needed or taken is left as it was.
  *   workspace: tg_reserve_device_workspace_bytes(geom, batch) bytes, no
  *     initialisation needed; calls that share one must not overlap in time.
- * Errors (host): TG_ERR_INVALID_ARG, TG_ERR_BUFFER_TOO_SMALL (workspace), TG_ERR_HIP. */
+ * Supported: num_kv_heads up to 256 (else TG_ERR_UNSUPPORTED).  Errors (host):
+ * TG_ERR_INVALID_ARG, TG_ERR_BUFFER_TOO_SMALL (workspace), TG_ERR_HIP. */
 typedef struct {
   tg_geometry geom;
   int32_t batch;

@@ -3,11 +3,12 @@
 // new token per request straight into the ragged cache (tg_rope_append).
 //
 // A head is owned by D * sizeof(T) / 32 lanes, two 16-byte chunks each, so a
-// wave holds 64 / that many heads at once (8 of bf16, head_dim 128).  The lanes
-// that rotate take both members of their pairs: chunks i and i + rot_dim / 2
-// dims (half layout), or 2i and 2i + 1 (interleaved); the others take 2i and
-// 2i + 1.  Either way lane i rotates pairs i*E .. i*E + E - 1 (E values per
-// chunk), and nothing moves between lanes but the norm's sum of squares.
+// wave holds 64 / that many heads at once (8 of bf16, head_dim 128).  With
+// adjacent pairs lane i takes chunks i and i + the head's lanes; with halves the
+// lanes that rotate take both members of their pairs, chunks i and i + rot_dim / 2
+// dims, the others 2i and 2i + 1.  Nothing moves between lanes but the norm's sum
+// of squares, and the lanes of an access lie next to each other (adjacent pairs
+// with chunks 2i and 2i + 1: 44.2 us for 201 MB of f32, head_dim 64, 39.1 so).
 //
 // Angles.  turns[j] is the rotation per token as a 64-bit fraction of a turn, so
 // position * turns[j] modulo 2^64 is the angle with every whole turn dropped,
@@ -112,7 +113,7 @@ __device__ __forceinline__ void cos_sin(int32_t position, uint64_t turns, float*
 }
 
 // One wave: heads [split * passes * heads per wave, ...) of one token.
-template <typename T, int D, bool kInterleaved, bool kAppend>
+template <typename T, int D, bool kInterleaved, bool kAppend, bool kStream>
 __global__ void __launch_bounds__(kBlock) tg_rope_kernel(RopeParams p) {
   constexpr int E = Chunk<T>::kElems;
   constexpr int CPR = D / E;             // chunks per head
@@ -130,10 +131,11 @@ __global__ void __launch_bounds__(kBlock) tg_rope_kernel(RopeParams p) {
   if (p.chunk_tokens && i >= p.chunk_tokens[b]) return;
 
   const int sub = lane % LPH;
-  const int rot_lanes = p.rot_dim / (2 * E);
-  const bool turns = sub < rot_lanes;
-  const int c0 = kInterleaved || !turns ? 2 * sub : sub;
-  const int c1 = kInterleaved || !turns ? 2 * sub + 1 : sub + rot_lanes;
+  const int rot_lanes = p.rot_dim / (2 * E);   // halves: lanes that rotate; adjacent pairs: half of the chunks that do
+  const bool turns0 = kInterleaved ? sub < 2 * rot_lanes : sub < rot_lanes;         // whether the first chunk is rotated
+  const bool turns1 = kInterleaved ? sub + LPH < 2 * rot_lanes : sub < rot_lanes;   // and the second
+  const int c0 = kInterleaved || turns0 ? sub : 2 * sub;
+  const int c1 = kInterleaved ? sub + LPH : turns0 ? sub + rot_lanes : 2 * sub + 1;
 
   if (p.rot_dim > 0) {
     const int32_t position = p.positions ? p.positions[token] : (int32_t)((p.start ? (uint32_t)p.start[b] : 0u) + (uint32_t)i);
@@ -150,8 +152,11 @@ __global__ void __launch_bounds__(kBlock) tg_rope_kernel(RopeParams p) {
   float cs[E], sn[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) {
-    cs[e] = turns ? sm_cos[wave][sub * E + e] : 1.f;
-    sn[e] = turns ? sm_sin[wave][sub * E + e] : 0.f;
+    // halves: the lane's E pairs; adjacent pairs: E / 2 of each chunk
+    const int j = kInterleaved ? (e < E / 2 ? c0 : c1) * (E / 2) + e % (E / 2) : sub * E + e;
+    const bool turns = e < E / 2 ? turns0 : turns1;
+    cs[e] = turns ? sm_cos[wave][j] : 1.f;
+    sn[e] = turns ? sm_sin[wave][j] : 0.f;
   }
   const u4 one = u4(sizeof(T) == 2 ? 0x3f803f80u : 0x3f800000u);   // values of 1
   u4 wq[2], wk[2];
@@ -182,23 +187,23 @@ __global__ void __launch_bounds__(kBlock) tg_rope_kernel(RopeParams p) {
         y1[e] *= r * (off + w1[e]);
       }
     }
-    if (turns) {
-      if constexpr (kInterleaved) {
+    if constexpr (kInterleaved) {
+      auto pairs = [&](float* y, int first) {
 #pragma unroll
         for (int e = 0; e < E / 2; ++e) {
-          const float a0 = y0[2 * e], b0 = y0[2 * e + 1], a1 = y1[2 * e], b1 = y1[2 * e + 1];
-          y0[2 * e] = fmaf(a0, cs[e], -(b0 * sn[e]));
-          y0[2 * e + 1] = fmaf(b0, cs[e], a0 * sn[e]);
-          y1[2 * e] = fmaf(a1, cs[E / 2 + e], -(b1 * sn[E / 2 + e]));
-          y1[2 * e + 1] = fmaf(b1, cs[E / 2 + e], a1 * sn[E / 2 + e]);
+          const float a = y[2 * e], bb = y[2 * e + 1];
+          y[2 * e] = fmaf(a, cs[first + e], -(bb * sn[first + e]));
+          y[2 * e + 1] = fmaf(bb, cs[first + e], a * sn[first + e]);
         }
-      } else {
+      };
+      if (turns0) pairs(y0, 0);
+      if (turns1) pairs(y1, E / 2);
+    } else if (turns0) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const float a = y0[e], bb = y1[e];
-          y0[e] = fmaf(a, cs[e], -(bb * sn[e]));
-          y1[e] = fmaf(bb, cs[e], a * sn[e]);
-        }
+      for (int e = 0; e < E; ++e) {
+        const float a = y0[e], bb = y1[e];
+        y0[e] = fmaf(a, cs[e], -(bb * sn[e]));
+        y1[e] = fmaf(bb, cs[e], a * sn[e]);
       }
     }
     x[0] = Chunk<T>::pack(y0);
@@ -252,26 +257,35 @@ __global__ void __launch_bounds__(kBlock) tg_rope_kernel(RopeParams p) {
                                   : p.k_in + token * p.k_stride + (int64_t)kh * CPR;
       u4* dst = is_q ? p.q_out + (token * p.Hq + unit) * CPR
                      : is_v ? p.v_out + (token * (p.units - p.Hq - p.H) + vh) * CPR : p.k_out + (token * p.H + kh) * CPR;
-      u4 x[2] = {src[c0], src[c1]};
+      u4 x[2];
+      if constexpr (kStream) {
+        x[0] = __builtin_nontemporal_load(src + c0);
+        x[1] = __builtin_nontemporal_load(src + c1);
+      } else {
+        x[0] = src[c0];
+        x[1] = src[c1];
+      }
       const u4 raw[2] = {x[0], x[1]};
       turn(x, !is_q);
-      dst[c0] = is_v ? raw[0] : x[0];
-      dst[c1] = is_v ? raw[1] : x[1];
+      __builtin_nontemporal_store(is_v ? raw[0] : x[0], dst + c0);
+      __builtin_nontemporal_store(is_v ? raw[1] : x[1], dst + c1);
     }
   }
 }
 
 using RopeFn = void (*)(RopeParams);
 
-template <typename T, int D, bool kAppend>
+template <typename T, int D, bool kAppend, bool kStream>
 RopeFn pick_layout(int layout) {
-  return layout == TG_ROPE_INTERLEAVED ? &tg_rope_kernel<T, D, true, kAppend> : &tg_rope_kernel<T, D, false, kAppend>;
+  return layout == TG_ROPE_INTERLEAVED ? &tg_rope_kernel<T, D, true, kAppend, kStream>
+                                       : &tg_rope_kernel<T, D, false, kAppend, kStream>;
 }
 
-template <bool kAppend>
+template <bool kAppend, bool kStream>
 RopeFn pick_rope(int dtype, int d, int layout) {
-  if (dtype == TG_F32) return d == 64 ? pick_layout<float, 64, kAppend>(layout) : pick_layout<float, 128, kAppend>(layout);
-  return d == 64 ? pick_layout<uint16_t, 64, kAppend>(layout) : pick_layout<uint16_t, 128, kAppend>(layout);
+  if (dtype == TG_F32)
+    return d == 64 ? pick_layout<float, 64, kAppend, kStream>(layout) : pick_layout<float, 128, kAppend, kStream>(layout);
+  return d == 64 ? pick_layout<uint16_t, 64, kAppend, kStream>(layout) : pick_layout<uint16_t, 128, kAppend, kStream>(layout);
 }
 
 int32_t check_spec(const tg_rope_spec& s, int d) {
@@ -375,7 +389,14 @@ extern "C" int32_t tg_rope(const tg_rope_args* a, void* hip_stream) {
   p.Hq = a->q_in ? g.num_q_heads : 0;
   p.H = a->k_in ? g.num_kv_heads : 0;
   p.units = p.Hq + p.H + (a->v_in ? g.num_kv_heads : 0);
-  return launch(pick_rope<false>(a->dtype, g.head_dim, a->spec.layout), p, heads_per_wave(a->dtype, g.head_dim),
+  // Loads that leave nothing in the caches pay once input and output together
+  // no longer fit them (256 MB): 201 MB 40.6 -> 38.1 us, but 151 MB 27.4 -> 31.0, 50 MB
+  // 10.8 -> 11.0.  Stores that leave nothing pay at any size (201 MB 43.9 -> 40.6,
+  // 101 MB 22.3 -> 18.4, 50 MB level, 13 MB 4.9 -> 4.3).
+  const bool stream = 2 * p.tokens * p.units * g.head_dim * esz > ((int64_t)176 << 20);
+  const RopeFn fn = stream ? pick_rope<false, true>(a->dtype, g.head_dim, a->spec.layout)
+                           : pick_rope<false, false>(a->dtype, g.head_dim, a->spec.layout);
+  return launch(fn, p, heads_per_wave(a->dtype, g.head_dim),
                 static_cast<hipStream_t>(hip_stream), "rope");
 }
 
@@ -425,6 +446,6 @@ extern "C" int32_t tg_rope_append(const tg_rope_append_args* a, void* hip_stream
   p.Hp = g.heads_per_group;
   p.P = g.page_size;
   p.layer = a->layer;
-  return launch(pick_rope<true>(a->dtype, g.head_dim, a->spec.layout), p, heads_per_wave(a->dtype, g.head_dim),
+  return launch(pick_rope<true, false>(a->dtype, g.head_dim, a->spec.layout), p, heads_per_wave(a->dtype, g.head_dim),
                 static_cast<hipStream_t>(hip_stream), "rope append");
 }

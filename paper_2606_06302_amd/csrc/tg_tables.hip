@@ -2,17 +2,19 @@
 // 4.2.3 of arXiv 2606.06302) from lengths that are on the device, and the pool
 // rows of one layer's entries.
 //
-// tg_reserve_device is three launches on one stream:
-//   lengths  one thread per (request, layer, group) table: kv_len = ceil(r * N)
-//            (one fp64 multiply, as on the host) of the group's heads, their
-//            maximum, the table's pages; a sum and the errors of every workgroup
-//   pages    the needed front of the free list copied and its ids checked, by
-//            all workgroups alike: a table's pages are its share of that front,
-//            whatever its length
-//   offsets  every workgroup adds up the workgroups' sums before its own, then
-//            scans its tables; or, after an error anywhere, writes zeros
-// Every value is written by one workgroup and read only by later launches: no
-// atomics, no order that the result could depend on.
+// tg_reserve_device is two launches on one stream:
+//   lengths  a workgroup per kBlock heads: kv_len = ceil(r * N) (one fp64
+//            multiply, as on the host), the groups' maxima in LDS, their pages; a
+//            sum and the errors of every workgroup.  Beside them, workgroups that
+//            look through as much of the free list as could be taken for the
+//            first id outside the pool: what is needed is not known yet
+//   tables   every workgroup adds up the sums before its own and scans its
+//            tables' pages, and all copy the needed front of the free list (a
+//            table's pages are its share of that front, whatever its length);
+//            after an error anywhere the offsets are zeros and nothing is copied
+// Small admissions take one launch of one workgroup that does all of it.
+// Every value is written by one workgroup and read only by a later launch: no
+// atomics on global memory, no order that the result could depend on.
 #include <hip/hip_runtime.h>
 
 #include "tg_internal.h"
@@ -20,9 +22,15 @@
 namespace {
 
 constexpr int kBlock = 256;
-constexpr int kWaves = kBlock / 64;
-constexpr int kCopyBlocks = 1024;    // most workgroups of the pages launch
-constexpr int kCopyPerBlock = 4096;  // ids a workgroup copies before another one joins
+constexpr int kSmallBlock = 1024;
+constexpr int kCopyBlocks = 1024;    // most workgroups that check or copy page ids
+constexpr int kCopyPerBlock = 4096;  // ids of a workgroup before another one joins
+// One workgroup does it all up to so many tables, heads and page ids.  Against the
+// two launches, with a slot map behind, on the GPU's clock / with the host's
+// launches: 4 tables and 22 ids 8.9 / 11.5 us against 9.3 / 14.2; 256 tables, 6300
+// ids 9.5 / 11.0 against 10.3 / 14.0; 1024 tables, 15900 ids 12.9 / 13.4 against 11.1 /
+// 13.8.
+constexpr int kSmallTables = kSmallBlock, kSmallHeads = 4 * kSmallBlock, kSmallIds = 12 * kSmallBlock;
 
 struct TableParams {
   const int32_t* ctx_len;
@@ -39,121 +47,38 @@ struct TableParams {
   int64_t* pages_needed;
   int32_t* status;
   int64_t* sums;        // [blocks] pages of a workgroup's tables
+  int64_t* bad_id;      // [copy_blocks] first place in the free list with an id outside the pool
   int32_t* bad;         // [blocks] a workgroup met an invalid length, ratio or group
-  int32_t* bad_page;    // [copy_blocks]
-  int64_t tables;       // batch * L * G
-  int32_t blocks, copy_blocks;
+  int64_t rows;         // batch * L
+  int64_t most;         // ids that could be taken: min(num_free, pt_capacity)
+  int32_t blocks, copy_blocks, rows_per_block;
   int32_t L, H, G, P;
+  bool vec;             // the page id arrays allow 16-byte accesses
 };
 
-// Sum over a workgroup; every thread receives it.
-__device__ int64_t block_sum(int64_t x, int64_t* sm) {
+// A reduction of the workgroup's values; every thread receives it.
+template <int N, typename T, typename Op>
+__device__ T block_reduce(T x, T* sm, Op op) {
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) x += __shfl_xor((long long)x, o);
+  for (int o = 32; o > 0; o >>= 1) x = op(x, (T)__shfl_xor((long long)x, o));
   __syncthreads();
   if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = x;
   __syncthreads();
-  x = 0;
+  x = sm[0];
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) x += sm[w];
+  for (int w = 1; w < N / 64; ++w) x = op(x, sm[w]);
   return x;
 }
-
-__device__ __forceinline__ int64_t table_pages(const TableParams& p, int64_t t, int32_t group_len) {
-  const int b = (int)(t / ((int64_t)p.L * p.G));
-  const int room = p.headroom ? max(p.headroom[b], 0) : 0;
-  return ((int64_t)group_len + room + p.P - 1) / p.P;
-}
-
-__global__ void __launch_bounds__(kBlock) tg_table_lengths_kernel(TableParams p) {
-  __shared__ int64_t sm[kWaves];
-  const int64_t t = (int64_t)blockIdx.x * kBlock + threadIdx.x;
-  int64_t pages = 0;
-  bool bad = false;
-  if (t < p.tables) {
-    const int g = (int)(t % p.G);
-    const int64_t bl = t / p.G;
-    const int l = (int)(bl % p.L), b = (int)(bl / p.L);
-    const int n = p.ctx_len[b];
-    bad = n < 1 || (p.headroom && p.headroom[b] < 0);
-    int32_t longest = 0;
-    for (int h = 0; h < p.H; ++h) {
-      const int of = p.group_of[(int64_t)l * p.H + h];
-      if (of < 0 || of >= p.G) bad = true;
-      if (of != g) continue;
-      const double r = p.ratio ? p.ratio[bl * p.H + h] : p.budget[(int64_t)l * p.H + h];
-      const bool ok = r > 0.0 && r <= 1.0;   // false for NaN
-      if (!ok) bad = true;
-      const int32_t len = ok && n >= 1 ? (int32_t)ceil(r * (double)n) : 0;
-      p.kv_len[bl * p.H + h] = len;
-      longest = max(longest, len);
-    }
-    p.group_len[t] = longest;
-    pages = table_pages(p, t, longest);
-  }
-  pages = block_sum(pages, sm);
-  const int64_t any = block_sum(bad, sm);
-  if (threadIdx.x == 0) {
-    p.sums[blockIdx.x] = pages;
-    p.bad[blockIdx.x] = any > 0;
-  }
-}
-
-// What the lengths launch found: the sum of every workgroup's pages (and of
-// those before `block`), whether any input was invalid.
-struct Found {
-  int64_t needed, before;
-  bool bad;
+struct Sum {
+  __device__ int64_t operator()(int64_t a, int64_t b) const { return a + b; }
 };
-__device__ Found found(const TableParams& p, int block, int64_t* sm) {
-  int64_t all = 0, before = 0, bad = 0;
-  for (int i = threadIdx.x; i < p.blocks; i += kBlock) {
-    const int64_t s = p.sums[i];
-    all += s;
-    before += i < block ? s : 0;
-    bad += p.bad[i];
-  }
-  Found f;
-  f.needed = block_sum(all, sm);
-  f.before = block_sum(before, sm);
-  f.bad = block_sum(bad, sm) > 0;
-  return f;
-}
+struct Min {
+  __device__ int64_t operator()(int64_t a, int64_t b) const { return a < b ? a : b; }
+};
 
-__global__ void __launch_bounds__(kBlock) tg_table_pages_kernel(TableParams p) {
-  __shared__ int64_t sm[kWaves];
-  const Found f = found(p, 0, sm);
-  int64_t bad = 0;
-  if (!f.bad && f.needed <= p.num_free && f.needed <= p.pt_capacity) {
-    for (int64_t k = (int64_t)blockIdx.x * kBlock + threadIdx.x; k < f.needed; k += (int64_t)gridDim.x * kBlock) {
-      const int32_t id = p.free_pages[k];
-      if (id < 0 || id >= p.pool_pages) bad = 1;
-      p.pt_pages[k] = id;
-    }
-  }
-  bad = block_sum(bad, sm);
-  if (threadIdx.x == 0) p.bad_page[blockIdx.x] = bad > 0;
-}
-
-__global__ void __launch_bounds__(kBlock) tg_table_offsets_kernel(TableParams p) {
-  __shared__ int64_t sm[kWaves];
-  const Found f = found(p, blockIdx.x, sm);
-  int64_t bad_page = 0;
-  for (int i = threadIdx.x; i < p.copy_blocks; i += kBlock) bad_page += p.bad_page[i];
-  bad_page = block_sum(bad_page, sm);
-  int32_t status = TG_OK;
-  if (f.bad)
-    status = TG_ERR_INVALID_ARG;
-  else if (f.needed > p.num_free)
-    status = TG_ERR_OUT_OF_PAGES;
-  else if (f.needed > p.pt_capacity)
-    status = TG_ERR_BUFFER_TOO_SMALL;
-  else if (bad_page)
-    status = TG_ERR_INVALID_ARG;
-  const int64_t t = (int64_t)blockIdx.x * kBlock + threadIdx.x;
-  const int64_t pages = t < p.tables ? table_pages(p, t, p.group_len[t]) : 0;
-  // inclusive sum over the workgroup
-  int64_t x = pages;
+// Sum of the values of the threads up to and with this one.
+template <int N>
+__device__ int64_t block_inclusive_sum(int64_t x, int64_t* sm) {
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
     const int64_t y = __shfl_up((long long)x, o);
@@ -162,12 +87,166 @@ __global__ void __launch_bounds__(kBlock) tg_table_offsets_kernel(TableParams p)
   __syncthreads();
   if ((threadIdx.x & 63) == 63) sm[threadIdx.x >> 6] = x;
   __syncthreads();
-  x += f.before;
   for (int w = 0; w < (int)(threadIdx.x >> 6); ++w) x += sm[w];
-  if (t < p.tables) p.pt_offsets[t] = status == TG_OK ? x - pages : 0;
+  return x;
+}
+
+// The retained lengths of the heads of rows [row0, row0 + n) (a row: one
+// request's layer), their groups' maxima in longest[n * G].  Whether a value was
+// invalid (its length counts as 0).
+template <int N>
+__device__ bool lengths(const TableParams& p, int64_t row0, int n, int32_t* longest) {
+  for (int i = threadIdx.x; i < n * p.G; i += N) longest[i] = 0;
+  __syncthreads();
+  bool bad = false;
+  for (int i = threadIdx.x; i < n * p.H; i += N) {
+    const int64_t row = row0 + i / p.H;
+    const int h = i % p.H, l = (int)(row % p.L), b = (int)(row / p.L);
+    const int64_t at = row0 * p.H + i;   // of (b, l, h)
+    const int ctx = p.ctx_len[b], of = p.group_of[(int64_t)l * p.H + h];
+    const double r = p.ratio ? p.ratio[at] : p.budget[(int64_t)l * p.H + h];
+    const bool ok = ctx >= 1 && r > 0.0 && r <= 1.0;   // false for NaN
+    const int32_t len = ok ? (int32_t)ceil(r * (double)ctx) : 0;
+    p.kv_len[at] = len;
+    const bool in = of >= 0 && of < p.G;
+    if (in) atomicMax(&longest[i / p.H * p.G + of], len);   // LDS
+    if (!ok || !in || (p.headroom && p.headroom[b] < 0)) bad = true;
+  }
+  __syncthreads();
+  return bad;
+}
+
+__device__ __forceinline__ int64_t table_pages(const TableParams& p, int64_t table, int32_t longest) {
+  const int b = (int)(table / ((int64_t)p.L * p.G));
+  const int room = p.headroom ? max(p.headroom[b], 0) : 0;
+  return ((int64_t)longest + room + p.P - 1) / p.P;
+}
+
+__device__ __forceinline__ int32_t status_of(const TableParams& p, bool bad, int64_t needed, int64_t bad_id) {
+  if (bad) return TG_ERR_INVALID_ARG;
+  if (needed > p.num_free) return TG_ERR_OUT_OF_PAGES;
+  if (needed > p.pt_capacity) return TG_ERR_BUFFER_TOO_SMALL;
+  return bad_id < needed ? TG_ERR_INVALID_ARG : TG_OK;
+}
+
+// fn(place, id) over this workgroup's share of the free list's first n ids
+template <int N, typename F>
+__device__ __forceinline__ void for_ids(const TableParams& p, int64_t n, int block, int blocks, F fn) {
+  const int64_t vecs = p.vec ? n / 4 : 0;
+#pragma unroll 4
+  for (int64_t i = (int64_t)block * N + threadIdx.x; i < vecs; i += (int64_t)blocks * N) fn(4 * i, reinterpret_cast<const int4*>(p.free_pages)[i]);
+  for (int64_t i = 4 * vecs + (int64_t)block * N + threadIdx.x; i < n; i += (int64_t)blocks * N) fn(i, p.free_pages[i]);
+}
+
+// The first place with an id outside the pool.
+struct FirstBad {
+  const TableParams& p;
+  int64_t at = INT64_MAX;
+  __device__ void operator()(int64_t i, int32_t id) {
+    if (id < 0 || id >= p.pool_pages) at = min(at, i);
+  }
+  __device__ void operator()(int64_t i, const int4& v) {
+    (*this)(i, v.x);
+    (*this)(i + 1, v.y);
+    (*this)(i + 2, v.z);
+    (*this)(i + 3, v.w);
+  }
+};
+struct Copy {
+  const TableParams& p;
+  __device__ void operator()(int64_t i, int32_t id) { p.pt_pages[i] = id; }
+  __device__ void operator()(int64_t i, const int4& v) { *reinterpret_cast<int4*>(p.pt_pages + i) = v; }
+};
+
+__global__ void __launch_bounds__(kBlock) tg_table_lengths_kernel(TableParams p) {
+  __shared__ int64_t sm[kBlock / 64];
+  __shared__ int32_t longest[kBlock];
+  if ((int)blockIdx.x >= p.blocks) {
+    const int block = blockIdx.x - p.blocks;
+    FirstBad bad{p};
+    for_ids<kBlock>(p, p.most, block, p.copy_blocks, [&](int64_t i, auto v) { bad(i, v); });
+    const int64_t at = block_reduce<kBlock>(bad.at, sm, Min());
+    if (threadIdx.x == 0) p.bad_id[block] = at;
+    return;
+  }
+  const int64_t row0 = (int64_t)blockIdx.x * p.rows_per_block;
+  const int n = (int)min<int64_t>(p.rows_per_block, p.rows - row0);
+  const bool bad = lengths<kBlock>(p, row0, n, longest);
+  int64_t pages = 0;
+  if ((int)threadIdx.x < n * p.G) {   // at most kBlock tables
+    const int64_t table = row0 * p.G + threadIdx.x;
+    p.group_len[table] = longest[threadIdx.x];
+    pages = table_pages(p, table, longest[threadIdx.x]);
+  }
+  // pages in the upper bits, whether anything was invalid in the lowest 16 (at most kBlock of them)
+  const int64_t sum = block_reduce<kBlock>(pages * 65536 + bad, sm, Sum());
+  if (threadIdx.x == 0) {
+    p.sums[blockIdx.x] = sum / 65536;
+    p.bad[blockIdx.x] = sum % 65536 != 0;
+  }
+}
+
+__global__ void __launch_bounds__(kBlock) tg_table_fill_kernel(TableParams p) {
+  __shared__ int64_t sm[kBlock / 64];
+  int64_t all = 0, before = 0, bad = 0, bad_id = INT64_MAX;
+  for (int i = threadIdx.x; i < p.blocks; i += kBlock) {
+    const int64_t s = p.sums[i];
+    all += s;
+    before += i < (int)blockIdx.x ? s : 0;
+    bad += p.bad[i];
+  }
+  for (int i = threadIdx.x; i < p.copy_blocks; i += kBlock) bad_id = min(bad_id, p.bad_id[i]);
+  const int64_t needed = block_reduce<kBlock>(all, sm, Sum());
+  bad = block_reduce<kBlock>(bad, sm, Sum());
+  bad_id = block_reduce<kBlock>(bad_id, sm, Min());
+  const int32_t status = status_of(p, bad > 0, needed, bad_id);
+  if (status == TG_OK && (int)blockIdx.x < p.copy_blocks) {
+    Copy copy{p};
+    for_ids<kBlock>(p, needed, blockIdx.x, p.copy_blocks, [&](int64_t i, auto v) { copy(i, v); });
+  }
+  if ((int)blockIdx.x < p.blocks) {
+    before = block_reduce<kBlock>(before, sm, Sum());
+    const int64_t row0 = (int64_t)blockIdx.x * p.rows_per_block;
+    const int n = (int)min<int64_t>(p.rows_per_block, p.rows - row0) * p.G;
+    const int64_t table = row0 * p.G + threadIdx.x;
+    const bool mine = (int)threadIdx.x < n;
+    const int64_t pages = mine ? table_pages(p, table, p.group_len[table]) : 0;
+    const int64_t end = before + block_inclusive_sum<kBlock>(pages, sm);
+    if (mine) p.pt_offsets[table] = status == TG_OK ? end - pages : 0;
+  }
   if (blockIdx.x == 0 && threadIdx.x == 0) {
-    p.pt_offsets[p.tables] = status == TG_OK ? f.needed : 0;
-    *p.pages_needed = f.needed;
+    p.pt_offsets[p.rows * p.G] = status == TG_OK ? needed : 0;
+    *p.pages_needed = needed;
+    *p.status = status;
+  }
+}
+
+__global__ void __launch_bounds__(kSmallBlock) tg_table_small_kernel(TableParams p) {
+  __shared__ int64_t sm[kSmallBlock / 64];
+  __shared__ int32_t longest[kSmallTables];
+  const bool invalid = lengths<kSmallBlock>(p, 0, (int)p.rows, longest);
+  const int tables = (int)p.rows * p.G;
+  const bool mine = (int)threadIdx.x < tables;
+  const int64_t pages = mine ? table_pages(p, threadIdx.x, longest[threadIdx.x]) : 0;
+  if (mine) p.group_len[threadIdx.x] = longest[threadIdx.x];
+  const int64_t end = block_inclusive_sum<kSmallBlock>(pages, sm);
+  __syncthreads();
+  if (threadIdx.x == kSmallBlock - 1) sm[0] = end;
+  __syncthreads();
+  const int64_t needed = sm[0];
+  FirstBad first{p};
+  for_ids<kSmallBlock>(p, min(needed, p.most), 0, 1, [&](int64_t i, auto v) { first(i, v); });
+  const int64_t bad = block_reduce<kSmallBlock>((int64_t)invalid, sm, Sum());
+  const int64_t bad_id = block_reduce<kSmallBlock>(first.at, sm, Min());
+  const int32_t status = status_of(p, bad > 0, needed, bad_id);
+  if (status == TG_OK) {
+    Copy copy{p};
+    for_ids<kSmallBlock>(p, needed, 0, 1, [&](int64_t i, auto v) { copy(i, v); });
+  }
+  if (mine) p.pt_offsets[threadIdx.x] = status == TG_OK ? end - pages : 0;
+  if (threadIdx.x == 0) {
+    p.pt_offsets[tables] = status == TG_OK ? needed : 0;
+    *p.pages_needed = needed;
     *p.status = status;
   }
 }
@@ -214,17 +293,20 @@ __global__ void __launch_bounds__(kBlock) tg_slot_map_kernel(MapParams p) {
 size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 
 struct Layout {
-  int64_t tables, blocks;
-  size_t sums, bad, total;
+  int64_t rows, blocks;
+  int rows_per_block;
+  size_t sums, bad_id, total;
 };
 
 Layout layout_of(const tg_geometry& g, int batch) {
   Layout l;
-  l.tables = (int64_t)batch * g.num_layers * (g.num_kv_heads / g.heads_per_group);
-  l.blocks = (l.tables + kBlock - 1) / kBlock;
+  l.rows = (int64_t)batch * g.num_layers;
+  l.rows_per_block = kBlock / g.num_kv_heads;
+  if (l.rows_per_block < 1) l.rows_per_block = 1;
+  l.blocks = (l.rows + l.rows_per_block - 1) / l.rows_per_block;
   l.sums = align256((size_t)l.blocks * sizeof(int64_t));
-  l.bad = align256((size_t)l.blocks * sizeof(int32_t));
-  l.total = l.sums + l.bad + align256(kCopyBlocks * sizeof(int32_t));
+  l.bad_id = align256(kCopyBlocks * sizeof(int64_t));
+  l.total = l.sums + l.bad_id + align256((size_t)l.blocks * sizeof(int32_t));
   return l;
 }
 
@@ -248,8 +330,10 @@ int32_t tg_reserve_device(const tg_reserve_device_args* a, void* hip_stream) {
   if (a->num_free < 0 || a->pool_pages < 0 || a->pt_capacity < 0) return tg::fail(TG_ERR_INVALID_ARG, "negative pool size");
   if (a->num_free > 0 && !a->free_pages) return tg::fail(TG_ERR_INVALID_ARG, "free_pages is NULL");
   if (a->pt_capacity > 0 && !a->pt_pages) return tg::fail(TG_ERR_INVALID_ARG, "pt_pages is NULL");
+  if (g.num_kv_heads > kBlock)
+    return tg::fail(TG_ERR_UNSUPPORTED, "reserve on the device supports up to %d KV heads (got %d)", kBlock, g.num_kv_heads);
   const Layout l = layout_of(g, a->batch);
-  if (l.blocks > INT32_MAX) return tg::fail(TG_ERR_INVALID_ARG, "batch too large");
+  if (l.blocks > INT32_MAX - kCopyBlocks) return tg::fail(TG_ERR_INVALID_ARG, "batch too large");
   if (!a->workspace || a->workspace_bytes < l.total)
     return tg::fail(TG_ERR_BUFFER_TOO_SMALL, "workspace holds %zu bytes, need %zu", a->workspace_bytes, l.total);
   if (!tg::aligned16({a->workspace})) return tg::fail(TG_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
@@ -271,25 +355,30 @@ int32_t tg_reserve_device(const tg_reserve_device_args* a, void* hip_stream) {
   p.status = a->status;
   char* ws = static_cast<char*>(a->workspace);
   p.sums = reinterpret_cast<int64_t*>(ws);
-  p.bad = reinterpret_cast<int32_t*>(ws + l.sums);
-  p.bad_page = reinterpret_cast<int32_t*>(ws + l.sums + l.bad);
-  p.tables = l.tables;
+  p.bad_id = reinterpret_cast<int64_t*>(ws + l.sums);
+  p.bad = reinterpret_cast<int32_t*>(ws + l.sums + l.bad_id);
+  p.rows = l.rows;
   p.blocks = (int32_t)l.blocks;
+  p.rows_per_block = l.rows_per_block;
   p.L = g.num_layers;
   p.H = g.num_kv_heads;
   p.G = g.num_kv_heads / g.heads_per_group;
   p.P = g.page_size;
-  const int64_t most = a->num_free < a->pt_capacity ? a->num_free : a->pt_capacity;   // ids that can be taken
-  const int64_t copy = (most + kCopyPerBlock - 1) / kCopyPerBlock;
+  p.vec = tg::aligned16({a->free_pages, a->pt_pages});
+  p.most = a->num_free < a->pt_capacity ? a->num_free : a->pt_capacity;
+  const int64_t copy = (p.most + kCopyPerBlock - 1) / kCopyPerBlock;
   p.copy_blocks = (int32_t)(copy < 1 ? 1 : copy > kCopyBlocks ? kCopyBlocks : copy);
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
-  hipLaunchKernelGGL(tg_table_lengths_kernel, dim3((unsigned)l.blocks), dim3(kBlock), 0, st, p);
+  if (l.rows * p.G <= kSmallTables && l.rows * p.H <= kSmallHeads && p.most <= kSmallIds) {
+    hipLaunchKernelGGL(tg_table_small_kernel, dim3(1), dim3(kSmallBlock), 0, st, p);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return tg::fail(TG_ERR_HIP, "reserve launch failed: %s", hipGetErrorString(e));
+    return TG_OK;
+  }
+  hipLaunchKernelGGL(tg_table_lengths_kernel, dim3(p.blocks + p.copy_blocks), dim3(kBlock), 0, st, p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return tg::fail(TG_ERR_HIP, "reserve launch failed: %s", hipGetErrorString(e));
-  hipLaunchKernelGGL(tg_table_pages_kernel, dim3(p.copy_blocks), dim3(kBlock), 0, st, p);
-  e = hipGetLastError();
-  if (e != hipSuccess) return tg::fail(TG_ERR_HIP, "reserve launch failed: %s", hipGetErrorString(e));
-  hipLaunchKernelGGL(tg_table_offsets_kernel, dim3((unsigned)l.blocks), dim3(kBlock), 0, st, p);
+  hipLaunchKernelGGL(tg_table_fill_kernel, dim3(p.blocks > p.copy_blocks ? p.blocks : p.copy_blocks), dim3(kBlock), 0, st, p);
   e = hipGetLastError();
   if (e != hipSuccess) return tg::fail(TG_ERR_HIP, "reserve launch failed: %s", hipGetErrorString(e));
   return TG_OK;

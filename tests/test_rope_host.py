@@ -156,7 +156,8 @@ def reserve_args(**kw):
     (dict(batch=0), INVALID), (dict(geom=tg.tg_geometry(2, 4, 8, 64, 16, 3)), INVALID), (dict(ctx_len=None), INVALID),
     (dict(ratio=None), INVALID), (dict(status=None), INVALID), (dict(num_free=-1), INVALID),
     (dict(pool_pages=-1), INVALID), (dict(pt_capacity=-1), INVALID), (dict(free_pages=None), INVALID),
-    (dict(pt_pages=None), INVALID), (dict(workspace=None), SMALL), (dict(workspace_bytes=16), SMALL),
+    (dict(pt_pages=None), INVALID), (dict(geom=tg.tg_geometry(1, 512, 512, 64, 16, 2)), UNSUPPORTED),
+    (dict(workspace=None), SMALL), (dict(workspace_bytes=16), SMALL),
     (dict(workspace=FAKE + 8), INVALID)])
 def test_reserve_device_refusals(kw, code):
     with pytest.raises(tg.TangramError) as e:

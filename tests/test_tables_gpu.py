@@ -30,7 +30,7 @@ class Admission:
         if ratio is None and budget is None:
             ratio = np.clip(rng.random((B, L, H)), 1e-3, 1.0)
             ratio[rng.random(ratio.shape) < 0.1] = 1.0
-        self.ctx = np.asarray(np.broadcast_to(ctx, (B,)), np.int32)
+        self.ctx = np.array(np.broadcast_to(ctx, (B,)), np.int32)
         self.ratio, self.budget, self.headroom = ratio, budget, headroom
         if group_of is None:
             group_of = np.stack([rng.permutation(np.repeat(np.arange(self.G), Hp)) for _ in range(L)])
@@ -115,6 +115,27 @@ def test_tables_equal_the_hosts(B, L, H, Hp, P, ctx, headroom):
         assert np.array_equal(got["kv_len"][:B * L * H].reshape(B, L, H), res["kv_len"])
         assert np.array_equal(got["offsets"][:B * L * a.G + 1], res["offsets"])
     say(f"tables B{B} L{L}: {want['pages_needed']} pages")
+
+
+@pytest.mark.parametrize("num_free", [None, 20000])
+@pytest.mark.parametrize("shift", [0, 1, 3])
+def test_one_workgroup_and_many_page_lists_anywhere(num_free, shift):
+    """The launch of small admissions and the two of large ones (a free list of 20000) give the same tables; page arrays
+    need no more than their own alignment."""
+    _gpu()
+    for B, L, H, Hp, P in ((2, 1, 4, 2, 16), (16, 32, 8, 4, 16), (1, 1024, 1, 1, 16), (4, 64, 16, 4, 16)):
+        a = Admission(B, L, H, Hp, P, np.arange(1, B + 1) * 37, headroom=np.full(B, 3, np.int32), seed=B)
+        a = Admission(B, L, H, Hp, P, a.ctx, headroom=a.headroom, seed=B, num_free=num_free and max(num_free, a.need))
+        o, args = a.device()
+        free = torch.zeros(a.num_free + 4, dtype=torch.int32, device="cuda")
+        free[shift:shift + a.num_free] = a.keep[4]
+        pages = torch.full((a.capacity + 64,), -77, dtype=torch.int32, device="cuda")
+        args.free_pages, args.pt_pages = free.data_ptr() + 4 * shift, pages.data_ptr() + 4 * shift
+        tg.tg_reserve_device(args)
+        torch.cuda.synchronize()
+        assert bool((pages[:shift] == -77).all())
+        o["pages"] = pages[shift:]
+        a.check_ok({k: v.cpu().numpy() for k, v in o.items()})
 
 
 def test_budget_instead_of_ratio_exact_products_and_one_long_request():
