@@ -45,6 +45,8 @@ constexpr int kPrefillSplitMaxBlocks = 1024;  // past it blocks outnumber the CU
 // / 65 us, two over 8192 61 / 57 / 68, four 95 / 109 / 110; over 57 shapes 0.99
 // / 1 / 1.02.
 constexpr int prefill_split_target(int head_dim) { return head_dim == 128 ? 208 : 448; }
+// One entry of tg_prefill_mod's work list.
+constexpr int kPrefillListEntryBytes = 32;
 // Whole-block launches of head_dim 64 with more blocks than this run two
 // workgroups per CU.
 constexpr int kPrefillOnePerCuBlocks = 512;

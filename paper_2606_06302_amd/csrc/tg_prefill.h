@@ -104,7 +104,7 @@ size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 struct SplitLayout {
   int row_tiles, part_waves, groups;
   int list_per_xcd;   // tg_prefill_mod: entries of its work list per XCD
-  size_t o_bytes, ml_bytes, pieces_bytes, blocks_bytes, bytes;
+  size_t o_bytes, ml_bytes, pieces_bytes, bytes;
 };
 
 SplitLayout split_layout(const tg_geometry& g, int batch, int chunk_len) {
@@ -123,8 +123,7 @@ SplitLayout split_layout(const tg_geometry& g, int batch, int chunk_len) {
   // sum over blocks of ceil(n / T) entries in eight classes, each class dealt to the 8 XCDs
   const int entries = split_target(g.head_dim) + (int)(units * row_tiles);
   s.list_per_xcd = (entries > split_at_once(g.head_dim) ? entries : split_at_once(g.head_dim)) / 8 + 9;
-  s.blocks_bytes = align256((size_t)(units * row_tiles) * sizeof(int4));
-  s.bytes = s.o_bytes + s.ml_bytes + s.pieces_bytes + s.blocks_bytes + align256((size_t)s.list_per_xcd * 8 * sizeof(int));
+  s.bytes = s.o_bytes + s.ml_bytes + s.pieces_bytes + align256((size_t)s.list_per_xcd * 8 * tg::kPrefillListEntryBytes);
   return s;
 }
 

@@ -69,12 +69,20 @@ struct ModParams {
   f32x4* part_o;            // [split_slots][part_waves][D/4][32 rows] unnormalised fp32 outputs
   float* part_ml;           // [split_slots][part_waves][2][32 rows]: reference maximum in log2 units, sum
   int2* pieces;             // [units * row_tiles]: first partial slot and piece count of every block
-  int4* blocks;             // [units * row_tiles]: history tiles, first chunk tile, tiles
-  int32_t* list;            // [8 * list_per_xcd]: block | piece << 10, or -1
+  struct ListEntry* list;   // [8 * list_per_xcd]
   int32_t part_waves;       // waves of a block that own rows: min(8, ceil(chunk*gqa / 32))
   int32_t list_len;
 };
-static_assert(tg::kPrefillSplitMaxBlocks <= 1024, "a list entry holds the block in 10 bits");
+
+// One workgroup of the key-split launch: a piece of a block of rows.
+struct ListEntry {
+  int32_t block;            // unit * row_tiles + row tile, or -1: nothing
+  int32_t t_begin, t_end;   // key tiles of the block's walk
+  int32_t nh, ct0;          // the walk: history tiles, first chunk tile
+  int32_t slot;             // partial slot, or -1: the whole block, the output is written
+  int32_t unused[2];
+};
+static_assert(sizeof(ListEntry) == tg::kPrefillListEntryBytes, "split_layout counts these");
 
 // The chunk keys [lo, hi) that row i of request b sees; the history where lo was
 // negative.  No key of the chunk: lo = INT32_MAX, hi = 0, neutral for the least
@@ -114,11 +122,67 @@ __device__ __forceinline__ Walk block_walk(int hist_tiles, int min_lo, int max_h
   return w;
 }
 
+// x of another lane of the 16-lane row (lanes without a source get `none`)
+template <int kCtrl>
+__device__ __forceinline__ int row_lane(int x, int none = 0) {
+  return __builtin_amdgcn_update_dpp(none, x, kCtrl, 0xF, 0xF, false);
+}
+
+// Reductions by lane moves inside the vector unit (a shuffle goes through LDS):
+// over the aligned 16 lanes, and over the wave; every lane receives the result.
+template <typename Op>
+__device__ __forceinline__ int row_reduce(int x, Op op) {
+  x = op(x, row_lane<kQuadXor1>(x));
+  x = op(x, row_lane<kQuadXor2>(x));
+  x = op(x, row_lane<kRowHalfMirror>(x));
+  return op(x, row_lane<kRowMirror>(x));
+}
+template <typename Op>
+__device__ __forceinline__ int wave_reduce(int x, Op op) {
+  x = row_reduce(x, op);
+  auto r = __builtin_amdgcn_permlane16_swap((uint32_t)x, (uint32_t)x, false, false);
+  x = op((int)r[0], (int)r[1]);
+  r = __builtin_amdgcn_permlane32_swap((uint32_t)x, (uint32_t)x, false, false);
+  return op((int)r[0], (int)r[1]);
+}
+struct Least {
+  __device__ int operator()(int a, int b) const { return min(a, b); }
+};
+struct Greatest {
+  __device__ int operator()(int a, int b) const { return max(a, b); }
+};
+struct Sum {
+  __device__ int operator()(int a, int b) const { return a + b; }
+};
+
 // Least of a wave's values, in scalar registers.
-__device__ __forceinline__ int wave_min(int x) {
+__device__ __forceinline__ int wave_min(int x) { return __builtin_amdgcn_readfirstlane(wave_reduce(x, Least())); }
+
+// Sum of the values of the lanes up to and with this one: within the 16-lane
+// rows, then the rows before.
+__device__ __forceinline__ int wave_inclusive_sum(int x) {
+  x += row_lane<0x111>(x);   // row_shr 1, 2, 4, 8
+  x += row_lane<0x112>(x);
+  x += row_lane<0x114>(x);
+  x += row_lane<0x118>(x);
+  const int row = (threadIdx.x & 63) >> 4;
+  const int s0 = __builtin_amdgcn_readlane(x, 15), s1 = __builtin_amdgcn_readlane(x, 31), s2 = __builtin_amdgcn_readlane(x, 47);
+  return x + (row > 0 ? s0 : 0) + (row > 1 ? s1 : 0) + (row > 2 ? s2 : 0);
+}
+
+// n / d for 0 <= n < 2^28, d >= 1, by the reciprocal and two corrections.
+__device__ __forceinline__ int quotient(int n, int d) {
+  int q = (int)((float)n * __builtin_amdgcn_rcpf((float)d));
+  int r = n - q * d;
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) x = min(x, __shfl_xor(x, o));
-  return __builtin_amdgcn_readfirstlane(x);
+  for (int i = 0; i < 2; ++i) {   // off by one at most where n has 24 bits, by 32 with 28 bits and a small d
+    const int e = (int)floorf((float)r * __builtin_amdgcn_rcpf((float)d));
+    q += e;
+    r -= e * d;
+  }
+  q += r >= d ? 1 : 0;
+  q -= r < 0 ? 1 : 0;
+  return q;
 }
 
 // Bits 15 and 31: whether the bf16 of a word's lower and upper half are infinite or NaN.
@@ -191,12 +255,10 @@ __global__ void __launch_bounds__(kBlock, kWavesPerSimd) tg_prefill_mod_kernel(M
   // block -> (unit, row tile): the key-split launch's list, the host schedule,
   // or units round-robin over the 8 XCDs
   int unit, rt;
-  int block = 0, piece = 0;   // key-split launch
+  const TG_CONST int32_t* const entry = (const TG_CONST int32_t*)(p.list + blockIdx.x);   // key-split launch
   if constexpr (kSplit) {
-    const int code = ((const TG_CONST int32_t*)p.list)[blockIdx.x];
-    if (code < 0) return;
-    block = code & 1023;
-    piece = code >> 10;
+    const int block = entry[0];
+    if (block < 0) return;
     unit = block / p.row_tiles;
     rt = block % p.row_tiles;
   } else if (p.block_order) {
@@ -236,17 +298,13 @@ __global__ void __launch_bounds__(kBlock, kWavesPerSimd) tg_prefill_mod_kernel(M
   const bool w_hist_all = !__any(row_ok && !mine.hist);
 
   Walk walk;
-  int t_begin = 0, t_end, np = 1, first_slot = 0;
+  int t_begin = 0, t_end, slot_out = -1;
   if constexpr (kSplit) {
-    const TG_CONST int32_t* bw = (const TG_CONST int32_t*)(p.blocks + block);
-    const TG_CONST int32_t* pc = (const TG_CONST int32_t*)(p.pieces + block);
-    walk.nh = bw[0];
-    walk.ct0 = bw[1];
-    walk.n_tiles = bw[2];
-    first_slot = pc[0];
-    np = pc[1];
-    t_begin = (int)((int64_t)piece * walk.n_tiles / np);
-    t_end = (int)((int64_t)(piece + 1) * walk.n_tiles / np);
+    t_begin = entry[1];
+    t_end = entry[2];
+    walk.nh = entry[3];
+    walk.ct0 = entry[4];
+    slot_out = entry[5];
   } else {
     if (lane == 0) {
       shared_int[wave][0] = w_min_lo;
@@ -543,9 +601,9 @@ __global__ void __launch_bounds__(kBlock, kWavesPerSimd) tg_prefill_mod_kernel(M
   // row sum over both halves of the row, then O = O^T / l
   const float lt = swap32_sum(l);
   if constexpr (kSplit) {
-    if (np > 1) {   // a piece: its partials, 16-byte stores contiguous over the 32 rows
+    if (slot_out >= 0) {   // a piece: its partials, 16-byte stores contiguous over the 32 rows
       if (wave < p.part_waves) {
-        const int64_t part = (int64_t)(first_slot + piece) * p.part_waves + wave;
+        const int64_t part = (int64_t)slot_out * p.part_waves + wave;
         f32x4* po = p.part_o + part * (D / 4) * 32 + (lane & 31);
 #pragma unroll
         for (int db = 0; db < S::kDB; ++db)
@@ -576,99 +634,92 @@ __global__ void __launch_bounds__(kBlock, kWavesPerSimd) tg_prefill_mod_kernel(M
 // of rows.
 constexpr int kPlanBlock = 1024;
 constexpr int kPlanWaves = kPlanBlock / 64;
-constexpr int kPairLanes = 16;
+constexpr int kPairLanes = 16;   // row_reduce's
 constexpr int kClasses = 8;   // 0: the pieces of cut blocks; 1..7 the other blocks by descending length
 
-__device__ __forceinline__ int wave_inclusive_sum(int x) {
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int y = __shfl_up(x, o);
-    if ((int)(threadIdx.x & 63) >= o) x += y;
-  }
-  return x;
-}
+// every thread's LDS accesses before, all threads' after (__syncthreads would
+// wait for the loads and stores of global memory too)
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-__global__ void __launch_bounds__(kPlanBlock) tg_prefill_mod_plan_kernel(ModParams p, int target, int slots) {
+// Bound by latency: four memory round trips (the head's group, its table beside
+// the masks, the list cleared, the list written).
+template <int D>
+__global__ void __launch_bounds__(kPlanBlock) tg_prefill_mod_plan_kernel(ModParams p) {
   // per (request, row tile): least lo, greatest hi, whether a row sees the history
   __shared__ int32_t min_lo[tg::kPrefillSplitMaxBlocks], max_hi[tg::kPrefillSplitMaxBlocks];
   __shared__ int32_t any_hist[tg::kPrefillSplitMaxBlocks];
+  __shared__ Walk walks[tg::kPrefillSplitMaxBlocks];
+  __shared__ int2 shares[tg::kPrefillSplitMaxBlocks];
   __shared__ int32_t starts[tg::kPrefillSplitMaxBlocks];   // first entry (and partial slot) of every cut block
-  __shared__ int64_t sums[kPlanWaves];
+  __shared__ int2 sums[kPlanWaves];
   __shared__ int32_t fits[kPlanWaves];
   __shared__ int32_t counts[kClasses][kPlanWaves], in_class[kClasses];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int pairs = p.batch * p.row_tiles, blocks = pairs * p.num_kv_heads;
   const int k = threadIdx.x;
-  // the block's history, asked for before the masks are read
-  int hist = 0, pair = 0;
-  if (k < blocks) {
-    const int unit = k / p.row_tiles, rt = k % p.row_tiles;
-    const int b = unit / p.num_kv_heads, h = unit % p.num_kv_heads;
-    pair = b * p.row_tiles + rt;
-    const int64_t len = p.kv_len[((int64_t)b * p.num_layers + p.layer) * p.num_kv_heads + h];
-    const int64_t ti = ((int64_t)b * p.num_layers + p.layer) * p.num_groups + p.group_of[(int64_t)p.layer * p.num_kv_heads + h];
-    const int64_t room = (p.pt_offsets[ti + 1] - p.pt_offsets[ti]) * kPage;
-    hist = (int)max<int64_t>(0, min<int64_t>(len, room));
-  }
-  for (int i = threadIdx.x; i < p.list_len; i += kPlanBlock) p.list[i] = -1;
+  // the block's history (threads past the last block read the last one's): asked
+  // for here, used after the masks
+  const int kk = min(k, blocks - 1);
+  const int unit = kk / p.row_tiles, b_k = unit / p.num_kv_heads, h_k = unit % p.num_kv_heads;
+  const int pair = b_k * p.row_tiles + kk % p.row_tiles;
+  const int64_t bl = (int64_t)b_k * p.num_layers + p.layer;
+  const int64_t ti = bl * p.num_groups + p.group_of[(int64_t)p.layer * p.num_kv_heads + h_k];
+  const int64_t len = p.kv_len[bl * p.num_kv_heads + h_k];
+  const int64_t off0 = p.pt_offsets[ti], off1 = p.pt_offsets[ti + 1];
+  for (int i = threadIdx.x; i < p.list_len; i += kPlanBlock) p.list[i].block = -1;
   // kPairLanes lanes per (request, row tile)
   const int sub = lane % kPairLanes;
   for (int at = threadIdx.x / kPairLanes; at < pairs; at += kPlanBlock / kPairLanes) {
     const int b = at / p.row_tiles, rt = at % p.row_tiles;
+    const int last = min(p.chunk - 1, ((rt + 1) * kRows - 1) / p.gqa);
     const int n_valid = valid_tokens(p, b);
-    const int last = min(n_valid - 1, ((rt + 1) * kRows - 1) / p.gqa);
     int lo = INT32_MAX, hi = 0, seen = 0;
 #pragma unroll 4
     for (int i = rt * kRows / p.gqa + sub; i <= last; i += kPairLanes) {
       const Seen s = row_sees(p, b, i, n_valid);
-      lo = min(lo, s.lo);
-      hi = max(hi, s.hi);
-      seen |= s.hist;
+      const bool row = i < n_valid;
+      lo = min(lo, row ? s.lo : INT32_MAX);
+      hi = max(hi, row ? s.hi : 0);
+      seen |= row && s.hist;
     }
-#pragma unroll
-    for (int o = kPairLanes / 2; o > 0; o >>= 1) {
-      lo = min(lo, __shfl_xor(lo, o));
-      hi = max(hi, __shfl_xor(hi, o));
-      seen |= __shfl_xor(seen, o);
-    }
+    lo = row_reduce(lo, Least());
+    hi = row_reduce(hi, Greatest());
+    seen = row_reduce(seen, Greatest());
     if (sub == 0) {
       min_lo[at] = lo;
       max_hi[at] = hi;
       any_hist[at] = seen;
     }
   }
-  __syncthreads();
+  lds_barrier();
   Walk w = {0, 0, 0};
   if (k < blocks) {
+    const int hist = (int)max<int64_t>(0, min<int64_t>(len, (off1 - off0) * kPage));
     w = block_walk((hist + kTile - 1) / kTile, min_lo[pair], max_hi[pair], any_hist[pair]);
-    p.blocks[k] = make_int4(w.nh, w.ct0, w.n_tiles, 0);
+    walks[k] = w;
   }
-  int64_t total = w.n_tiles;
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) total += __shfl_xor((long long)total, o);
-  if (lane == 0) sums[wave] = total;
-  if (k < blocks) starts[k] = w.n_tiles;
-  __syncthreads();
-  total = sums[lane % kPlanWaves];
-#pragma unroll
-  for (int o = kPlanWaves / 2; o > 0; o >>= 1) total += __shfl_xor((long long)total, o);
+  // the sum of all, in two parts: a block has up to 2^26 tiles
+  const int low = wave_reduce(w.n_tiles & 0xffff, Sum()), high = wave_reduce(w.n_tiles >> 16, Sum());
+  if (lane == 0) sums[wave] = make_int2(low, high);
+  lds_barrier();
+  const int2 part = sums[lane % kPlanWaves];
+  const int64_t total = row_reduce(part.x, Sum()) + ((int64_t)row_reduce(part.y, Sum()) << 16);
   // T: the shortest of a few that give no more pieces than run at once, so that
   // all end together, or total / target where that is shorter: many short
   // blocks leave their places early
-  const int fair = (int)((total + slots - 1) / slots);
+  constexpr int kSlots = split_at_once(D), kTarget = split_target(D);
+  const int fair = (int)((total + kSlots - 1) / kSlots);
   const int try_T = max(tg::kPrefillSplitMinTiles, fair + (fair * wave + 31) / 32);   // this wave's
   int tried = 0;
-  for (int i = lane; i < blocks; i += 64) tried += max(1, (starts[i] + try_T - 1) / try_T);
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) tried += __shfl_xor(tried, o);
-  if (lane == 0) fits[wave] = tried <= slots ? try_T : INT32_MAX;
-  __syncthreads();
-  int T = fits[lane % kPlanWaves];
-#pragma unroll
-  for (int o = kPlanWaves / 2; o > 0; o >>= 1) T = min(T, __shfl_xor(T, o));
-  T = min(T, (int)max<int64_t>(tg::kPrefillSplitMinTiles, (total + target - 1) / target));
-  const int np = k < blocks ? max(1, (w.n_tiles + T - 1) / T) : 0;
-  const int cls = np == 0 ? -1 : np > 1 ? 0 : 7 - w.n_tiles * 6 / T;   // n_tiles <= T there
+  for (int i = lane; i < blocks; i += 64) tried += max(1, quotient(walks[i].n_tiles + try_T - 1, try_T));
+  tried = wave_reduce(tried, Sum());
+  if (lane == 0) fits[wave] = tried <= kSlots ? try_T : INT32_MAX;
+  lds_barrier();
+  int T = row_reduce(fits[lane % kPlanWaves], Least());
+  T = min(T, (int)max<int64_t>(tg::kPrefillSplitMinTiles, (total + kTarget - 1) / kTarget));
+  const int np = k < blocks ? max(1, quotient(w.n_tiles + T - 1, T)) : 0;
+  // descending length: n_tiles <= T there
+  const int cls = np == 0 ? -1 : np > 1 ? 0 : 7 - (int)(6.f * (float)w.n_tiles * __builtin_amdgcn_rcpf((float)T));
   // place of the block's first entry in its class: within the wave, then over the waves
   int before = 0, count = 0;   // count, lane c: entries of class c in this wave
 #pragma unroll
@@ -679,33 +730,35 @@ __global__ void __launch_bounds__(kPlanBlock) tg_prefill_mod_plan_kernel(ModPara
   }
   const int cut = cls == 0 ? np : 0;
   const int cut_sum = wave_inclusive_sum(cut);
-  const int cut_all = __shfl(cut_sum, 63);
+  const int cut_all = __builtin_amdgcn_readlane(cut_sum, 63);
   if (lane == 0) count = cut_all;
   if (lane < kClasses) counts[lane][wave] = count;
-  __syncthreads();
+  lds_barrier();
   if (wave < kClasses) {   // counts: entries of the class in the waves before; in_class: in all
     const int c = lane < kPlanWaves ? counts[wave][lane] : 0;
     const int sum = wave_inclusive_sum(c);
     if (lane < kPlanWaves) counts[wave][lane] = sum - c;
     if (lane == 63) in_class[wave] = sum;
   }
-  __syncthreads();
+  lds_barrier();
   if (cls > 0) before += counts[cls][wave];
   const int cut_before = counts[0][wave] + cut_sum - cut;
   if (k < blocks) {
     starts[k] = cut_before;
+    const int q = quotient(w.n_tiles, np);   // tiles of a piece; the first few have one more
+    shares[k] = make_int2(q, w.n_tiles - q * np);
     p.pieces[k] = make_int2(cut_before, np);
   }
   // entry r of class c: XCD 8 r / n, there behind the classes before c
   auto place = [&](int c, int r) {
     const int n = in_class[c];
-    const int x = 8 * r / n;   // n is at most the list's length
+    const int x = quotient(8 * r, n);   // n is at most the list's length
     int pos = r - (x * n + 7) / 8;
     for (int i = 0; i < c; ++i) pos += ((x + 1) * in_class[i] + 7) / 8 - (x * in_class[i] + 7) / 8;
     return 8 * pos + x;
   };
-  __syncthreads();   // starts complete, and the list's -1 before its entries
-  if (cls > 0) p.list[place(cls, before)] = k;
+  __syncthreads();   // starts complete, and the list cleared before its entries are written
+  if (cls > 0) p.list[place(cls, before)] = ListEntry{k, 0, w.n_tiles, w.nh, w.ct0, -1, {0, 0}};
   for (int r = threadIdx.x; r < in_class[0]; r += kPlanBlock) {
     int lo = 0, hi = blocks - 1;   // the last block that starts at or before r
     while (lo < hi) {
@@ -715,7 +768,10 @@ __global__ void __launch_bounds__(kPlanBlock) tg_prefill_mod_plan_kernel(ModPara
       else
         hi = mid - 1;
     }
-    p.list[place(0, r)] = lo | ((r - starts[lo]) << 10);
+    const Walk cw = walks[lo];
+    const int2 share = shares[lo];
+    const int piece = r - starts[lo], t = piece * share.x + min(piece, share.y);
+    p.list[place(0, r)] = ListEntry{lo, t, t + share.x + (piece < share.y ? 1 : 0), cw.nh, cw.ct0, r, {0, 0}};
   }
 }
 
@@ -857,12 +913,11 @@ extern "C" int32_t tg_prefill_mod(const tg_prefill_args* a, const tg_score_mod* 
     p.part_o = reinterpret_cast<f32x4*>(ws);
     p.part_ml = reinterpret_cast<float*>(ws + sl.o_bytes);
     p.pieces = reinterpret_cast<int2*>(ws + sl.o_bytes + sl.ml_bytes);
-    p.blocks = reinterpret_cast<int4*>(ws + sl.o_bytes + sl.ml_bytes + sl.pieces_bytes);
-    p.list = reinterpret_cast<int32_t*>(ws + sl.o_bytes + sl.ml_bytes + sl.pieces_bytes + sl.blocks_bytes);
+    p.list = reinterpret_cast<ListEntry*>(ws + sl.o_bytes + sl.ml_bytes + sl.pieces_bytes);
     p.part_waves = sl.part_waves;
     p.list_len = 8 * sl.list_per_xcd;
-    hipLaunchKernelGGL(tg_prefill_mod_plan_kernel, dim3(1), dim3(kPlanBlock), 0, st, p, split_target(g.head_dim),
-                       split_at_once(g.head_dim));
+    auto plan = g.head_dim == 128 ? &tg_prefill_mod_plan_kernel<128> : &tg_prefill_mod_plan_kernel<64>;
+    hipLaunchKernelGGL(plan, dim3(1), dim3(kPlanBlock), 0, st, p);
     e = hipGetLastError();
     if (e != hipSuccess) return tg::fail(TG_ERR_HIP, "prefill plan launch failed: %s", hipGetErrorString(e));
     hipLaunchKernelGGL(pick_mod<true>(g.head_dim, cap), dim3(p.list_len), dim3(kBlock), 0, st, p);
