@@ -49,7 +49,8 @@ int32_t check_geometry(const tg_geometry* g) {
 
 int32_t check_softcap(float softcap, float sm_scale) {
   if (!(softcap >= 1e-3f && softcap <= 1e6f)) return fail(TG_ERR_INVALID_ARG, "softcap %g outside [1e-3, 1e6]", softcap);
-  if (!(sm_scale >= 0.f) || !std::isfinite(sm_scale)) return fail(TG_ERR_INVALID_ARG, "sm_scale must be finite and >= 0");
+  if (!(sm_scale >= 0.f) || !std::isfinite(sm_scale) || !std::isfinite(sm_scale / softcap))
+    return fail(TG_ERR_INVALID_ARG, "sm_scale must be finite and >= 0, also over softcap");
   return TG_OK;
 }
 

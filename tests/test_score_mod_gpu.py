@@ -171,7 +171,7 @@ def test_prefill_masks_and_caps(mask, cap, split, H, gqa, d, Hp, B, C, ctx, toke
     p.check(f"prefill {mask} cap {cap} split {split}")
 
 
-@pytest.mark.parametrize("cap,q_scale", [(50.0, 3.0), (1.0, 10.0), (1000.0, 1.0), (30.0, 8.0), (0.01, 4.0), (1e-3, 1.0)])
+@pytest.mark.parametrize("cap,q_scale", [(50.0, 3.0), (1.0, 10.0), (1000.0, 1.0), (30.0, 8.0), (0.01, 4.0), (1e-3, 1.0), (1e6, 2.0)])
 @pytest.mark.parametrize("d", [64, 128])
 def test_prefill_caps_from_far_below_to_far_above_the_scores(cap, q_scale, d):
     _gpu()

@@ -48,6 +48,11 @@ def test_scales(scale):
     refused(lambda: tg.tg_decode_capped(decode_args(sm_scale=scale), 5.0), INVALID)
 
 
+def test_a_scale_that_the_cap_cannot_take():
+    refused(lambda: tg.tg_prefill_mod(prefill_args(sm_scale=3e38), tg.make_score_mod(1e-3)), INVALID)
+    refused(lambda: tg.tg_decode_capped(decode_args(sm_scale=3e38), 1e-3), INVALID)
+
+
 @pytest.mark.parametrize("kw,code", [(dict(dtype=tg.TG_F32), UNSUPPORTED), (dict(chunk_len=0), INVALID),
                                      (dict(layer=2), INVALID), (dict(q=None), INVALID), (dict(out=FAKE + 8), INVALID),
                                      (dict(geom=tg.tg_geometry(2, 4, 8, 96, 16, 2)), UNSUPPORTED),
