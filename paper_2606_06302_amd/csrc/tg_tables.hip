@@ -262,13 +262,12 @@ struct MapParams {
   int32_t n, layer, L, H, G, Hp, P;
 };
 
-// Grid (ceil(n / kMapPerBlock), units): kMapPerBlock entries of one head.
+// Grid (ceil(n / kMapPerBlock), heads, requests): kMapPerBlock entries of one head.
 constexpr int kMapPerBlock = 4 * kBlock;
 
 __global__ void __launch_bounds__(kBlock) tg_slot_map_kernel(MapParams p) {
-  const int64_t unit = blockIdx.y + (int64_t)blockIdx.z * gridDim.y;
-  const int h = (int)(unit % p.H);
-  const int64_t b = unit / p.H;
+  const int h = blockIdx.y;
+  const int64_t b = blockIdx.z, unit = b * p.H + h;
   const int64_t at = (b * p.L + p.layer) * p.H + h;
   const int64_t lh = (int64_t)p.layer * p.H + h;
   const int64_t t = (b * p.L + p.layer) * p.G + p.group_of[lh];
@@ -278,7 +277,7 @@ __global__ void __launch_bounds__(kBlock) tg_slot_map_kernel(MapParams p) {
   const int64_t end = p.len ? min<int64_t>(p.len[at], cap) : cap;
   const int slot = p.slot_of[lh];
   for (int q = 0; q < 4; ++q) {
-    const int j = (int)blockIdx.x * kMapPerBlock + q * kBlock + threadIdx.x;
+    const int64_t j = (int64_t)blockIdx.x * kMapPerBlock + q * kBlock + threadIdx.x;
     if (j >= p.n) return;
     const int64_t e = first + j;
     int64_t row = -1;
