@@ -694,7 +694,8 @@ int32_t tg_rope_turns(int32_t n, const double* theta, uint64_t* turns);
  *   (y_a, y_b) of every rotated pair becomes attn_factor * (y_a cos t - y_b sin t,
  *     y_b cos t + y_a sin t), t = position * theta_j; dims at or past rot_dim
  *     are left as y.
- * Everything in fp32, rounded to the type once, at the end.
+ * Everything in fp32 (the sum of x^2 too: a head past 1e19 in size is outside
+ * its range), rounded to the type once, at the end.
  * rot_dim: 0 (no rotation, turns not read) or a multiple of 16 up to head_dim;
  * attn_factor: 0 means 1; eps >= 0.  turns, q_weight [d] and k_weight [d]
  * (dtype of the call) are DEVICE pointers, the weights 16-byte aligned. */
@@ -837,8 +838,8 @@ int32_t tg_reserve_device(const tg_reserve_device_args* args, void* hip_stream);
  * lengths these are the slots that the next n tokens take; with begin NULL and
  * len = the live lengths, the whole head.
  * DEVICE pointers: pt_offsets, pt_pages, group_of, slot_of as tg_append's; begin,
- * len [B][L][H] int32 or NULL; map [B][H][n] int64.  n >= 1.  Any head_dim and
- * page_size.  Errors: TG_ERR_INVALID_ARG, TG_ERR_HIP. */
+ * len [B][L][H] int32 or NULL; map [B][H][n] int64.  n >= 1; batch and
+ * num_kv_heads <= 65535.  Any head_dim and page_size.  Errors: TG_ERR_INVALID_ARG, TG_ERR_HIP. */
 typedef struct {
   tg_geometry geom;
   int32_t batch;
@@ -870,7 +871,7 @@ int32_t tg_slot_map(const tg_slot_map_args* args, void* hip_stream);
  *   chunk_tokens [B] int32 DEVICE pointer or NULL (all C): tokens at or past
  *     chunk_tokens[b] are no keys, and their output rows are left as they were.
  * A row that sees no key gives zeros (so does one whose visible scores are all
- * -inf).  What keys that a row does not see hold, NaN and infinities included,
+ * -inf, without a cap; with one they are -softcap).  What keys that a row does not see hold, NaN and infinities included,
  * does not reach its output.
  * The other arguments, the workspace, the schedule (whose costs count the causal
  * tiles) and the supported shapes are tg_prefill's; sm_scale must be >= 0. */

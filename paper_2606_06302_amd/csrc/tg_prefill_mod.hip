@@ -36,6 +36,7 @@
 // launch.
 #include <hip/hip_runtime.h>
 
+#include <cfloat>
 #include <cmath>
 #include <type_traits>
 
@@ -482,8 +483,10 @@ __global__ void __launch_bounds__(kBlock, kWavesPerSimd) tg_prefill_mod_kernel(M
         int from = is_chunk ? mine.lo - first : mine.hist ? 0 : 32;
         int to = (is_chunk ? mine.hi : hist) - first;
         auto sees = [&](int r) { return 8 * (r >> 2) + (r & 3) >= from && 8 * (r >> 2) + (r & 3) < to; };
-        float mx = -INFINITY, big = 0.f;
+        // a seen score of -infinity is a score of -softcap where there is a cap
+        float mx = kCap ? -FLT_MAX : -INFINITY, big = 0.f;
         if (masked) {
+          if (max(from + 4 * half, 0) >= min(to + 4 * half, 32)) mx = -INFINITY;   // no key of the block
 #pragma unroll
           for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sees(r) ? sc[r] : -INFINITY);
         } else {

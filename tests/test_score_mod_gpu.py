@@ -292,6 +292,21 @@ def test_history_that_only_some_rows_see_may_hold_infinities():
         assert torch.equal(p.s.out[0, 0::2][..., rest], clean[0, 0::2][..., rest])
 
 
+@pytest.mark.parametrize("split", [False, True])
+@pytest.mark.parametrize("d", [64, 128])
+def test_infinite_scores_are_capped(d, split):
+    """Scores of +-infinity are +-softcap: also where they are the first that a row sees, or all that it sees."""
+    _gpu()
+    for mask, cap in (("causal", 2.0), ("bidirectional", 4.0), ("documents", 1.0), ("any", 3.0), ("causal", 200.0)):
+        p = Prefill(13, 1, 4, d, 1, 1, 100, 70, mask, cap, hist=0, split=split)
+        p.s.q[..., 0] = 1.0
+        p.s.k_new[0, :40, 0, 0] = -float("inf")
+        p.s.k_new[0, 70, 0, 0] = float("inf")
+        p.s.run()
+        torch.cuda.synchronize()
+        p.check(f"infinite scores {mask} cap {cap} split {split}")
+
+
 def test_prefill_graph_and_streams():
     """Two captured calls with workspaces of their own, replayed side by side with new inputs, against the eager call."""
     _gpu()
