@@ -338,3 +338,40 @@ def test_append_graph_replays():
         torch.cuda.synchronize()
         assert torch.equal(q, q2) and torch.equal(pool, ref_pool) and torch.equal(live, ref_live), i
     assert int(live.min()) == 8
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f32", 64)])
+def test_rows_and_pages_past_32_bits(dtype, d):
+    """Projection rows whose second token lies past 2^32 bytes, and a pool whose pages do: bit for bit the result of
+    dense ones."""
+    _gpu()
+    H, Hp, gqa, P = 4, 2, 2, 16
+    c = Case(dtype, d, gqa, H, 2, 1, 32, "half", True, seed=31)
+    c.geom = tg.tg_geometry(1, H, H * gqa, d, P, Hp)
+    esz = c.rows.element_size()
+    outs, far = c.outputs(), c.outputs()
+    tg.tg_rope(c.args(outs))
+    stride = (2 ** 32 + 2 ** 20) // esz
+    wide = torch.empty(stride + c.rows.shape[1], dtype=c.rows.dtype, device="cuda")
+    near = c.rows
+    c.rows = torch.as_strided(wide, near.shape, (stride, 1))
+    c.rows.copy_(near)
+    tg.tg_rope(c.args(far))
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(outs, far))
+
+    group_of, slot_of, offsets, pages, live, n = tables(2, 1, H, Hp, P, np.full((2, 1, H), 17), 48, 3)
+    page = 2 * Hp * P * d
+    shift = (2 ** 32 + 2 ** 20) // (page * esz)
+    pools = [torch.zeros(n, 2, Hp, P, d, dtype=c.rows.dtype, device="cuda"),
+             torch.empty(n + shift, 2, Hp, P, d, dtype=c.rows.dtype, device="cuda")]
+    pools[1][shift:].zero_()
+    q = [x[0] for x in (outs, far)]
+    for pool, q_, pg, rows in zip(pools, q, (pages, pages + shift), (near, c.rows)):
+        q_.fill_(float("nan"))
+        c.rows = rows
+        tg.tg_rope_append(tg.make_rope_append_args(c.geom, 2, 0, c.tg_dtype, c.spec, *c.parts(), c.positions, q_, pool, pg,
+                                                   offsets, group_of, slot_of, live.clone()))
+    torch.cuda.synchronize()
+    assert torch.equal(*q) and torch.equal(pools[0], pools[1][shift:])
+    assert int((pools[0] != 0).any(-1).sum()) == 2 * H * 2

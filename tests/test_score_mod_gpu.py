@@ -335,6 +335,27 @@ def test_prefill_graph_and_streams():
             assert torch.equal(got.nan_to_num(1e9), p.s.out.nan_to_num(1e9)), i
 
 
+@pytest.mark.parametrize("split", [False, True])
+@pytest.mark.parametrize("d", [64, 128])
+def test_pages_past_32_bits(d, split):
+    """The same cache at the end of a pool of more than 2^32 bytes."""
+    _gpu()
+    p = Prefill(15, 2, 4, d, 1, 2, 70, 300, "documents", 10.0, split=split)
+    p.s.run()
+    torch.cuda.synchronize()
+    near = p.s.out.clone()
+    n, page = p.s.pool.shape[0], p.s.pool[0].numel() * 2
+    shift = (2 ** 32 + 2 ** 20) // page
+    pool = torch.empty(n + shift, *p.s.pool.shape[1:], dtype=torch.bfloat16, device="cuda")
+    pool[shift:].copy_(p.s.pool)
+    pages = p.t.d_pt_pages + shift
+    p.s.args.kv_pool, p.s.args.pt_pages = pool.data_ptr(), pages.data_ptr()
+    p.s.out.fill_(float("nan"))
+    p.s.run()
+    torch.cuda.synchronize()
+    assert torch.equal(p.s.out, near)
+
+
 # ---------------------------------------------------------------------- decode
 def check_decode(s, cap, what):
     g, t, wl = s.wl.geom, s.t, s.wl

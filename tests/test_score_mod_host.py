@@ -77,3 +77,21 @@ def test_null_arguments():
     assert tg._lib.tg_prefill_mod(None, C.byref(mod), None) == INVALID
     assert tg._lib.tg_prefill_mod(C.byref(prefill_args()), None, None) == INVALID
     assert tg._lib.tg_decode_capped(None, 5.0, None) == INVALID
+
+
+def test_struct_layout_matches_the_header(tmp_path):
+    import os
+    import shutil
+    import subprocess
+    cc = shutil.which("gcc") or shutil.which("cc")
+    if cc is None:
+        pytest.skip("no host C compiler")
+    s = tg.tg_score_mod
+    lines = ['#include <stdio.h>', '#include <stddef.h>', '#include "tangram.h"', "int main(void) {",
+             'printf("%zu\\n", sizeof(tg_score_mod));']
+    lines += [f'printf("%zu\\n", offsetof(tg_score_mod, {f[0]}));' for f in s._fields_]
+    (tmp_path / "l.c").write_text("\n".join(lines + ["return 0; }"]))
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    subprocess.run([cc, "-std=c99", f"-I{root}/include", str(tmp_path / "l.c"), "-o", str(tmp_path / "l")], check=True)
+    got = [int(x) for x in subprocess.run([str(tmp_path / "l")], capture_output=True, text=True, check=True).stdout.split()]
+    assert got == [C.sizeof(s)] + [getattr(s, f[0]).offset for f in s._fields_]
