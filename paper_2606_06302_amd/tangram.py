@@ -551,13 +551,17 @@ def make_rope_spec(layout=TG_ROPE_HALF, rot_dim=0, turns=None, attn_factor=1.0, 
                         float(weight_offset), _dptr(q_weight), _dptr(k_weight))
 
 
-def _token_stride(t):
+def _token_stride(t, tokens, width):
     """Elements between consecutive tokens of a [tokens][heads * d] tensor (a view of wider rows, say)."""
     if t is None:
         return 0
-    assert t.dim() == 2 and t.stride(1) == 1, "projection rows are [tokens][heads * d] with contiguous heads"
-    # a single row may report any stride
-    return int(t.stride(0)) if t.shape[0] > 1 else max(int(t.stride(0)), int(t.shape[1]))
+    assert tuple(t.shape) == (tokens, width) and t.stride(1) == 1, "projection rows are [tokens][heads * d], heads contiguous"
+    return int(t.stride(0)) if tokens > 1 else width   # a single row may report any stride
+
+
+def _qkv_strides(g, tokens, q, k, v):
+    qw, kw = g.num_q_heads * g.head_dim, g.num_kv_heads * g.head_dim
+    return _token_stride(q, tokens, qw), _token_stride(k, tokens, kw), _token_stride(v, tokens, kw)
 
 
 def make_rope_args(geom, batch, chunk_len, dtype, spec, q_in, k_in, v_in, q_out, k_out, v_out, positions=None,
@@ -565,7 +569,7 @@ def make_rope_args(geom, batch, chunk_len, dtype, spec, q_in, k_in, v_in, q_out,
     """Packs a tg_rope_args from device tensors (kept alive by the caller); q_in, k_in, v_in are [B*C][heads * d],
     views of one projection's rows or tensors of their own."""
     return tg_rope_args(_geom(geom), int(batch), int(chunk_len), int(dtype), spec, _dptr(q_in), _dptr(k_in), _dptr(v_in),
-                        _token_stride(q_in), _token_stride(k_in), _token_stride(v_in), _dptr(positions), _dptr(start),
+                        *_qkv_strides(geom, int(batch) * int(chunk_len), q_in, k_in, v_in), _dptr(positions), _dptr(start),
                         _dptr(chunk_tokens), _dptr(q_out), _dptr(k_out), _dptr(v_out))
 
 
@@ -578,8 +582,8 @@ def make_rope_append_args(geom, batch, layer, dtype, spec, q_in, k_in, v_in, pos
     """Packs a tg_rope_append_args from device tensors (kept alive by the caller); q_in, k_in, v_in are
     [B][heads * d] as in make_rope_args."""
     return tg_rope_append_args(_geom(geom), int(batch), int(layer), int(dtype), spec, _dptr(q_in), _dptr(k_in),
-                               _dptr(v_in), _token_stride(q_in), _token_stride(k_in), _token_stride(v_in),
-                               _dptr(positions), _dptr(q_out), _dptr(kv_pool), _dptr(pt_pages), _dptr(pt_offsets),
+                               _dptr(v_in), *_qkv_strides(geom, int(batch), q_in, k_in, v_in), _dptr(positions),
+                               _dptr(q_out), _dptr(kv_pool), _dptr(pt_pages), _dptr(pt_offsets),
                                _dptr(group_of), _dptr(slot_of), _dptr(live_len), _dptr(full))
 
 

@@ -175,6 +175,20 @@ def test_slot_map_refusals(kw):
     assert e.value.code == INVALID
 
 
+@pytest.mark.parametrize("shape", [(3, 512), (5, 512), (4, 448), (4, 576), (512, 4)])
+def test_projection_rows_of_another_shape(shape):
+    """The binding takes a projection's rows by their shape: other ones would be read past their end."""
+    import torch
+    ok, bad = torch.zeros(4, 512), torch.zeros(*shape)
+    assert tg.make_rope_args(G, 2, 2, tg.TG_F32, tg.make_rope_spec(), ok, None, None, ok, None, None).q_stride == 512
+    assert tg.make_rope_args(G, 2, 2, tg.TG_F32, tg.make_rope_spec(), torch.zeros(4, 640)[:, :512], None, None, ok, None,
+                             None).q_stride == 640
+    with pytest.raises(AssertionError):
+        tg.make_rope_args(G, 2, 2, tg.TG_F32, tg.make_rope_spec(), bad, None, None, ok, None, None)
+    with pytest.raises(AssertionError):
+        tg.make_rope_append_args(G, 4, 0, tg.TG_F32, tg.make_rope_spec(), bad, ok, ok, ok, ok, ok, ok, ok, ok, ok, ok)
+
+
 def test_null_argument_blocks():
     for name in ("tg_rope", "tg_rope_append", "tg_reserve_device", "tg_slot_map"):
         assert getattr(tg._lib, name)(None, None) == INVALID
