@@ -29,14 +29,20 @@
 //
 // Key-split launch.  With masks the blocks differ in length even within one
 // (request, KV head), so that a cut by the unit's length leaves most of the chip
-// idle (documents, five requests of 8 KV heads, chunk 333, head_dim 64: 68 us).  A first
-// launch of one workgroup reads the masks, sums every block's key tiles, cuts
-// blocks of more than T = max(kPrefillSplitMinTiles, total / target) tiles into
-// equal pieces and lays the pieces out in a list: the cut blocks' first, then the others in seven
-// classes of descending length, every class dealt to the 8 XCDs in runs, so
-// that the row tiles that share keys mostly run on one XCD.  Workgroup k runs
-// entry k / 8 of XCD k mod 8.  The pieces' fp32 partials are merged by a third
-// launch.
+// idle (documents, five requests of 8 KV heads, chunk 333, head_dim 64: 68 us, 57 by
+// the blocks' lengths).  A first launch of one workgroup reads the masks, sums every
+// block's key tiles, cuts blocks of more than T tiles (tg_prefill_mod_plan_kernel
+// says which) into equal pieces and lays the pieces out in a list: the cut blocks'
+// first, then the others in seven classes of descending length, every class dealt
+// to the 8 XCDs in runs, so that the row tiles that share keys mostly run on one
+// XCD.  Workgroup k runs entry k / 8 of XCD k mod 8.  The pieces' fp32 partials are
+// merged by a third launch.
+//
+// Bound as tg_prefill.hip's kernel, by products, their LDS reads and the softmax's
+// vector work that two waves of a SIMD share: 930 TFLOP/s without a cap, 800 with
+// one, on 16 requests of 16384 tokens.  A short call is bound by its three launches
+// (one request, chunk 512 behind 16384 tokens: plan 4, tiles 65, merge 9 us) and the
+// 5 us that a workgroup needs to its first tile.
 #include <hip/hip_runtime.h>
 
 #include <cfloat>

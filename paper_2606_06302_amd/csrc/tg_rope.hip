@@ -10,6 +10,10 @@
 // of squares, and the lanes of an access lie next to each other (adjacent pairs
 // with chunks 2i and 2i + 1: 44.2 us for 201 MB of f32, head_dim 64, 39.1 so).
 //
+// Bound by HBM where there are tokens enough (16 x 512 tokens of 32 + 16 heads of 128,
+// 201 MB: 38.6 us, 5.2 TB/s, the rate of a large copy), by latency for a step's
+// tokens (64 requests in 4.8 us, one in 3.9).
+//
 // Angles.  turns[j] is the rotation per token as a 64-bit fraction of a turn, so
 // position * turns[j] modulo 2^64 is the angle with every whole turn dropped,
 // exactly, at any position: no fp64 and no table over positions.  Its top 32

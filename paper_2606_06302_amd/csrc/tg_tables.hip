@@ -30,9 +30,9 @@ constexpr int kCopyBlocks = 1024;    // most workgroups that check or copy page 
 constexpr int kCopyPerBlock = 4096;  // ids of a workgroup before another one joins
 // One workgroup does it all up to so many tables, heads and page ids.  Against the
 // two launches, with a slot map behind, on the GPU's clock / with the host's
-// launches: 4 tables and 22 ids 8.9 / 11.5 us against 9.3 / 14.2; 256 tables, 6300
-// ids 9.5 / 11.0 against 10.3 / 14.0; 1024 tables, 15900 ids 12.9 / 13.4 against 11.1 /
-// 13.8.
+// launches: 4 tables and 74 ids 8.3 / 11.1 us against 8.9 / 14.0; 256 tables, 5700
+// ids 8.9 / 10.8 against 9.5 / 13.6; 1024 tables, 7400 ids 10.3 / 11.0 against 10.1 /
+// 13.7.
 constexpr int kSmallTables = kSmallBlock, kSmallHeads = 4 * kSmallBlock, kSmallIds = 12 * kSmallBlock;
 
 struct TableParams {
