@@ -13,14 +13,16 @@
 // the 32-key blocks that any of its rows sees and masks those that not all of
 // them see whole.
 //
-// Caps.  z = softcap * tanh(s / softcap) has exp's cost twice over, so where a
-// block's scores let it (the scores of a trained model do) tanh is an odd
+// Caps.  z = softcap * tanh(s / softcap) has exp's cost twice over, so where the
+// scores let it (the scores of a trained model do) tanh is an odd
 // polynomial whose last product goes into the exponent's subtraction: e = s *
 // P(s^2) - m, four full-rate instructions instead of one up to 0.365 of the cap
 // (16 requests of 8 KV heads, chunk 512, 16384 tokens before it, head_dim 128, cap 50: 830
 // us, 856 with five always, 719 uncapped; six requests, chunk 674, head_dim 64: 234 and
-// 255), five up to 0.65 of it, and tanh itself past that.  tanh is monotone: the
-// running maximum is kept of the raw scores and capped only when it is raised.
+// 255), five up to 0.65 of it, and tanh itself past that.  The greatest of the 16 scores
+// that a lane's row sees chooses for the lane, so that what a row does not see, other
+// rows' scores among it, changes no bit; the wave takes the longest of its lanes' ways.
+// tanh is monotone: the running maximum is kept of the raw scores and capped only when it is raised.
 //
 // Infinities and NaN that a row does not see.  A hidden key has probability 0,
 // and 0 * infinity is NaN.  Nothing is spent on it in the walk over the tiles: a
@@ -499,14 +501,18 @@ __global__ void __launch_bounds__(kBlock, kWavesPerSimd) tg_prefill_mod_kernel(M
         if (masked) {
           if (max(from + 4 * half, 0) >= min(to + 4 * half, 32)) mx = -INFINITY;   // no key of the block
 #pragma unroll
-          for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sees(r) ? sc[r] : -INFINITY);
+          for (int r = 0; r < 16; ++r) {
+            const bool seen = sees(r);
+            mx = fmaxf(mx, seen ? sc[r] : -INFINITY);
+            if constexpr (kCap) big = fmaxf(big, seen ? fabsf(sc[r]) : 0.f);
+          }
         } else {
 #pragma unroll
           for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sc[r]);
-        }
-        if constexpr (kCap) {
+          if constexpr (kCap) {
 #pragma unroll
-          for (int r = 0; r < 16; ++r) big = fmaxf(big, fabsf(sc[r]));
+            for (int r = 0; r < 16; ++r) big = fmaxf(big, fabsf(sc[r]));
+          }
         }
         mx = swap32_max(mx);
         const bool raise = (mx - m) * p.scale_log2 > kSlack;
@@ -526,26 +532,33 @@ __global__ void __launch_bounds__(kBlock, kWavesPerSimd) tg_prefill_mod_kernel(M
         if constexpr (!kCap) {
 #pragma unroll
           for (int r = 0; r < 16; ++r) sc[r] = fmaf(sc[r], p.scale_log2, -zr);
-        } else if (!kCareful && !__any(big > p.near_split)) {
+        } else if (!__any(big > p.near_split)) {
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
             const float u = sc[r] * sc[r];
             sc[r] = fmaf(sc[r], fmaf(u, fmaf(u, p.near[2], p.near[1]), p.near[0]), -zr);
           }
-        } else if (!kCareful && !__any(big > p.cap_split)) {
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const float u = sc[r] * sc[r];
-            float q = fmaf(u, p.poly[3], p.poly[2]);
-            q = fmaf(u, q, p.poly[1]);
-            q = fmaf(u, q, p.poly[0]);
-            sc[r] = fmaf(sc[r], q, -zr);
-          }
         } else {
+          // the lane's own greatest seen score chooses its polynomial: near's with a
+          // fourth coefficient of 0 is near's, bit for bit
+          const bool far = big > p.near_split;
+          const float c0 = far ? p.poly[0] : p.near[0], c1 = far ? p.poly[1] : p.near[1];
+          const float c2 = far ? p.poly[2] : p.near[2], c3 = far ? p.poly[3] : 0.f;
+          auto polynomial = [&](float x) {
+            const float u = x * x;
+            return fmaf(x, fmaf(u, fmaf(u, fmaf(u, c3, c2), c1), c0), -zr);
+          };
+          const bool beyond = big > p.cap_split;
+          if (!__any(beyond)) {
 #pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            sc[r] = fmaf(p.cap_log2, tanh_f32(sc[r] * p.cap_in), -zr);
-            __builtin_amdgcn_sched_barrier(0);   // one after the other: registers
+            for (int r = 0; r < 16; ++r) sc[r] = polynomial(sc[r]);
+          } else {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              const float e = fmaf(p.cap_log2, tanh_f32(sc[r] * p.cap_in), -zr);
+              sc[r] = beyond ? e : polynomial(sc[r]);
+              __builtin_amdgcn_sched_barrier(0);   // one after the other: registers
+            }
           }
         }
         if (masked) {
