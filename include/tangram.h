@@ -859,7 +859,7 @@ int32_t tg_slot_map(const tg_slot_map_args* args, void* hip_stream);
 /* ------------------------------- 12. attention with modified scores and masks
  * 12a. tg_prefill_mod: tg_prefill with
  *   softcap: 0, or in [1e-3, 1e6]: the scores s = sm_scale * q.k become
- *     softcap * tanh(s / softcap);
+ *     softcap * tanh(s / softcap), within 2^-13 + 6e-7 |s| beside what s itself is off by;
  *   key_begin, key_end [B][C] int32 DEVICE pointers or NULL: row i of request b
  *     sees the chunk keys j with key_begin[b][i] <= j < key_end[b][i] (clamped to
  *     the valid tokens; the row's own index is no limit), and the whole history

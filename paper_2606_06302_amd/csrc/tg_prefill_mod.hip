@@ -19,7 +19,7 @@
 // P(s^2) - m, four full-rate instructions instead of one up to 0.365 of the cap
 // (16 requests of 8 KV heads, chunk 512, 16384 tokens before it, head_dim 128, cap 50: 830
 // us, 856 with five always, 719 uncapped; six requests, chunk 674, head_dim 64: 234 and
-// 255), five up to 0.65 of it, and tanh itself past that.  The greatest of the 16 scores
+// 255), five up to 0.65 of it, and tanh itself past that and past scores of 31.  The greatest of the 16 scores
 // that a lane's row sees chooses for the lane, so that what a row does not see, other
 // rows' scores among it, changes no bit; the wave takes the longest of its lanes' ways.
 // tanh is monotone: the running maximum is kept of the raw scores and capped only when it is raised.
@@ -47,6 +47,7 @@
 // 5 us that a workgroup needs to its first tile.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cfloat>
 #include <cmath>
 #include <type_traits>
@@ -880,12 +881,15 @@ ModFn pick_mod(int d, bool cap) {
 }
 
 // tanh(x) / x as a polynomial in x^2 up to kCapSplit, and with one term less up to
-// kNearSplit, both fitted for the smallest relative error: 3.9e-6 and 3.7e-6, 1e-4 of
-// an exponent at a cap of 50 (P is rounded to 2^-8).
+// kNearSplit, both fitted for the smallest relative error: 3.9e-6 and 3.7e-6.  They are
+// an exponent's error by the score's size, so both also end at the score where it
+// reaches 2^-13, a 32nd of P's own rounding: 31.3, which caps up to 48 never reach within
+// kCapSplit, and past which tanh_f32 (2e-7) has it.
 constexpr double kCapSplit = 0.65;
 constexpr double kTanhPoly[4] = {0.999996112, -0.333035354, 0.129691085, -0.0391216061};
 constexpr double kNearSplit = 0.365;
 constexpr double kNearPoly[3] = {0.999996334, -0.332835182, 0.123176935};
+constexpr double kPolyReach = 0x1p-13 / 3.9e-6;   // in scaled scores
 
 }  // namespace
 
@@ -932,14 +936,15 @@ extern "C" int32_t tg_prefill_mod(const tg_prefill_args* a, const tg_score_mod* 
   if (cap) {
     p.cap_in = scale / mod->softcap;
     p.cap_log2 = mod->softcap * kLog2e;
-    p.cap_split = (float)(kCapSplit / p.cap_in);
+    const double reach = kPolyReach / mod->softcap;   // of the cap
+    p.cap_split = (float)(std::min(kCapSplit, reach) / p.cap_in);
     double power = (double)p.cap_log2 * p.cap_in;
     for (int i = 0; i < 4; ++i, power *= (double)p.cap_in * p.cap_in) {
       p.poly[i] = (float)(kTanhPoly[i] * power);
       // a coefficient that is no normal number: every block takes tanh itself
       if (!std::isnormal(p.poly[i])) p.cap_split = -1.f;
     }
-    p.near_split = p.cap_split < 0.f ? -1.f : (float)(kNearSplit / p.cap_in);
+    p.near_split = p.cap_split < 0.f ? -1.f : (float)(std::min(kNearSplit, reach) / p.cap_in);
     power = (double)p.cap_log2 * p.cap_in;
     for (int i = 0; i < 3; ++i, power *= (double)p.cap_in * p.cap_in) p.near[i] = (float)(kNearPoly[i] * power);
   }
