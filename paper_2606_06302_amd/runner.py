@@ -221,6 +221,17 @@ class DecodeSession:
             self.set_bin_weights(np.maximum(1, np.round(1000 * speed[cls])).astype(np.int32))
         return speed
 
+    def _append_tables(self):
+        """The flag and the tables that packed appends point at: made once, so that enable_append and
+        enable_projection do not take them from under each other.  The flag is cleared every time."""
+        if getattr(self, "full", None) is not None:
+            self.full.zero_()
+            return
+        self.full = torch.zeros(1, dtype=torch.int32, device=self.device)
+        self.d_offsets = to_device(self.t.pt_offsets, self.device)
+        self.d_group_of = to_device(self.t.group_of, self.device)
+        self.d_slot_of = to_device(self.t.slot_of, self.device)
+
     def enable_append(self, k_tok=None, v_tok=None, fused=False):
         """Device buffers for one decode step's new token per layer ([L][B][H][d] K and V) and the
         tg_append arguments of every layer; run_decode_step then appends before attending, with
@@ -231,10 +242,7 @@ class DecodeSession:
         shape = (g.num_layers, B, g.num_kv_heads, g.head_dim)
         self.k_tok = k_tok if k_tok is not None else torch.zeros(shape, dtype=self.dtype, device=dev)
         self.v_tok = v_tok if v_tok is not None else torch.zeros(shape, dtype=self.dtype, device=dev)
-        self.full = torch.zeros(1, dtype=torch.int32, device=dev)
-        self.d_offsets = to_device(self.t.pt_offsets, dev)
-        self.d_group_of = to_device(self.t.group_of, dev)
-        self.d_slot_of = to_device(self.t.slot_of, dev)
+        self._append_tables()
         self.append_args = {l: tg.make_append_args(g, B, l, self.tg_dtype, self.k_tok[l], self.v_tok[l], self.pool,
                                                    self.t.d_pt_pages, self.d_offsets, self.d_group_of,
                                                    self.d_slot_of, self.live_len, self.full) for l in self.layers}
@@ -260,12 +268,9 @@ class DecodeSession:
         then values) with the tokens' positions [B] int32: run_projected_step normalises, rotates and stores them
         (tg_rope_append into self.q and the cache), then attends."""
         assert self.open_end, "appending needs open-ended plans and live lengths"
-        g, B, dev = self.wl.geom, self.wl.batch, self.device
+        g, B = self.wl.geom, self.wl.batch
         self.rows, self.positions, self.spec = rows, positions, spec
-        self.full = torch.zeros(1, dtype=torch.int32, device=dev)
-        self.d_offsets = to_device(self.t.pt_offsets, dev)
-        self.d_group_of = to_device(self.t.group_of, dev)
-        self.d_slot_of = to_device(self.t.slot_of, dev)
+        self._append_tables()
         q, k = g.num_q_heads * g.head_dim, g.num_kv_heads * g.head_dim
         self.rope_append_args = {l: tg.make_rope_append_args(
             g, B, l, self.tg_dtype, spec, rows[l][:, :q], rows[l][:, q:q + k], rows[l][:, q + k:], positions, self.q[l],
