@@ -546,9 +546,33 @@ def tg_rope_turns(theta):
 def make_rope_spec(layout=TG_ROPE_HALF, rot_dim=0, turns=None, attn_factor=1.0, norm=False, eps=1e-6,
                    weight_offset=0.0, q_weight=None, k_weight=None) -> tg_rope_spec:
     """Packs a tg_rope_spec; turns is the device copy (8 bytes per pair) of tg_rope_freqs' result, the weights
-    [head_dim] device tensors of the call's type, or None."""
-    return tg_rope_spec(int(layout), int(rot_dim), _dptr(turns), float(attn_factor), int(norm), float(eps),
+    [head_dim] device tensors of the call's type, or None (kept alive by the caller)."""
+    assert turns is None or (turns.element_size() == 8 and turns.is_contiguous() and 2 * turns.numel() >= int(rot_dim)), \
+        "turns are rot_dim / 2 dense elements of 8 bytes"
+    spec = tg_rope_spec(int(layout), int(rot_dim), _dptr(turns), float(attn_factor), int(norm), float(eps),
                         float(weight_offset), _dptr(q_weight), _dptr(k_weight))
+    spec.weights = dict(q_weight=q_weight, k_weight=k_weight)   # their type is the call's, which is not known yet
+    return spec
+
+
+_FLOAT = {TG_F32: "float32", TG_BF16: "bfloat16"}
+
+
+def _array(what, t, dtype, n=0):
+    """t's pointer, or None: a dense tensor of the given type (of a call's dtype code, or by name) and at least n
+    elements, which is what the kernels take a pointer to be."""
+    if t is None:
+        return None
+    want = _FLOAT.get(dtype, dtype)
+    assert str(t.dtype) == f"torch.{want}", f"{what} is {want} (got {t.dtype})"
+    assert t.is_contiguous(), f"{what} is not contiguous"
+    assert t.numel() >= n, f"{what} holds {t.numel()} elements, needs {n}"
+    return _dptr(t)
+
+
+def _check_weights(spec, dtype):
+    for name, t in getattr(spec, "weights", {}).items():
+        _array(name, t, dtype)
 
 
 def _token_stride(t, tokens, width):
@@ -559,7 +583,10 @@ def _token_stride(t, tokens, width):
     return int(t.stride(0)) if tokens > 1 else width   # a single row may report any stride
 
 
-def _qkv_strides(g, tokens, q, k, v):
+def _qkv_strides(g, dtype, tokens, q, k, v):
+    for name, t in (("q_in", q), ("k_in", k), ("v_in", v)):
+        want = _FLOAT.get(int(dtype))
+        assert t is None or want is None or str(t.dtype) == f"torch.{want}", f"{name} is {want} (got {t.dtype})"
     qw, kw = g.num_q_heads * g.head_dim, g.num_kv_heads * g.head_dim
     return _token_stride(q, tokens, qw), _token_stride(k, tokens, kw), _token_stride(v, tokens, kw)
 
@@ -568,9 +595,14 @@ def make_rope_args(geom, batch, chunk_len, dtype, spec, q_in, k_in, v_in, q_out,
                    start=None, chunk_tokens=None) -> tg_rope_args:
     """Packs a tg_rope_args from device tensors (kept alive by the caller); q_in, k_in, v_in are [B*C][heads * d],
     views of one projection's rows or tensors of their own."""
-    return tg_rope_args(_geom(geom), int(batch), int(chunk_len), int(dtype), spec, _dptr(q_in), _dptr(k_in), _dptr(v_in),
-                        *_qkv_strides(geom, int(batch) * int(chunk_len), q_in, k_in, v_in), _dptr(positions), _dptr(start),
-                        _dptr(chunk_tokens), _dptr(q_out), _dptr(k_out), _dptr(v_out))
+    g, dtype, tokens = _geom(geom), int(dtype), int(batch) * int(chunk_len)
+    _check_weights(spec, dtype)
+    qn, kn = tokens * g.num_q_heads * g.head_dim, tokens * g.num_kv_heads * g.head_dim
+    return tg_rope_args(g, int(batch), int(chunk_len), dtype, spec, _dptr(q_in), _dptr(k_in), _dptr(v_in),
+                        *_qkv_strides(g, dtype, tokens, q_in, k_in, v_in), _array("positions", positions, "int32", tokens),
+                        _array("start", start, "int32", batch), _array("chunk_tokens", chunk_tokens, "int32", batch),
+                        _array("q_out", q_out, dtype, qn), _array("k_out", k_out, dtype, kn),
+                        _array("v_out", v_out, dtype, kn))
 
 
 def tg_rope(args: tg_rope_args, stream=None):
@@ -581,10 +613,16 @@ def make_rope_append_args(geom, batch, layer, dtype, spec, q_in, k_in, v_in, pos
                           pt_offsets, group_of, slot_of, live_len, full=None) -> tg_rope_append_args:
     """Packs a tg_rope_append_args from device tensors (kept alive by the caller); q_in, k_in, v_in are
     [B][heads * d] as in make_rope_args."""
-    return tg_rope_append_args(_geom(geom), int(batch), int(layer), int(dtype), spec, _dptr(q_in), _dptr(k_in),
-                               _dptr(v_in), *_qkv_strides(geom, int(batch), q_in, k_in, v_in), _dptr(positions),
-                               _dptr(q_out), _dptr(kv_pool), _dptr(pt_pages), _dptr(pt_offsets),
-                               _dptr(group_of), _dptr(slot_of), _dptr(live_len), _dptr(full))
+    g, B, dtype = _geom(geom), int(batch), int(dtype)
+    _check_weights(spec, dtype)
+    LH, tables = g.num_layers * g.num_kv_heads, B * g.num_layers * (g.num_kv_heads // max(1, g.heads_per_group))
+    return tg_rope_append_args(g, B, int(layer), dtype, spec, _dptr(q_in), _dptr(k_in), _dptr(v_in),
+                               *_qkv_strides(g, dtype, B, q_in, k_in, v_in), _array("positions", positions, "int32", B),
+                               _array("q_out", q_out, dtype, B * g.num_q_heads * g.head_dim),
+                               _array("kv_pool", kv_pool, dtype), _array("pt_pages", pt_pages, "int32"),
+                               _array("pt_offsets", pt_offsets, "int64", tables + 1),
+                               _array("group_of", group_of, "int32", LH), _array("slot_of", slot_of, "int32", LH),
+                               _array("live_len", live_len, "int32", B * LH), _array("full", full, "int32", 1))
 
 
 def tg_rope_append(args: tg_rope_append_args, stream=None):
@@ -600,11 +638,17 @@ def make_reserve_device_args(geom, batch, ctx_len, ratio, budget, group_of, free
     """Packs a tg_reserve_device_args from device tensors (kept alive by the caller): ctx_len, headroom int32 [B];
     ratio float64 [B][L][H] or budget float64 [L][H]; free_pages, pt_pages int32 (their lengths are num_free and
     pt_capacity); pages_needed int64 [1], status int32 [1]."""
-    return tg_reserve_device_args(_geom(geom), int(batch), _dptr(ctx_len), _dptr(headroom), _dptr(ratio), _dptr(budget),
-                                  _dptr(group_of), _dptr(free_pages), int(free_pages.numel()), int(pool_pages),
-                                  _dptr(kv_len), _dptr(group_len), _dptr(pt_offsets), _dptr(pt_pages),
-                                  int(pt_pages.numel()), _dptr(pages_needed), _dptr(status), _dptr(workspace),
-                                  0 if workspace is None else workspace.numel() * workspace.element_size())
+    g, B = _geom(geom), int(batch)
+    LH, tables = g.num_layers * g.num_kv_heads, B * g.num_layers * (g.num_kv_heads // max(1, g.heads_per_group))
+    return tg_reserve_device_args(g, B, _array("ctx_len", ctx_len, "int32", B), _array("headroom", headroom, "int32", B),
+                                  _array("ratio", ratio, "float64", B * LH), _array("budget", budget, "float64", LH),
+                                  _array("group_of", group_of, "int32", LH), _array("free_pages", free_pages, "int32"),
+                                  int(free_pages.numel()), int(pool_pages), _array("kv_len", kv_len, "int32", B * LH),
+                                  _array("group_len", group_len, "int32", tables),
+                                  _array("pt_offsets", pt_offsets, "int64", tables + 1),
+                                  _array("pt_pages", pt_pages, "int32"), int(pt_pages.numel()),
+                                  _array("pages_needed", pages_needed, "int64", 1), _array("status", status, "int32", 1),
+                                  _dptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size())
 
 
 def tg_reserve_device(args: tg_reserve_device_args, stream=None):
@@ -614,8 +658,13 @@ def tg_reserve_device(args: tg_reserve_device_args, stream=None):
 def make_slot_map_args(geom, batch, layer, pt_offsets, pt_pages, group_of, slot_of, n, map, begin=None,
                        len=None) -> tg_slot_map_args:
     """Packs a tg_slot_map_args from device tensors (kept alive by the caller); map is int64 [B][H][n]."""
-    return tg_slot_map_args(_geom(geom), int(batch), int(layer), _dptr(pt_offsets), _dptr(pt_pages), _dptr(group_of),
-                            _dptr(slot_of), _dptr(begin), _dptr(len), int(n), _dptr(map))
+    g, B = _geom(geom), int(batch)
+    LH, tables = g.num_layers * g.num_kv_heads, B * g.num_layers * (g.num_kv_heads // max(1, g.heads_per_group))
+    return tg_slot_map_args(g, B, int(layer), _array("pt_offsets", pt_offsets, "int64", tables + 1),
+                            _array("pt_pages", pt_pages, "int32"), _array("group_of", group_of, "int32", LH),
+                            _array("slot_of", slot_of, "int32", LH), _array("begin", begin, "int32", B * LH),
+                            _array("len", len, "int32", B * LH), int(n),
+                            _array("map", map, "int64", B * g.num_kv_heads * int(n)))
 
 
 def tg_slot_map(args: tg_slot_map_args, stream=None):
@@ -625,7 +674,8 @@ def tg_slot_map(args: tg_slot_map_args, stream=None):
 def make_score_mod(softcap=0.0, chunk_tokens=None, key_begin=None, key_end=None) -> tg_score_mod:
     """Packs a tg_score_mod from int32 device tensors (kept alive by the caller): chunk_tokens [B], key_begin and
     key_end [B][C]."""
-    return tg_score_mod(float(softcap), _dptr(chunk_tokens), _dptr(key_begin), _dptr(key_end))
+    return tg_score_mod(float(softcap), _array("chunk_tokens", chunk_tokens, "int32"), _array("key_begin", key_begin, "int32"),
+                        _array("key_end", key_end, "int32"))
 
 
 def tg_prefill_mod(args: tg_prefill_args, mod: tg_score_mod, stream=None):
