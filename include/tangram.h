@@ -796,10 +796,13 @@ int32_t tg_rope_append(const tg_rope_append_args* args, void* hip_stream);
  *     outside (0, 1], a group id outside [0, G) or a consumed page id outside
  *     the pool; TG_ERR_OUT_OF_PAGES; TG_ERR_BUFFER_TOO_SMALL (in this order).
  *   Unlike tg_reserve, distinctness of the consumed page ids is not checked.
- *   Where *status is not TG_OK every table is empty (all of pt_offsets is 0), so
- *     that calls already enqueued behind it touch no page; pages_needed is what
- *     the lengths need (lengths that are invalid count as 0), and pt_pages past
- *     the pages needed or taken is left as it was.
+ *   Where *status is not TG_OK every table is empty (all of pt_offsets is 0):
+ *     calls already enqueued behind it that go by pt_offsets (tg_append,
+ *     tg_rope_append, tg_slot_map, tg_prefill, tg_prefill_mod) touch no page.  In
+ *     all of these a group id outside [0, G) stands for an empty table too.
+ *     (tg_decode and tg_compress go by items that the host made of lengths it knew.)
+ *     pages_needed is then what the lengths need (lengths that are invalid count
+ *     as 0), and pt_pages past the pages needed or taken is left as it was.
  *   workspace: tg_reserve_device_workspace_bytes(geom, batch) bytes, no
  *     initialisation needed; calls that share one must not overlap in time.
  * Supported: num_kv_heads up to 256 (else TG_ERR_UNSUPPORTED).  Errors (host):

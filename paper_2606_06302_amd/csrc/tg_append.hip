@@ -9,6 +9,7 @@
 // after the rows are stored.
 #include <hip/hip_runtime.h>
 
+#include "tg_device.h"
 #include "tg_internal.h"
 
 namespace {
@@ -41,14 +42,12 @@ __global__ __launch_bounds__(kThreads) void tg_append_kernel(AppendParams p) {
   const int64_t lh = (int64_t)p.layer * p.H + h;
   int32_t* live = p.live_len + ((int64_t)b * p.L + p.layer) * p.H + h;
   const int n = *live;
-  const int64_t t = ((int64_t)b * p.L + p.layer) * p.G + p.group_of[lh];
-  const int64_t base = p.pt_offsets[t];
-  const int64_t cap = (p.pt_offsets[t + 1] - base) * p.P;
-  if (n < 0 || n >= cap) {
+  const tgd::TablePages table = tgd::table_of(p.pt_offsets, ((int64_t)b * p.L + p.layer) * p.G, p.group_of[lh], p.G);
+  if (n < 0 || n >= table.pages * p.P) {
     if (p.full && sub == 0) *p.full = 1;
     return;
   }
-  const int64_t page = p.pt_pages[base + n / p.P];
+  const int64_t page = p.pt_pages[table.base + n / p.P];
   const int64_t dst = ((page * 2 * p.Hp + p.slot_of[lh]) * p.P + n % p.P) * lpr + sub;
   const int64_t src = unit * lpr + sub;
   p.pool[dst] = p.k_tok[src];

@@ -99,4 +99,17 @@ __device__ __forceinline__ float tanh_f32(float x) {
   return a < kTanhSplit ? small : copysignf(large, x);
 }
 
+// Page tables in CSR form: the pages of a head whose group id may be anything, as
+// after a refused tg_reserve_device.  An id outside [0, groups) has none.
+struct TablePages {
+  int64_t base, pages;
+};
+template <typename Offsets>
+__device__ __forceinline__ TablePages table_of(Offsets pt_offsets, int64_t layer_tables, int group, int groups) {
+  const bool has = (uint32_t)group < (uint32_t)groups;
+  const int64_t t = layer_tables + (has ? group : 0);
+  const int64_t base = pt_offsets[t], end = pt_offsets[t + 1];
+  return {base, has ? end - base : 0};
+}
+
 }  // namespace tgd

@@ -146,9 +146,9 @@ __global__ void __launch_bounds__(kBlock, kWavesPerSimd) tg_prefill_kernel(Prefi
     int n = 0;
     if (u < n_units) {
       const int ub = u / p.num_kv_heads, uh = u % p.num_kv_heads;
-      const int64_t ti = ((int64_t)ub * p.num_layers + p.layer) * p.num_groups +
-                         p.group_of[(int64_t)p.layer * p.num_kv_heads + uh];
-      const int64_t ucap = (p.pt_offsets[ti + 1] - p.pt_offsets[ti]) * kPage;
+      const int ugrp = p.group_of[(int64_t)p.layer * p.num_kv_heads + uh];
+      const int64_t ucap =
+          table_of(p.pt_offsets, ((int64_t)ub * p.num_layers + p.layer) * p.num_groups, ugrp, p.num_groups).pages * kPage;
       const int64_t len = p.kv_len[((int64_t)ub * p.num_layers + p.layer) * p.num_kv_heads + uh];
       n = (int)((max<int64_t>(0, min<int64_t>(len, ucap)) + kTile - 1) / kTile) + p.last_tiles;
     }
@@ -213,10 +213,10 @@ __global__ void __launch_bounds__(kBlock, kWavesPerSimd) tg_prefill_kernel(Prefi
   const int b = unit / p.num_kv_heads, h = unit % p.num_kv_heads;
   const int grp = group_of[(int64_t)p.layer * p.num_kv_heads + h];
   const int slot = slot_of[(int64_t)p.layer * p.num_kv_heads + h];
-  const int64_t tidx = ((int64_t)b * p.num_layers + p.layer) * p.num_groups + grp;
-  const int64_t tbase = pt_offsets[tidx];
+  const TablePages table = table_of(pt_offsets, ((int64_t)b * p.num_layers + p.layer) * p.num_groups, grp, p.num_groups);
+  const int64_t tbase = table.base;
   // the history is clamped to the head's table: [0, pages * page_size]
-  const int64_t cap = (pt_offsets[tidx + 1] - tbase) * kPage;
+  const int64_t cap = table.pages * kPage;
   const int hist = (int)max<int64_t>(0, min<int64_t>(kv_len[((int64_t)b * p.num_layers + p.layer) * p.num_kv_heads + h], cap));
   const int npages = (hist + kPage - 1) / kPage;
   const int n_hist_tiles = (hist + kTile - 1) / kTile;

@@ -291,10 +291,10 @@ __global__ void __launch_bounds__(kBlock, kWavesPerSimd) tg_prefill_mod_kernel(M
   const int b = unit / p.num_kv_heads, h = unit % p.num_kv_heads;
   const int grp = group_of[(int64_t)p.layer * p.num_kv_heads + h];
   const int slot = slot_of[(int64_t)p.layer * p.num_kv_heads + h];
-  const int64_t tidx = ((int64_t)b * p.num_layers + p.layer) * p.num_groups + grp;
-  const int64_t tbase = pt_offsets[tidx];
+  const TablePages table = table_of(pt_offsets, ((int64_t)b * p.num_layers + p.layer) * p.num_groups, grp, p.num_groups);
+  const int64_t tbase = table.base;
   // the history is clamped to the head's table: [0, pages * page_size]
-  const int64_t cap = (pt_offsets[tidx + 1] - tbase) * kPage;
+  const int64_t cap = table.pages * kPage;
   const int hist = (int)max<int64_t>(0, min<int64_t>(kv_len[((int64_t)b * p.num_layers + p.layer) * p.num_kv_heads + h], cap));
   const int npages = (hist + kPage - 1) / kPage;
   const int row0 = rt * kRows;
@@ -697,9 +697,9 @@ __global__ void __launch_bounds__(kPlanBlock) tg_prefill_mod_plan_kernel(ModPara
   const int unit = kk / p.row_tiles, b_k = unit / p.num_kv_heads, h_k = unit % p.num_kv_heads;
   const int pair = b_k * p.row_tiles + kk % p.row_tiles;
   const int64_t bl = (int64_t)b_k * p.num_layers + p.layer;
-  const int64_t ti = bl * p.num_groups + p.group_of[(int64_t)p.layer * p.num_kv_heads + h_k];
+  const TablePages table =
+      table_of(p.pt_offsets, bl * p.num_groups, p.group_of[(int64_t)p.layer * p.num_kv_heads + h_k], p.num_groups);
   const int64_t len = p.kv_len[bl * p.num_kv_heads + h_k];
-  const int64_t off0 = p.pt_offsets[ti], off1 = p.pt_offsets[ti + 1];
   for (int i = threadIdx.x; i < p.list_len; i += kPlanBlock) p.list[i].block = -1;
   // kPairLanes lanes per (request, row tile)
   const int sub = lane % kPairLanes;
@@ -728,7 +728,7 @@ __global__ void __launch_bounds__(kPlanBlock) tg_prefill_mod_plan_kernel(ModPara
   lds_barrier();
   Walk w = {0, 0, 0};
   if (k < blocks) {
-    const int hist = (int)max<int64_t>(0, min<int64_t>(len, (off1 - off0) * kPage));
+    const int hist = (int)max<int64_t>(0, min<int64_t>(len, table.pages * kPage));
     w = block_walk((hist + kTile - 1) / kTile, min_lo[pair], max_hi[pair], any_hist[pair]);
     walks[k] = w;
   }

@@ -232,10 +232,8 @@ __global__ void __launch_bounds__(kBlock) tg_rope_kernel(RopeParams p) {
       const int64_t lh = (int64_t)p.layer * p.H + h;
       int32_t* live = p.live_len + (token * p.L + p.layer) * p.H + h;
       const int n = *live;
-      const int64_t t = (token * p.L + p.layer) * p.G + p.group_of[lh];
-      const int64_t base = p.pt_offsets[t];
-      const int64_t cap = (p.pt_offsets[t + 1] - base) * p.P;
-      if (n < 0 || n >= cap) {
+      const TablePages table = table_of(p.pt_offsets, (token * p.L + p.layer) * p.G, p.group_of[lh], p.G);
+      if (n < 0 || n >= table.pages * p.P) {
         if (p.full && sub == 0) *p.full = 1;
         continue;
       }
@@ -243,7 +241,7 @@ __global__ void __launch_bounds__(kBlock) tg_rope_kernel(RopeParams p) {
       const u4* vs = p.v_in + token * p.v_stride + (int64_t)h * CPR;
       u4 x[2] = {ks[c0], ks[c1]};
       const u4 v0 = vs[c0], v1 = vs[c1];
-      const int64_t page = p.pt_pages[base + n / p.P];
+      const int64_t page = p.pt_pages[table.base + n / p.P];
       u4* dst = p.pool + ((page * 2 * p.Hp + p.slot_of[lh]) * p.P + n % p.P) * CPR;
       turn(x, true);
       dst[c0] = x[0];

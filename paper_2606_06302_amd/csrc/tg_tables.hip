@@ -20,6 +20,7 @@
 // atomics on global memory, no order that the result could depend on.
 #include <hip/hip_runtime.h>
 
+#include "tg_device.h"
 #include "tg_internal.h"
 
 namespace {
@@ -295,9 +296,8 @@ __global__ void __launch_bounds__(kBlock) tg_slot_map_kernel(MapParams p) {
   const int64_t b = blockIdx.z, unit = b * p.H + h;
   const int64_t at = (b * p.L + p.layer) * p.H + h;
   const int64_t lh = (int64_t)p.layer * p.H + h;
-  const int64_t t = (b * p.L + p.layer) * p.G + p.group_of[lh];
-  const int64_t base = p.pt_offsets[t];
-  const int64_t cap = (p.pt_offsets[t + 1] - base) * p.P;
+  const tgd::TablePages table = tgd::table_of(p.pt_offsets, (b * p.L + p.layer) * p.G, p.group_of[lh], p.G);
+  const int64_t cap = table.pages * p.P;
   const int64_t first = p.begin ? p.begin[at] : 0;
   const int64_t end = p.len ? min<int64_t>(p.len[at], cap) : cap;
   const int slot = p.slot_of[lh];
@@ -307,7 +307,7 @@ __global__ void __launch_bounds__(kBlock) tg_slot_map_kernel(MapParams p) {
     const int64_t e = first + j;
     int64_t row = -1;
     if (e >= 0 && e < end) {
-      const int64_t page = p.pt_pages[base + e / p.P];
+      const int64_t page = p.pt_pages[table.base + e / p.P];
       row = (page * 2 * p.Hp + slot) * p.P + e % p.P;
     }
     p.map[unit * p.n + j] = row;
