@@ -55,12 +55,20 @@ class Tables:
         return int(kv.sum()) * 2 * g.head_dim * esz
 
 
+def _torch_stream(stream, device):
+    """The torch stream of a call's stream argument (None: the device's default stream, as in the library)."""
+    if stream is None:
+        return torch.cuda.default_stream(device)
+    return stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream), device=device)
+
+
 class DeviceTables:
     """The reservation of one workload with the block tables built on the GPU (tg_reserve_device): context lengths,
     ratios and the free list are device tensors, and nothing comes back to the host unless asked for.
 
     ctx_len, headroom int32 [B]; ratio float64 [B][L][H]; group_of, slot_of int32 [L][H]; free_pages int32, ids below
-    pool_pages; capacity: entries of the page array, at least what the lengths can need."""
+    pool_pages; capacity: entries of the page array, at least what the lengths can need.  What it allocates is cleared on
+    the current stream: a run on another one has to wait for that, as for the inputs."""
 
     def __init__(self, geom, ctx_len, ratio, group_of, slot_of, free_pages, pool_pages, capacity, headroom=None):
         B, L, H, G = ctx_len.numel(), geom.num_layers, geom.num_kv_heads, geom.num_kv_heads // geom.heads_per_group
@@ -75,23 +83,29 @@ class DeviceTables:
         self.d_status = torch.zeros(1, dtype=torch.int32, device=dev)
         self.workspace = torch.empty(tg.tg_reserve_device_workspace_bytes(geom, B), dtype=torch.uint8, device=dev)
         self.inputs = (ctx_len, ratio, free_pages, headroom)
+        self.enqueued = False
         self.args = tg.make_reserve_device_args(geom, B, ctx_len, ratio, None, group_of, free_pages, pool_pages,
                                                 self.d_kv_len, self.d_group_len, self.d_offsets, self.d_pt_pages,
                                                 self.d_needed, self.d_status, self.workspace, headroom=headroom)
 
     def run(self, stream=None):
         tg.tg_reserve_device(self.args, stream)
+        self.enqueued = True
 
     def check(self):
-        """Waits for the tables; raises TangramError where the reservation failed."""
+        """Waits for the tables, on whatever stream they are made (a captured run is replayed on any); raises
+        TangramError where the reservation failed."""
+        assert self.enqueued, "run() makes the tables"
+        torch.cuda.synchronize(self.device)
         code = int(self.d_status)
         if code != tg.TG_OK:
             raise tg.TangramError(code, "tg_reserve_device", tg.tg_status_string(code))
 
     def slot_map(self, layer, n, begin=None, length=None, out=None, stream=None):
-        """Pool rows of n entries per head of the layer (tg_slot_map): int64 [B][H][n]."""
+        """Pool rows of n entries per head of the layer (tg_slot_map): int64 [B][H][n], in memory of the call's stream."""
         if out is None:
-            out = torch.empty(self.batch, self.geom.num_kv_heads, n, dtype=torch.int64, device=self.device)
+            with torch.cuda.stream(_torch_stream(stream, self.device)):
+                out = torch.empty(self.batch, self.geom.num_kv_heads, n, dtype=torch.int64, device=self.device)
         tg.tg_slot_map(tg.make_slot_map_args(self.geom, self.batch, layer, self.d_offsets, self.d_pt_pages, self.d_group_of,
                                              self.d_slot_of, n, out, begin=begin, len=length), stream)
         return out

@@ -3,13 +3,14 @@ import numpy as np
 import pytest
 import torch
 
+from test_tables_gpu import Admission, cuda
 from workloads import Geometry, custom
 
 pytestmark = pytest.mark.gpu
 
 if torch.cuda.is_available():
     from paper_2606_06302_amd import tangram as tg
-    from paper_2606_06302_amd.runner import DecodeSession, Tables
+    from paper_2606_06302_amd.runner import DecodeSession, DeviceTables, Tables
 
 
 @pytest.mark.parametrize("fused", [False, True])
@@ -59,3 +60,62 @@ def test_steps_that_append_and_steps_that_project_alternate(fused):
         results.append((s.pool, *outs))
     for other in results[1:]:
         assert all(torch.equal(a, b) for a, b in zip(results[0], other))
+
+
+def device_tables(num_free=None):
+    a = Admission(3, 2, 4, 2, 16, [100, 77, 4000], num_free=num_free)
+    t = DeviceTables(a.geom, cuda(a.ctx), cuda(a.ratio), cuda(a.group_of), cuda(a.slot_of), cuda(a.free), a.pool_pages,
+                     a.capacity)
+    torch.cuda.synchronize()
+    return a, t
+
+
+@pytest.mark.parametrize("how", ["stream", "handle", "default behind another", "graph"])
+def test_the_status_is_waited_for_wherever_the_tables_are_made(how):
+    """Tables made on another stream than the current one, behind work that takes a while."""
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    full, _ = device_tables()
+    for num_free in (None, full.need - 1):
+        a, t = device_tables(num_free)
+        with pytest.raises(AssertionError):
+            t.check()
+        side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+        if how == "graph":
+            with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+                t.run(torch.cuda.current_stream())
+        on = torch.cuda.default_stream() if how == "default behind another" else side
+        with torch.cuda.stream(on):
+            torch.cuda._sleep(20_000_000)
+            if how == "graph":
+                graph.replay()
+            else:
+                t.run({"stream": side, "handle": side.cuda_stream}.get(how))
+        with torch.cuda.stream(torch.cuda.Stream()):
+            if num_free is None:
+                t.check()
+                assert int(t.d_needed) == a.need
+            else:
+                with pytest.raises(tg.TangramError) as e:
+                    t.check()
+                assert e.value.code == tg.TG_ERR_OUT_OF_PAGES
+
+
+@pytest.mark.parametrize("handle", [False, True])
+def test_a_slot_maps_memory_is_its_streams(handle):
+    """The map is allocated for the stream that writes it: memory that work on the current stream still reads is not taken."""
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    a, t = device_tables()
+    t.run()
+    t.check()
+    want = t.slot_map(1, 5000)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    busy = torch.full_like(want, 3)
+    torch.cuda._sleep(20_000_000)
+    sums = busy.sum()                  # enqueued, not run
+    del busy
+    got = t.slot_map(1, 5000, stream=side.cuda_stream if handle else side)
+    torch.cuda.synchronize()
+    assert int(sums) == 3 * want.numel() and torch.equal(got, want)
