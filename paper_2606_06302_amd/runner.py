@@ -112,7 +112,7 @@ class DeviceTables:
 
 
 class DecodeSession:
-    """Pool, queries, outputs and per-layer plans of one decode workload.  softcap > 0: the scores are capped
+    """Pool, queries, outputs and per-layer plans of one decode workload.  softcap not 0: the scores are capped
     (tg_decode_capped)."""
 
     def __init__(self, wl, tables: Tables = None, mode=tg.TG_PLAN_AOT, n_bins=None, split_target=None,
@@ -297,7 +297,7 @@ class DecodeSession:
             self._decode(self.dplans[l].args, stream)
 
     def _decode(self, args, stream):
-        if self.softcap > 0:
+        if self.softcap != 0:   # tg_decode_capped refuses what is no cap
             tg.tg_decode_capped(args, self.softcap, stream)
         else:
             tg.tg_decode(args, stream)

@@ -8,11 +8,11 @@ from paper_2606_06302_amd.runner import DecodeSession, Tables
 from workloads import Geometry, custom
 
 
-def session(fused=False):
+def session(fused=False, softcap=0.0):
     wl = custom(71, Geometry(2, 4, 8, 64, 16, 2), 3, "f32", (20, 60))
     t = Tables(wl, device="cpu", headroom=np.full(3, 4, np.int32))
     return DecodeSession(wl, tables=t, mode=tg.TG_PLAN_AOT_FILL, n_bins=8, fill="host", device="cpu", open_end=True,
-                         fused_merge=fused)
+                         fused_merge=fused, softcap=softcap)
 
 
 def project(s):
@@ -59,3 +59,13 @@ def test_enabling_clears_the_flag():
     s.full.fill_(1)
     project(s)
     assert int(s.full) == 0
+
+
+@pytest.mark.parametrize("cap", [-1.0, float("nan"), float("inf"), 1e-5])
+def test_a_cap_that_is_none_is_refused(cap):
+    """Not taken for no cap at all (the library refuses it on the host: nothing is launched)."""
+    s = session(softcap=cap)
+    for call in (lambda: s.run_layer(0), s.run_step):
+        with pytest.raises(tg.TangramError) as e:
+            call()
+        assert e.value.code == tg.TG_ERR_INVALID_ARG
