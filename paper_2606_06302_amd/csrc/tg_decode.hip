@@ -172,8 +172,8 @@ __device__ __forceinline__ int resolve_end(int tok_begin, int tok_end, int b, in
 
 // softcap * tanh(sm_scale * s / softcap) in log2 units.  The decode is bound by
 // memory, so a tanh per score in fp32 costs little: 32 requests of 8192 tokens, 8 KV
-// heads, head_dim 128, 61.4 -> 62.8 us (5.5 TB/s); at most 6 % (16 heads per KV head,
-// head_dim 64: 24.8 -> 26.3).
+// heads, head_dim 128, 61.4 -> 62.8 us (5.5 TB/s); more where the vector kernel has no
+// spare issue slots, up to 9 % (fp32, head_dim 64, three heads per KV head: 32.1 -> 35.0).
 __device__ __forceinline__ float cap_score(float s, const DecodeParams& p) { return p.scale * tanh_f32(s * p.scale_log2); }
 // log2 units and natural units per unit of score: capped scores are in log2 units
 template <bool kCap>
@@ -235,8 +235,15 @@ struct Tile {
   static_assert(kCPR == 8 || kCPR == 16 || kCPR == 32, "unsupported row size");
 };
 
+// Workgroups per CU that the compiler has to leave room for.  tg_decode_max_ctas counts
+// the uncapped kernels', and a plan of that many bins has to run at once with a cap
+// too: three fp32 heads of 64 dims take 95 registers without one and took 98 with it,
+// four workgroups instead of five (32 requests of 4096 tokens, 8 KV heads: 37.2 us, 35.7 so).
 template <typename T, int D, int GQA, bool kCap>
-__global__ void __launch_bounds__(kBlock) tg_decode_kernel(DecodeParams p, const tg_work_item* __restrict__ items,
+constexpr int vector_blocks() { return kCap && sizeof(T) == 4 && D == 64 && GQA == 3 ? 5 : 1; }
+
+template <typename T, int D, int GQA, bool kCap>
+__global__ void __launch_bounds__(kBlock, (vector_blocks<T, D, GQA, kCap>())) tg_decode_kernel(DecodeParams p, const tg_work_item* __restrict__ items,
                                                           const int32_t* __restrict__ pt_pages,
                                                           const int32_t* __restrict__ bin_offsets,
                                                           const u4* __restrict__ pool) {
