@@ -672,9 +672,11 @@ int32_t tg_read_probe(const tg_geometry* geom, int32_t dtype, const void* kv_poo
  *                   (1 - w) theta_j / factor + w theta_j, w = (n_j - low) / (high - low)
  *   TG_ROPE_YARN    the same, and cosine and sine times 0.1 ln(factor) + 1
  * All arithmetic in fp64.  turns [rot_dim / 2] uint64 out: turns per token,
- * theta_j / (2 pi) modulo 1, as a 64-bit binary fraction, which the kernels
- * multiply by the position modulo 2^64: the angle of any int32 position is
- * exact to 2^-52 of theta.  attn_factor out: 0.1 ln(factor) + 1 for TG_ROPE_YARN, else 1.
+ * theta_j / (2 pi) modulo 1, as a 64-bit binary fraction to the nearest 2^-64,
+ * which the kernels multiply by the position modulo 2^64.  In turns, an angle is
+ * off by position * 2^-64 (2^-33 at the ends of int32), by theta's own rounding
+ * in fp64 times the position, and by the 2^-32 below which the kernels drop it.
+ * attn_factor out: 0.1 ln(factor) + 1 for TG_ROPE_YARN, else 1.
  *   rot_dim even, >= 2; base > 1; factor >= 1; original_len >= 1 and 0 < low <
  *   high (BANDS, YARN; not read otherwise).
  * tg_rope_turns: the same conversion for n caller-made angular frequencies

@@ -1040,7 +1040,9 @@ static uint64_t turn_fraction(double theta) {
   constexpr long double kTwoPi = 6.283185307179586476925286766559L;
   const long double turns = (long double)theta / kTwoPi;
   const long double scaled = std::ldexp(turns - std::floor(turns), 64);
-  return scaled >= 18446744073709551615.5L ? 0 : (uint64_t)(scaled + 0.5L);
+  if (scaled >= 18446744073709551616.0L) return 0;   // a whole turn, after rounding
+  const uint64_t whole = (uint64_t)scaled;           // exact, and so is the rest (scaled + 0.5 is not, past 2^63)
+  return whole + (scaled - (long double)whole >= 0.5L ? 1 : 0);
 }
 
 extern "C" int32_t tg_rope_turns(int32_t n, const double* theta, uint64_t* turns) {
