@@ -670,7 +670,10 @@ int32_t tg_read_probe(const tg_geometry* geom, int32_t dtype, const void* kv_poo
  *                   the original context: theta_j where n_j >= high, theta_j /
  *                   factor where n_j <= low, between them
  *                   (1 - w) theta_j / factor + w theta_j, w = (n_j - low) / (high - low)
- *   TG_ROPE_YARN    the same, and cosine and sine times 0.1 ln(factor) + 1
+ *   TG_ROPE_YARN    the same, and cosine and sine times 0.1 ln(factor) + 1.  The ramp
+ *                   w is linear in the turns n_j; a model tuned with another one (linear
+ *                   in j between the pairs of high and low turns, say) has its own
+ *                   frequencies, which tg_rope_turns takes
  * All arithmetic in fp64.  turns [rot_dim / 2] uint64 out: turns per token,
  * theta_j / (2 pi) modulo 1, as a 64-bit binary fraction to the nearest 2^-64,
  * which the kernels multiply by the position modulo 2^64.  In turns, an angle is
@@ -872,7 +875,9 @@ int32_t tg_slot_map(const tg_slot_map_args* args, void* hip_stream);
  *     chunk from its first key); key_end NULL: i + 1 (causal).  A prefix mask is
  *     key_end = max(i + 1, prefix), documents packed into a chunk key_begin = the
  *     first token of the row's document (-1 for the one that continues the
- *     history), a window inside the chunk key_begin = i + 1 - window;
+ *     history), a window inside the chunk key_begin = max(i + 1 - window, 0), which
+ *     hides the history from every row (a history of kept entries has no distances
+ *     to cut it by); without the max, rows before the window-th see all of it;
  *   chunk_tokens [B] int32 DEVICE pointer or NULL (all C): tokens at or past
  *     chunk_tokens[b] are no keys, and their output rows are left as they were.
  * A row that sees no key gives zeros (so does one whose visible scores are all
