@@ -391,10 +391,15 @@ extern "C" int32_t tg_rope(const tg_rope_args* a, void* hip_stream) {
   p.Hq = a->q_in ? g.num_q_heads : 0;
   p.H = a->k_in ? g.num_kv_heads : 0;
   p.units = p.Hq + p.H + (a->v_in ? g.num_kv_heads : 0);
-  // Loads that leave nothing in the caches pay once input and output together
-  // no longer fit them (256 MB): 201 MB 40.6 -> 38.1 us, but 151 MB 27.4 -> 31.0, 50 MB
-  // 10.8 -> 11.0.  Stores that leave nothing pay at any size (201 MB 43.9 -> 40.6,
-  // 101 MB 22.3 -> 18.4, 50 MB level, 13 MB 4.9 -> 4.3).
+  // Loads that leave nothing in the caches, against plain ones, by where the rows are.
+  // Behind the product that wrote them (32 + 16 heads of 128, bf16): input and output
+  // 201 MB 36.6 -> 36.5 us, 403 MB 80.5 -> 70.0 (64 + 16 heads, 336 MB: 70.6 -> 71.8; head_dim 64,
+  // 235 MB: 46.3 -> 46.0).  From HBM they pay 1 to 4 % from 60 MB on (201 MB 40.2 -> 39.0; bf16
+  // of head_dim 64 loses as much: 43.1 -> 45.7), and rows still in the caches of a call before lose by
+  // them at every size (100 MB 17.6 -> 19.7, 201 MB 33.6 -> 37.5, 400 MB 61.5 -> 70.3).
+  // Between 151 and 201 MB nothing singles out a size: past it rows mostly come from HBM,
+  // below it from the caches.  Stores that leave nothing pay at any size (201 MB 43.9 ->
+  // 40.6, 101 MB 22.3 -> 18.4, 50 MB level, 13 MB 4.9 -> 4.3).
   const bool stream = 2 * p.tokens * p.units * g.head_dim * esz > ((int64_t)176 << 20);
   const RopeFn fn = stream ? pick_rope<false, true>(a->dtype, g.head_dim, a->spec.layout)
                            : pick_rope<false, false>(a->dtype, g.head_dim, a->spec.layout);
