@@ -16,12 +16,14 @@
 // Caps.  z = softcap * tanh(s / softcap) has exp's cost twice over, so where the
 // scores let it (the scores of a trained model do) tanh is an odd
 // polynomial whose last product goes into the exponent's subtraction: e = s *
-// P(s^2) - m, four full-rate instructions instead of one up to 0.365 of the cap
-// (16 requests of 8 KV heads, chunk 512, 16384 tokens before it, head_dim 128, cap 50: 830
-// us, 856 with five always, 719 uncapped; six requests, chunk 674, head_dim 64: 234 and
-// 255), five up to 0.65 of it, and tanh itself past that and past scores of 31.  The greatest of the 16 scores
+// P(s^2) - m, four full-rate instructions instead of one up to 0.365 of the cap,
+// five up to 0.625 of it.  Past that (and past scores of 33 and 42, which only caps past
+// 66 reach) tanh itself.  The greatest of the 16 scores
 // that a lane's row sees chooses for the lane, so that what a row does not see, other
 // rows' scores among it, changes no bit; the wave takes the longest of its lanes' ways.
+// 16 requests of 8 KV heads, chunk 512, 16384 tokens before it, gqa 4, head_dim 128, in us
+// by cap over the scores' standard deviation: none 670, 50/3 (all within 0.365) 780, 50/6
+// 838, 50/9 1009, 20/4 1074, 5/4 1237; head_dim 64: 380, 468, 511, 623, 648, 793.
 // tanh is monotone: the running maximum is kept of the raw scores and capped only when it is raised.
 //
 // Infinities and NaN that a row does not see.  A hidden key has probability 0,
@@ -80,6 +82,7 @@ struct ModParams {
   float cap_in, cap_log2, cap_split;
   float poly[4];
   float near_split, near[3];
+  float cap_exp;            // log2 of e^(2 |s| cap_in) per |s|; 0: the polynomials end before kCapSplit of the cap
   // key-split launch only
   f32x4* part_o;            // [split_slots][part_waves][D/4][32 rows] unnormalised fp32 outputs
   float* part_ml;           // [split_slots][part_waves][2][32 rows]: reference maximum in log2 units, sum
@@ -553,6 +556,16 @@ __global__ void __launch_bounds__(kBlock, kWavesPerSimd) tg_prefill_mod_kernel(M
           if (!__any(beyond)) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) sc[r] = polynomial(sc[r]);
+          } else if (p.cap_exp > 0.f) {
+            // tanh as 1 - 2 / (e^(2|x|) + 1), which does not cancel past the polynomial
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              const float s = sc[r];
+              const float large =
+                  fmaf(-2.f * p.cap_log2, __builtin_amdgcn_rcpf(fast_exp2(fabsf(s) * p.cap_exp) + 1.f), p.cap_log2);
+              sc[r] = fabsf(s) > p.cap_split ? copysignf(large, s) - zr : polynomial(s);
+              __builtin_amdgcn_sched_barrier(0);   // one after the other: registers
+            }
           } else {
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
@@ -881,15 +894,17 @@ ModFn pick_mod(int d, bool cap) {
 }
 
 // tanh(x) / x as a polynomial in x^2 up to kCapSplit, and with one term less up to
-// kNearSplit, both fitted for the smallest relative error: 3.9e-6 and 3.7e-6.  They are
-// an exponent's error by the score's size, so both also end at the score where it
-// reaches 2^-13, a 32nd of P's own rounding: 31.3, which caps up to 48 never reach within
-// kCapSplit, and past which tanh_f32 (2e-7) has it.
-constexpr double kCapSplit = 0.65;
-constexpr double kTanhPoly[4] = {0.999996112, -0.333035354, 0.129691085, -0.0391216061};
+// kNearSplit, both fitted for the smallest relative error.  They are an exponent's error
+// by the score's size, so both also end at the score where it reaches 2^-13, a 32nd of
+// P's own rounding: 41.8 and 33.3, which caps up to 66 and 91 do not reach within the
+// splits, and past which tanh_f32 (2e-7) has it.
+constexpr double kCapSplit = 0.625;
+constexpr double kTanhPoly[4] = {0.99999709, -0.333092316, 0.130154592, -0.0400295162};
+constexpr double kTanhError = 2.92e-6;
 constexpr double kNearSplit = 0.365;
-constexpr double kNearPoly[3] = {0.999996334, -0.332835182, 0.123176935};
-constexpr double kPolyReach = 0x1p-13 / 3.9e-6;   // in scaled scores
+constexpr double kNearPoly[3] = {0.999996334, -0.332835182, 0.123176933};
+constexpr double kNearError = 3.67e-6;
+constexpr double kPolyError = 0x1p-13;
 
 }  // namespace
 
@@ -936,7 +951,7 @@ extern "C" int32_t tg_prefill_mod(const tg_prefill_args* a, const tg_score_mod* 
   if (cap) {
     p.cap_in = scale / mod->softcap;
     p.cap_log2 = mod->softcap * kLog2e;
-    const double reach = kPolyReach / mod->softcap;   // of the cap
+    const double reach = kPolyError / kTanhError / mod->softcap;   // of the cap
     p.cap_split = (float)(std::min(kCapSplit, reach) / p.cap_in);
     double power = (double)p.cap_log2 * p.cap_in;
     for (int i = 0; i < 4; ++i, power *= (double)p.cap_in * p.cap_in) {
@@ -944,7 +959,8 @@ extern "C" int32_t tg_prefill_mod(const tg_prefill_args* a, const tg_score_mod* 
       // a coefficient that is no normal number: every block takes tanh itself
       if (!std::isnormal(p.poly[i])) p.cap_split = -1.f;
     }
-    p.near_split = p.cap_split < 0.f ? -1.f : (float)(std::min(kNearSplit, reach) / p.cap_in);
+    p.cap_exp = p.cap_split > 0.f && reach >= kCapSplit ? (float)(2.0 * kLog2e * p.cap_in) : 0.f;
+    p.near_split = p.cap_split < 0.f ? -1.f : (float)(std::min(kNearSplit, kPolyError / kNearError / mod->softcap) / p.cap_in);
     power = (double)p.cap_log2 * p.cap_in;
     for (int i = 0; i < 3; ++i, power *= (double)p.cap_in * p.cap_in) p.near[i] = (float)(kNearPoly[i] * power);
   }

@@ -53,8 +53,8 @@ def test_equal_scores_have_equal_weights(cap, d, split):
 
 @pytest.mark.parametrize("split", [False, True])
 @pytest.mark.parametrize("d", [64, 128])
-@pytest.mark.parametrize("cap", [50.0, 1e3, 1e4])
-@pytest.mark.parametrize("part", [0.2, 0.33, 0.45, 0.6])
+@pytest.mark.parametrize("cap", [50.0, 60.0, 80.0, 1e3, 1e4])
+@pytest.mark.parametrize("part", [0.2, 0.33, 0.45, 0.6, 0.7, 0.9])
 def test_scores_a_fifth_to_three_fifths_of_the_cap(part, cap, d, split):
     """Scores a few units apart around `part` of the cap; every other block also holds one far below."""
     _gpu()
