@@ -22,8 +22,8 @@
 // that a lane's row sees chooses for the lane, so that what a row does not see, other
 // rows' scores among it, changes no bit; the wave takes the longest of its lanes' ways.
 // 16 requests of 8 KV heads, chunk 512, 16384 tokens before it, gqa 4, head_dim 128, in us
-// by cap over the scores' standard deviation: none 670, 50/3 (all within 0.365) 780, 50/6
-// 838, 50/9 1009, 20/4 1074, 5/4 1237; head_dim 64: 380, 468, 511, 623, 648, 793.
+// by cap over the scores' standard deviation: none 727, 50/3 (all within 0.365) 822, 50/6
+// 883, 50/9 1080, 20/4 1156, 5/4 1324; head_dim 64: 418, 505, 546, 693, 730, 891.
 // tanh is monotone: the running maximum is kept of the raw scores and capped only when it is raised.
 //
 // Infinities and NaN that a row does not see.  A hidden key has probability 0,
@@ -42,11 +42,12 @@
 // XCD.  Workgroup k runs entry k / 8 of XCD k mod 8.  The pieces' fp32 partials are
 // merged by a third launch.
 //
-// Bound as tg_prefill.hip's kernel, by products, their LDS reads and the softmax's
-// vector work that two waves of a SIMD share: 930 TFLOP/s without a cap, 800 with
-// one, on 16 requests of 16384 tokens.  A short call is bound by its three launches
-// (one request, chunk 512 behind 16384 tokens: plan 4, tiles 65, merge 9 us) and the
-// 5 us that a workgroup needs to its first tile.
+// Bound as tg_prefill.hip's kernel, by products and the softmax's vector work, which the
+// two waves of a SIMD hardly overlap: counted on those 16 requests, the matrix cores are
+// busy 43 % of a SIMD's cycles and its vector ALU 46 % without a cap (918 TFLOP/s), 37 and
+// 57 % with one (813), LDS 19 to 22 %.  A short call is bound by its three
+// launches (one request, chunk 512 behind 16384 tokens: plan 4, tiles 65, merge 9 us) and
+// the 5 us that a workgroup needs to its first tile.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -580,6 +581,9 @@ __global__ void __launch_bounds__(kBlock, kWavesPerSimd) tg_prefill_mod_kernel(M
 #pragma unroll
           for (int r = 0; r < 16; ++r) sc[r] = sees(r) ? sc[r] : -INFINITY;
         }
+        // P is rounded to bf16 (2^-8) for its product and not for its sum: with normal
+        // values that is 1.3e-3 to 1.6e-3 of an output beside the 1.7e-3 of its own rounding; a second product for the rest of P would be 256 cycles more than a
+        // block's 512 of products
         u4 pb[2];
         {
           uint32_t pw[8];
