@@ -895,8 +895,8 @@ typedef struct {
 int32_t tg_prefill_mod(const tg_prefill_args* args, const tg_score_mod* mod, void* hip_stream);
 
 /* 12b. tg_decode_capped: tg_decode with the scores s = sm_scale * q.k replaced
- * by softcap * tanh(s / softcap), softcap in [1e-3, 1e6] (out, lse and the
- * partials are those of the capped scores).  Everything else, the in-launch
+ * by softcap * tanh(s / softcap), within 6e-7 |s|, softcap in [1e-3, 1e6] (out,
+ * lse and the partials are those of the capped scores).  Everything else, the in-launch
  * merge and append included, is tg_decode's; sm_scale must be >= 0. */
 int32_t tg_decode_capped(const tg_decode_args* args, float softcap, void* hip_stream);
 

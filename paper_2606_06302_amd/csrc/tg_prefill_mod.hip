@@ -582,8 +582,8 @@ __global__ void __launch_bounds__(kBlock, kWavesPerSimd) tg_prefill_mod_kernel(M
           for (int r = 0; r < 16; ++r) sc[r] = sees(r) ? sc[r] : -INFINITY;
         }
         // P is rounded to bf16 (2^-8) for its product and not for its sum: with normal
-        // values that is 1.3e-3 to 1.6e-3 of an output beside the 1.7e-3 of its own rounding; a second product for the rest of P would be 256 cycles more than a
-        // block's 512 of products
+        // values that is 1.3e-3 to 1.6e-3 of an output beside the 1.7e-3 of its own
+        // rounding; products for the rest of P would add half to the block's
         u4 pb[2];
         {
           uint32_t pw[8];
