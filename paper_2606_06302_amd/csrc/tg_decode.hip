@@ -243,10 +243,9 @@ template <typename T, int D, int GQA, bool kCap>
 constexpr int vector_blocks() { return kCap && sizeof(T) == 4 && D == 64 && GQA == 3 ? 5 : 1; }
 
 template <typename T, int D, int GQA, bool kCap>
-__global__ void __launch_bounds__(kBlock, (vector_blocks<T, D, GQA, kCap>())) tg_decode_kernel(DecodeParams p, const tg_work_item* __restrict__ items,
-                                                          const int32_t* __restrict__ pt_pages,
-                                                          const int32_t* __restrict__ bin_offsets,
-                                                          const u4* __restrict__ pool) {
+__global__ void __launch_bounds__(kBlock, (vector_blocks<T, D, GQA, kCap>()))
+    tg_decode_kernel(DecodeParams p, const tg_work_item* __restrict__ items, const int32_t* __restrict__ pt_pages,
+                     const int32_t* __restrict__ bin_offsets, const u4* __restrict__ pool) {
   using TL = Tile<T, D>;
   constexpr int CPR = TL::kCPR, EPC = TL::kEPC, TPL = TL::kTPL, NS = TL::kSlots;
 

@@ -18,13 +18,14 @@
 // polynomial whose last product goes into the exponent's subtraction: e = s *
 // P(s^2) - m, four full-rate instructions instead of one up to 0.365 of the cap,
 // five up to 0.625 of it.  Past that (and past scores of 33 and 42, which only caps past
-// 66 reach) tanh itself.  The greatest of the 16 scores
-// that a lane's row sees chooses for the lane, so that what a row does not see, other
-// rows' scores among it, changes no bit; the wave takes the longest of its lanes' ways.
+// 66 reach) tanh itself.  The greatest of the 16 scores that a lane's row sees chooses for
+// the lane, so that what a row does not see, other rows' scores among it, changes no bit;
+// the wave takes the longest of its lanes' ways.
 // 16 requests of 8 KV heads, chunk 512, 16384 tokens before it, gqa 4, head_dim 128, in us
 // by cap over the scores' standard deviation: none 727, 50/3 (all within 0.365) 822, 50/6
 // 883, 50/9 1080, 20/4 1156, 5/4 1324; head_dim 64: 418, 505, 546, 693, 730, 891.
-// tanh is monotone: the running maximum is kept of the raw scores and capped only when it is raised.
+// tanh is monotone: the running maximum is kept of the raw scores and capped only when
+// it is raised.
 //
 // Infinities and NaN that a row does not see.  A hidden key has probability 0,
 // and 0 * infinity is NaN.  Nothing is spent on it in the walk over the tiles: a
