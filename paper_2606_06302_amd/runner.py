@@ -236,15 +236,16 @@ class DecodeSession:
         return speed
 
     def _append_tables(self):
-        """The flag and the tables that packed appends point at: made once, so that enable_append and
-        enable_projection do not take them from under each other.  The flag is cleared every time."""
-        if getattr(self, "full", None) is not None:
-            self.full.zero_()
+        """The flag and the tables that packed appends point at: allocated once, so that enable_append and
+        enable_projection do not take them from under each other; the flag cleared and the tables taken anew every time."""
+        tables = self.t.pt_offsets, self.t.group_of, self.t.slot_of
+        if getattr(self, "full", None) is None:
+            self.full = torch.zeros(1, dtype=torch.int32, device=self.device)
+            self.d_offsets, self.d_group_of, self.d_slot_of = (to_device(a, self.device) for a in tables)
             return
-        self.full = torch.zeros(1, dtype=torch.int32, device=self.device)
-        self.d_offsets = to_device(self.t.pt_offsets, self.device)
-        self.d_group_of = to_device(self.t.group_of, self.device)
-        self.d_slot_of = to_device(self.t.slot_of, self.device)
+        self.full.zero_()
+        for d, a in zip((self.d_offsets, self.d_group_of, self.d_slot_of), tables):
+            d.copy_(torch.from_numpy(np.ascontiguousarray(a)))
 
     def enable_append(self, k_tok=None, v_tok=None, fused=False):
         """Device buffers for one decode step's new token per layer ([L][B][H][d] K and V) and the

@@ -53,6 +53,20 @@ def test_appends_and_projections_of_one_session_keep_their_tensors(order, fused)
     check(s, "append" in order, "projection" in order)
 
 
+@pytest.mark.parametrize("first,second", [("append", "append"), ("append", "projection"), ("projection", "append")])
+def test_enabling_again_takes_the_tables_as_they_are(first, second):
+    s = session()
+    enable = dict(append=s.enable_append, projection=lambda: project(s))
+    enable[first]()
+    held = s.d_offsets
+    s.t.pt_offsets, s.t.group_of = s.t.pt_offsets + 7, s.t.group_of[:, ::-1].copy()
+    enable[second]()
+    assert s.d_offsets is held
+    for d, a in ((s.d_offsets, s.t.pt_offsets), (s.d_group_of, s.t.group_of), (s.d_slot_of, s.t.slot_of)):
+        assert np.array_equal(d.numpy(), a)
+    check(s, "append" in (first, second), "projection" in (first, second))
+
+
 def test_enabling_clears_the_flag():
     s = session()
     s.enable_append()
