@@ -900,6 +900,103 @@ int32_t tg_prefill_mod(const tg_prefill_args* args, const tg_score_mod* mod, voi
  * merge and append included, is tg_decode's; sm_scale must be >= 0. */
 int32_t tg_decode_capped(const tg_decode_args* args, float softcap, void* hip_stream);
 
+/* --------------------------- 13. a cache in 4 or 8 bits (microscaled formats)
+ * The same ragged pages and tables with the retained rows quantised: a group of
+ * 32 consecutive dims of a K or V row shares a power-of-two scale, its elements
+ * are 4-bit (e2m1) or 8-bit (e4m3) floating-point numbers.  K and V choose their
+ * formats apart; a layer's entry of one head takes d * bits / 8 + d / 32 bytes a
+ * part (4 bits, head_dim 128: 68 instead of bf16's 256).
+ *   scale    2^e, e the least integer with max|x| <= top * 2^e over the group, top
+ *            7 (4 bits) or 464 (8 bits): the midpoint between the largest value
+ *            and the step that would follow it; e within [-125, 125] / [-117, 119]
+ *   element  x / 2^e to the nearest value, ties to the even code, at most the
+ *            largest (6 / 448); the sign is kept, also of 0
+ *   a group that holds a NaN or an infinity stands for NaNs (scale byte 255, codes 0)
+ * Every step but the element's rounding is exact, so what is stored depends on the
+ * row alone, and every stored value is a bf16 number.  The calls below attend to,
+ * and read back, exactly these values.
+ * Rows of normal values come back with an RMS error of 11.2 % of theirs in 4 bits
+ * and of 2.7 % in 8; keys whose channels differ much in size lose most in 4 bits.
+ *
+ * Layout.  A page holds H_p slabs, slab (page p, slot s) at byte (p * H_p + s) *
+ * slab, slab = 16 * d * (k_bits + v_bits) / 8 + d: K codes, V codes, K scales, V
+ * scales (bytes, e + 127).  Inside a part's codes the 64 lanes of a wave follow
+ * each other: lane 16 j + t has dims j * d/4 .. of token t's K row, lane 16 j + c
+ * dims c * d/16 .. of tokens 4j .. 4j + 3's V rows (token by token), d/4 elements a
+ * lane, the lower one of a byte's two in its low bits; lanes of 32 bytes lie in two
+ * planes of 16 bytes a lane.  Scales: K [d/32][16 tokens], V [4][d/32][4 tokens].
+ *
+ * Supported in all of these: head_dim 64 or 128, page_size 16 (else
+ * TG_ERR_UNSUPPORTED).  pools are 16-byte aligned DEVICE memory of pool_pages *
+ * tg_mx_page_bytes bytes. */
+enum { TG_MX_FP4 = 4, TG_MX_FP8 = 8 };
+typedef struct {
+  int32_t k_format;
+  int32_t v_format;
+} tg_mx_format;
+
+/* Bytes of one page of a group; 0 for shapes or formats that are not supported
+ * (tg_last_error says why). */
+size_t tg_mx_page_bytes(const tg_geometry* geom, const tg_mx_format* format);
+
+/* 13a. tg_append with the token quantised into the pool (kv_pool: the quantised
+ * pool).  k_tok and v_tok are rows of dtype; everything else is tg_append's. */
+int32_t tg_append_mx(const tg_append_args* args, const tg_mx_format* format, void* hip_stream);
+
+/* 13b. tg_compress with the kept rows quantised into the pool: the same plan, the
+ * same selection and kept[], k_new and v_new rows of dtype. */
+int32_t tg_compress_mx(const tg_compress_args* args, const tg_mx_format* format, void* hip_stream);
+
+/* 13c. tg_unpack_mx (device): entries [begin, len) of one layer's heads read back
+ * as rows of dtype into a cache of the layout in the file header, where tg_prefill
+ * and tg_prefill_mod take a chunk's history from.
+ * DEVICE pointers: mx_pool; pt_pages, pt_offsets, group_of, slot_of as tg_append's;
+ * begin [B][L][H] int32 or NULL (0; a negative one counts as 0); len [B][L][H]
+ * int32, at most the table's capacity (clamped to it); kv_pool [pages][2][H_p][16][d]
+ * dtype, written at these entries only; dst_pages int32, or NULL: the page of
+ * kv_pool that takes the page at the same index of pt_pages (NULL: the same id).
+ * With dst_pages counting a layer's own pages from 0, one layer's history is all
+ * that kv_pool has to hold.
+ * Supported: dtype TG_F32 or TG_BF16 (the values are exact in both).  No workspace. */
+typedef struct {
+  tg_geometry geom;
+  int32_t batch;
+  int32_t layer;
+  int32_t dtype;
+  tg_mx_format format;
+  const void* mx_pool;
+  const int32_t* pt_pages;
+  const int64_t* pt_offsets;
+  const int32_t* group_of;
+  const int32_t* slot_of;
+  const int32_t* begin;
+  const int32_t* len;
+  void* kv_pool;
+  const int32_t* dst_pages;
+} tg_unpack_mx_args;
+
+int32_t tg_unpack_mx(const tg_unpack_mx_args* args, void* hip_stream);
+
+/* 13d. Bins that a plan for these lengths should have (host): as many workgroups
+ * as the kernel runs at once on `device`, fewer where the layer's pages are too few
+ * to share.  kv_len [B][L][H] (host), with batch and layer; NULL: the most.
+ * n_bins out.  Errors: TG_ERR_INVALID_ARG, TG_ERR_UNSUPPORTED, TG_ERR_HIP. */
+int32_t tg_decode_mx_bins(const tg_geometry* geom, int32_t dtype, const tg_mx_format* format, int32_t device,
+                          int32_t batch, int32_t layer, const int32_t* kv_len, int32_t* n_bins);
+
+/* 13e. tg_decode over the quantised pool (args->kv_pool), for the values that it
+ * stands for: q, out and append rows are of dtype, plans, workspace, lse, live_len,
+ * timestamps (a bin is a workgroup) and errors are tg_decode's.  softcap 0, or a
+ * cap as tg_decode_capped's.  sm_scale must be finite and >= 0.
+ *   append_k, append_v: the token is quantised into its entry first and attended to
+ *     as stored: one call gives what tg_append_mx and tg_decode_mx give, bit for bit.
+ *   merge_counters: any dtype and head_dim; the results are the same without, bit
+ *     for bit.
+ * Scores that overflow to -inf have no weight; a head with no other scores gives
+ * zeros and an lse of -FLT_MAX.
+ * Supported: dtype TG_F32 or TG_BF16, gqa 1..16. */
+int32_t tg_decode_mx(const tg_decode_args* args, const tg_mx_format* format, float softcap, void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -21,9 +21,15 @@
 //     one unit): 16-byte loads of the K and V rows named by kept[] from the
 //     chunk, 16-byte stores to page pt_pages[pt_base + pos / P], row pos % P,
 //     pos = cursor + rank.  These rows are the HBM traffic.
+//
+// tg_compress_mx is the same selection with the kept rows quantised on their way
+// into the pages of a quantised cache (Quantised below).
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "tg_internal.h"
+#include "tg_mx.h"
 
 namespace {
 
@@ -52,6 +58,14 @@ struct CopyParams {
   int32_t H, C, Hp, P;
   int32_t p_shift;                   // log2(P) when P is a power of two, else -1
   int32_t row_u4;                    // 16-byte vectors per K or V row: 8, 16 or 32
+  int32_t kb, vb;                    // tg_compress_mx: bits of the pool's K and V
+};
+
+// What the copy does with a row: stores it as it is, or quantises rows of T.
+struct Raw {};
+template <typename T>
+struct Quantised {
+  using type = T;
 };
 
 // Order-preserving key of an fp32 score: a > b as numbers iff key(a) > key(b);
@@ -238,7 +252,7 @@ __global__ __launch_bounds__(kSelThreads) void tg_compress_select_kernel(SelectP
 // caches: at 8192 (290 MB) repeated passes took 68 instead of 76 us, because
 // the rows read last time stayed in the caches, but a first pass, what a chunk
 // is in use, 103 instead of 88: plain stores there.
-template <int kUnroll, bool kStream, typename TokFn>
+template <typename Row, int kUnroll, bool kStream, typename TokFn>
 __device__ __forceinline__ void copy_rows(const CopyParams& p, const tg_compress_item& it, int r0, int rows,
                                           TokFn tok, int tid = threadIdx.x, int nthreads = kThreads) {
   const int lpr = p.row_u4;
@@ -263,6 +277,30 @@ __device__ __forceinline__ void copy_rows(const CopyParams& p, const tg_compress
       const int pos = it.cursor + r0 + j;
       page[u] = p.pt_pages[it.pt_base + (p.p_shift >= 0 ? pos >> p.p_shift : pos / p.P)];
     }
+    if constexpr (!std::is_same_v<Row, Raw>) {
+      using T = typename Row::type;
+      constexpr int E = tgd::Row16<T>::kElems;
+      const int d = lpr * E;
+      const tgd::MxParts at = tgd::mx_parts(d, p.kb, p.vb);
+      uint8_t* const pool = reinterpret_cast<uint8_t*>(p.pool);
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) {
+        const int j = base + u * rpp + rsel;
+        float x[E];
+        uint32_t ks, vs;
+        tgd::Row16<T>::unpack(kk[u], x);
+        const tgd::u2 kc = tgd::mx_quantise<E>(x, p.kb, &ks);
+        tgd::Row16<T>::unpack(vv[u], x);
+        const tgd::u2 vc = tgd::mx_quantise<E>(x, p.vb, &vs);
+        if (j < rows) {   // the lanes of a row together
+          const int t = (it.cursor + r0 + j) % tgd::kMxPage;
+          uint8_t* slab = pool + ((int64_t)page[u] * p.Hp + it.slot) * tgd::mx_slab_bytes(d, p.kb, p.vb);
+          tgd::mx_store<E>(slab, slab + at.k_scales, t, sub * E, d, p.kb, false, kc, ks);
+          tgd::mx_store<E>(slab + at.v_codes, slab + at.v_scales, t, sub * E, d, p.vb, true, vc, vs);
+        }
+      }
+      continue;
+    }
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
       const int j = base + u * rpp + rsel;
@@ -282,12 +320,13 @@ __device__ __forceinline__ void copy_rows(const CopyParams& p, const tg_compress
   }
 }
 
+template <typename Row>
 __global__ __launch_bounds__(kThreads) void tg_compress_copy_kernel(CopyParams p) {
   const tg_compress_item it = load_item((const TG_CONST tg_compress_item*)p.items + blockIdx.x);
   const int r0 = max(it.rank_begin, 0);
   const int r1 = min(min(it.rank_end, min(it.count, p.C)), r0 + TG_COMPRESS_MAX_ROWS);
   const int32_t* src_tok = p.kept + ((int64_t)it.b * p.H + it.kv_head) * p.C + r0;
-  copy_rows<kUnroll, false>(p, it, r0, r1 - r0, [&](int j) { return src_tok[j]; });
+  copy_rows<Row, kUnroll, false>(p, it, r0, r1 - r0, [&](int j) { return src_tok[j]; });
 }
 
 // Short chunks in one launch, one single-wave workgroup per work item and no
@@ -300,7 +339,7 @@ __global__ __launch_bounds__(kThreads) void tg_compress_copy_kernel(CopyParams p
 // first item also writes kept[].  KPL = keys per lane.  Single-wave
 // workgroups spread the items over every CU (measured at chunk 512: 7.9 us,
 // against 8.1, 9.3 and 12.1 us with 4, 8 and 16 items per workgroup).
-template <int KPL>
+template <typename Row, int KPL>
 __global__ __launch_bounds__(64) void tg_compress_wave_kernel(SelectParams sp, CopyParams p, int32_t n_items) {
   constexpr int kSpill = kFusedMaxChunk;        // per-lane dummy entries for branch-free stores
   __shared__ __align__(16) uint32_t hist[kBins];
@@ -390,17 +429,44 @@ __global__ __launch_bounds__(64) void tg_compress_wave_kernel(SelectParams sp, C
   }
   const int r0 = max(it.rank_begin, 0);
   const int r1 = min(min(it.rank_end, min(count, min(it.count, p.C))), r0 + TG_COMPRESS_MAX_ROWS);
-  copy_rows<8, true>(p, it, r0, r1 - r0, [&](int j) { return kl[r0 + j]; }, lane, 64);
+  copy_rows<Row, 8, true>(p, it, r0, r1 - r0, [&](int j) { return kl[r0 + j]; }, lane, 64);
   if (it.rank_begin == 0) {
     int32_t* out = sp.kept + unit * p.C;
     for (int r = lane; r < count; r += 64) out[r] = kl[r];
   }
 }
 
-}  // namespace
+// One wave per item, or the two launches of longer chunks.
+template <typename Row>
+int32_t launch(const tg_compress_args* a, const SelectParams& s, const CopyParams& c, hipStream_t stream) {
+  if (a->chunk_len <= kFusedMaxChunk) {
+    const int kpl = (a->chunk_len + 63) / 64;
+    const dim3 grid((unsigned)a->num_items), block(64);
+    if (kpl <= 1) hipLaunchKernelGGL((tg_compress_wave_kernel<Row, 1>), grid, block, 0, stream, s, c, a->num_items);
+    else if (kpl <= 2) hipLaunchKernelGGL((tg_compress_wave_kernel<Row, 2>), grid, block, 0, stream, s, c, a->num_items);
+    else if (kpl <= 4) hipLaunchKernelGGL((tg_compress_wave_kernel<Row, 4>), grid, block, 0, stream, s, c, a->num_items);
+    else if (kpl <= 8) hipLaunchKernelGGL((tg_compress_wave_kernel<Row, 8>), grid, block, 0, stream, s, c, a->num_items);
+    else hipLaunchKernelGGL((tg_compress_wave_kernel<Row, 16>), grid, block, 0, stream, s, c, a->num_items);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return tg::fail(TG_ERR_HIP, "compress launch failed: %s", hipGetErrorString(e));
+    return TG_OK;
+  }
+  // 4 to 16 keys per thread: 512 threads up to 4096 entries, 1024 above
+  const dim3 units(a->batch * a->geom.num_kv_heads);
+  if (a->chunk_len <= 2048) hipLaunchKernelGGL((tg_compress_select_kernel<512, 4>), units, dim3(512), 0, stream, s);
+  else if (a->chunk_len <= 4096) hipLaunchKernelGGL((tg_compress_select_kernel<512, 8>), units, dim3(512), 0, stream, s);
+  else if (a->chunk_len <= 8192) hipLaunchKernelGGL((tg_compress_select_kernel<1024, 8>), units, dim3(1024), 0, stream, s);
+  else hipLaunchKernelGGL((tg_compress_select_kernel<1024, 16>), units, dim3(1024), 0, stream, s);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return tg::fail(TG_ERR_HIP, "compress select launch failed: %s", hipGetErrorString(e));
+  hipLaunchKernelGGL(tg_compress_copy_kernel<Row>, dim3(a->num_items), dim3(kThreads), 0, stream, c);
+  e = hipGetLastError();
+  if (e != hipSuccess) return tg::fail(TG_ERR_HIP, "compress copy launch failed: %s", hipGetErrorString(e));
+  return TG_OK;
+}
 
-extern "C" int32_t tg_compress(const tg_compress_args* a, void* hip_stream) {
-  if (!a) return tg::fail(TG_ERR_INVALID_ARG, "args is NULL");
+// format NULL: the rows as they are.
+int32_t compress_impl(const tg_compress_args* a, const tg_mx_format* format, void* hip_stream) {
   const tg_geometry& g = a->geom;
   if (int32_t rc = tg::check_geometry(&g)) return rc;
   if (a->dtype != TG_F32 && a->dtype != TG_BF16) return tg::fail(TG_ERR_UNSUPPORTED, "dtype must be f32 or bf16");
@@ -431,34 +497,28 @@ extern "C" int32_t tg_compress(const tg_compress_args* a, void* hip_stream) {
   c.P = g.page_size;
   c.p_shift = (g.page_size & (g.page_size - 1)) == 0 ? __builtin_ctz((unsigned)g.page_size) : -1;
   c.row_u4 = g.head_dim * (a->dtype == TG_F32 ? 4 : 2) / 16;
+  c.kb = c.vb = 0;
   s.scores = reinterpret_cast<const uint32_t*>(a->scores);
   s.chunk_tokens = a->chunk_tokens;
   s.keep_count = a->keep_count;
   s.kept = a->kept;
   s.H = g.num_kv_heads;
   s.C = a->chunk_len;
-  if (a->chunk_len <= kFusedMaxChunk) {
-    const int kpl = (a->chunk_len + 63) / 64;
-    const dim3 grid((unsigned)a->num_items), block(64);
-    if (kpl <= 1) hipLaunchKernelGGL(tg_compress_wave_kernel<1>, grid, block, 0, stream, s, c, a->num_items);
-    else if (kpl <= 2) hipLaunchKernelGGL(tg_compress_wave_kernel<2>, grid, block, 0, stream, s, c, a->num_items);
-    else if (kpl <= 4) hipLaunchKernelGGL(tg_compress_wave_kernel<4>, grid, block, 0, stream, s, c, a->num_items);
-    else if (kpl <= 8) hipLaunchKernelGGL(tg_compress_wave_kernel<8>, grid, block, 0, stream, s, c, a->num_items);
-    else hipLaunchKernelGGL(tg_compress_wave_kernel<16>, grid, block, 0, stream, s, c, a->num_items);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return tg::fail(TG_ERR_HIP, "compress launch failed: %s", hipGetErrorString(e));
-    return TG_OK;
-  }
-  // 4 to 16 keys per thread: 512 threads up to 4096 entries, 1024 above
-  const dim3 units(a->batch * g.num_kv_heads);
-  if (a->chunk_len <= 2048) hipLaunchKernelGGL((tg_compress_select_kernel<512, 4>), units, dim3(512), 0, stream, s);
-  else if (a->chunk_len <= 4096) hipLaunchKernelGGL((tg_compress_select_kernel<512, 8>), units, dim3(512), 0, stream, s);
-  else if (a->chunk_len <= 8192) hipLaunchKernelGGL((tg_compress_select_kernel<1024, 8>), units, dim3(1024), 0, stream, s);
-  else hipLaunchKernelGGL((tg_compress_select_kernel<1024, 16>), units, dim3(1024), 0, stream, s);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return tg::fail(TG_ERR_HIP, "compress select launch failed: %s", hipGetErrorString(e));
-  hipLaunchKernelGGL(tg_compress_copy_kernel, dim3(a->num_items), dim3(kThreads), 0, stream, c);
-  e = hipGetLastError();
-  if (e != hipSuccess) return tg::fail(TG_ERR_HIP, "compress copy launch failed: %s", hipGetErrorString(e));
-  return TG_OK;
+  if (!format) return launch<Raw>(a, s, c, stream);
+  c.kb = tg::mx_bits(format->k_format);
+  c.vb = tg::mx_bits(format->v_format);
+  return a->dtype == TG_F32 ? launch<Quantised<float>>(a, s, c, stream) : launch<Quantised<uint16_t>>(a, s, c, stream);
+}
+
+}  // namespace
+
+extern "C" int32_t tg_compress(const tg_compress_args* a, void* hip_stream) {
+  if (!a) return tg::fail(TG_ERR_INVALID_ARG, "args is NULL");
+  return compress_impl(a, nullptr, hip_stream);
+}
+
+extern "C" int32_t tg_compress_mx(const tg_compress_args* a, const tg_mx_format* format, void* hip_stream) {
+  if (!a) return tg::fail(TG_ERR_INVALID_ARG, "args is NULL");
+  if (int32_t rc = tg::check_mx(&a->geom, format)) return rc;
+  return compress_impl(a, format, hip_stream);
 }

@@ -147,21 +147,6 @@ struct DecodeParams {
   int32_t* append_full;      // set when a unit cannot take its token, or NULL
 };
 
-// An open-ended item (tok_end = -capacity) runs to the head's live length n,
-// kept within [tok_begin + 1, capacity]; without live lengths, to capacity.
-// With the in-launch append, an open item with tok_begin <= n < capacity
-// takes the new token as entry n and runs to n + 1 (*arow = n); otherwise
-// *arow = -1, and -2 for an open item that cannot take the token.
-__device__ __forceinline__ int resolve_open(int tok_begin, int tok_end, int n, bool append, int* arow) {
-  const int cap = -tok_end;
-  if (append && n >= tok_begin && n < cap) {
-    *arow = n;
-    return n + 1;
-  }
-  *arow = append ? -2 : -1;
-  return min(max(n, tok_begin + 1), cap);
-}
-
 __device__ __forceinline__ int resolve_end(int tok_begin, int tok_end, int b, int h, const DecodeParams& p,
                                            int* arow) {
   *arow = -1;
@@ -1508,16 +1493,68 @@ int bins_per_wg(int dtype, int d, int gqa, int n_bins) {
   return wave_per_bin(dtype, d, gqa, n_bins) ? waves_per_wg(n_bins) : 1;
 }
 
+}  // namespace
+
+namespace tg {
+
 int32_t check_decode_shape(const tg_geometry* g, int dtype) {
-  if (int32_t rc = tg::check_geometry(g)) return rc;
-  if (dtype != TG_F32 && dtype != TG_BF16) return tg::fail(TG_ERR_INVALID_ARG, "unknown dtype %d", dtype);
-  if (g->page_size != kPage) return tg::fail(TG_ERR_UNSUPPORTED, "decode supports page_size 16 only (got %d)", g->page_size);
+  if (int32_t rc = check_geometry(g)) return rc;
+  if (dtype != TG_F32 && dtype != TG_BF16) return fail(TG_ERR_INVALID_ARG, "unknown dtype %d", dtype);
+  if (g->page_size != kPage) return fail(TG_ERR_UNSUPPORTED, "decode supports page_size 16 only (got %d)", g->page_size);
   if (g->head_dim != 64 && g->head_dim != 128)
-    return tg::fail(TG_ERR_UNSUPPORTED, "decode supports head_dim 64 or 128 (got %d)", g->head_dim);
+    return fail(TG_ERR_UNSUPPORTED, "decode supports head_dim 64 or 128 (got %d)", g->head_dim);
   const int gqa = g->num_q_heads / g->num_kv_heads;
-  if (gqa < 1 || gqa > kMaxGqa) return tg::fail(TG_ERR_UNSUPPORTED, "decode supports 1..16 query heads per KV head");
+  if (gqa < 1 || gqa > kMaxGqa) return fail(TG_ERR_UNSUPPORTED, "decode supports 1..16 query heads per KV head");
   return TG_OK;
 }
+
+int32_t check_decode_args(const tg_decode_args* a, const void* ws_ptr, size_t ws_bytes) {
+  if (!a) return fail(TG_ERR_INVALID_ARG, "args is NULL");
+  if (int32_t rc = check_decode_shape(&a->geom, a->dtype)) return rc;
+  const tg_geometry& g = a->geom;
+  if (a->batch < 1 || a->n_bins < 1 || a->num_items < 0 || a->num_partials < 0)
+    return fail(TG_ERR_INVALID_ARG, "batch, n_bins must be >= 1; counts >= 0");
+  if (!a->q || !a->kv_pool || !a->pt_pages || !a->items || !a->bin_offsets || !a->out)
+    return fail(TG_ERR_INVALID_ARG, "NULL device pointer");
+  if (a->num_partials > 0 && (!a->unit_splits || !a->unit_partial_base))
+    return fail(TG_ERR_INVALID_ARG, "split plan needs unit_splits and unit_partial_base");
+  const size_t need = tg_decode_workspace_bytes(&g, a->batch, a->num_partials);
+  if (a->num_partials > 0 && (!ws_ptr || ws_bytes < need))
+    return fail(TG_ERR_BUFFER_TOO_SMALL, "workspace holds %zu bytes, need %zu", ws_bytes, need);
+  if (!aligned16({a->q, a->kv_pool, a->out, a->append_k, a->append_v, a->num_partials > 0 ? ws_ptr : nullptr}))
+    return fail(TG_ERR_INVALID_ARG, "device buffers must be 16-byte aligned");
+  if (a->live_len && (a->layer < 0 || a->layer >= g.num_layers))
+    return fail(TG_ERR_INVALID_ARG, "layer %d out of range", a->layer);
+  if ((a->append_k == nullptr) != (a->append_v == nullptr))
+    return fail(TG_ERR_INVALID_ARG, "append_k and append_v go together");
+  if (a->append_k && !a->live_len) return fail(TG_ERR_INVALID_ARG, "the in-launch append needs live_len");
+  return TG_OK;
+}
+
+bool decode_merges_in_one_chain(const tg_decode_args* a) {
+  return merge_lanes(a->num_partials, (int64_t)a->batch * a->geom.num_kv_heads) == 1;
+}
+
+int32_t launch_decode_merge(const tg_decode_args* a, const float* part_o, const float* part_lse, void* hip_stream) {
+  const tg_geometry& g = a->geom;
+  const int gqa = g.num_q_heads / g.num_kv_heads;
+  const int lanes = merge_lanes(a->num_partials, (int64_t)a->batch * g.num_kv_heads);
+  MergeFn mf = pick_merge(a->dtype, g.head_dim, lanes);
+  // one chain: four outputs per thread; several: a workgroup per (unit, head), D/4 threads per chain
+  const int block = lanes == 1 ? kBlock : g.head_dim / 4 * lanes;
+  const int grid_y = lanes == 1 ? (gqa * g.head_dim / 4 + kBlock - 1) / kBlock : gqa;
+  hipLaunchKernelGGL(mf, dim3(a->batch * g.num_kv_heads, grid_y), dim3(block), 0, static_cast<hipStream_t>(hip_stream),
+                     a->unit_splits, a->unit_partial_base, part_o, part_lse, a->out, a->lse, g.num_kv_heads, gqa);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return fail(TG_ERR_HIP, "merge launch failed: %s", hipGetErrorString(e));
+  return TG_OK;
+}
+
+}  // namespace tg
+
+namespace {
+
+using tg::check_decode_shape;
 
 size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 
@@ -1558,20 +1595,8 @@ int32_t scratch_address(void** out) {
 // tg_decode with the partials' memory passed in: ws (ws_bytes bytes) stands for
 // the caller's workspace; softcap > 0 caps the scores.
 int32_t decode_impl(const tg_decode_args* a, void* ws_ptr, size_t ws_bytes, float softcap, void* hip_stream) {
-  if (!a) return tg::fail(TG_ERR_INVALID_ARG, "args is NULL");
-  if (int32_t rc = check_decode_shape(&a->geom, a->dtype)) return rc;
+  if (int32_t rc = tg::check_decode_args(a, ws_ptr, ws_bytes)) return rc;
   const tg_geometry& g = a->geom;
-  if (a->batch < 1 || a->n_bins < 1 || a->num_items < 0 || a->num_partials < 0)
-    return tg::fail(TG_ERR_INVALID_ARG, "batch, n_bins must be >= 1; counts >= 0");
-  if (!a->q || !a->kv_pool || !a->pt_pages || !a->items || !a->bin_offsets || !a->out)
-    return tg::fail(TG_ERR_INVALID_ARG, "NULL device pointer");
-  if (a->num_partials > 0 && (!a->unit_splits || !a->unit_partial_base))
-    return tg::fail(TG_ERR_INVALID_ARG, "split plan needs unit_splits and unit_partial_base");
-  const size_t need = tg_decode_workspace_bytes(&g, a->batch, a->num_partials);
-  if (a->num_partials > 0 && (!ws_ptr || ws_bytes < need))
-    return tg::fail(TG_ERR_BUFFER_TOO_SMALL, "workspace holds %zu bytes, need %zu", ws_bytes, need);
-  if (!tg::aligned16({a->q, a->kv_pool, a->out, a->append_k, a->append_v, a->num_partials > 0 ? ws_ptr : nullptr}))
-    return tg::fail(TG_ERR_INVALID_ARG, "device buffers must be 16-byte aligned");
   const int gqa = g.num_q_heads / g.num_kv_heads;
   const int esz = a->dtype == TG_F32 ? 4 : 2;
   const size_t o_bytes = align256((size_t)a->num_partials * gqa * g.head_dim * 4);
@@ -1595,13 +1620,8 @@ int32_t decode_impl(const tg_decode_args* a, void* ws_ptr, size_t ws_bytes, floa
   p.n_bins = a->n_bins;
   p.gqa = gqa;
   p.timestamps = a->timestamps;
-  if (a->live_len && (a->layer < 0 || a->layer >= g.num_layers))
-    return tg::fail(TG_ERR_INVALID_ARG, "layer %d out of range", a->layer);
   p.live = a->live_len ? a->live_len + (int64_t)a->layer * g.num_kv_heads : nullptr;
   p.live_stride = g.num_layers * g.num_kv_heads;
-  if ((a->append_k == nullptr) != (a->append_v == nullptr))
-    return tg::fail(TG_ERR_INVALID_ARG, "append_k and append_v go together");
-  if (a->append_k && !a->live_len) return tg::fail(TG_ERR_INVALID_ARG, "the in-launch append needs live_len");
   p.append_k = static_cast<const u4*>(a->append_k);
   p.append_v = static_cast<const u4*>(a->append_v);
   p.pool_w = static_cast<u4*>(a->kv_pool);
@@ -1613,9 +1633,9 @@ int32_t decode_impl(const tg_decode_args* a, void* ws_ptr, size_t ws_bytes, floa
   // all: 24 requests of 2000 to 16000 tokens (6.2 pieces per unit) 92 us there,
   // 65 in one chain there, 53 with the second launch; 16 requests (8.9) 76, 52
   // and 36; one of 40000 tokens (129) 211, 158 and 17.
-  const int lanes = merge_lanes(a->num_partials, (int64_t)a->batch * g.num_kv_heads);
+  const bool one_chain = tg::decode_merges_in_one_chain(a);
   const bool fused_merge =
-      a->merge_counters && a->num_partials > 0 && lanes == 1 && a->dtype == TG_BF16 && g.head_dim == 128;
+      a->merge_counters && a->num_partials > 0 && one_chain && a->dtype == TG_BF16 && g.head_dim == 128;
   p.merge_counters = fused_merge ? a->merge_counters : nullptr;
   p.scale = a->sm_scale != 0.f ? a->sm_scale : 1.0f / std::sqrt((float)g.head_dim);
   p.scale_log2 = p.scale * kLog2e;
@@ -1632,16 +1652,7 @@ int32_t decode_impl(const tg_decode_args* a, void* ws_ptr, size_t ws_bytes, floa
                      a->bin_offsets, p.pool);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return tg::fail(TG_ERR_HIP, "decode launch failed: %s", hipGetErrorString(e));
-  if (a->num_partials > 0 && !fused_merge) {
-    MergeFn mf = pick_merge(a->dtype, g.head_dim, lanes);
-    // one chain: four outputs per thread; several: a workgroup per (unit, head), D/4 threads per chain
-    const int block = lanes == 1 ? kBlock : g.head_dim / 4 * lanes;
-    const int grid_y = lanes == 1 ? (gqa * g.head_dim / 4 + kBlock - 1) / kBlock : gqa;
-    hipLaunchKernelGGL(mf, dim3(a->batch * g.num_kv_heads, grid_y), dim3(block), 0, st, a->unit_splits,
-                       a->unit_partial_base, p.part_o, p.part_lse, a->out, a->lse, g.num_kv_heads, gqa);
-    e = hipGetLastError();
-    if (e != hipSuccess) return tg::fail(TG_ERR_HIP, "merge launch failed: %s", hipGetErrorString(e));
-  }
+  if (a->num_partials > 0 && !fused_merge) return tg::launch_decode_merge(a, p.part_o, p.part_lse, hip_stream);
   return TG_OK;
 }
 

@@ -112,4 +112,19 @@ __device__ __forceinline__ TablePages table_of(Offsets pt_offsets, int64_t layer
   return {base, has ? end - base : 0};
 }
 
+// An open-ended item (tok_end = -capacity) runs to the head's live length n,
+// kept within [tok_begin + 1, capacity]; without live lengths, to capacity.
+// With the in-launch append, an open item with tok_begin <= n < capacity
+// takes the new token as entry n and runs to n + 1 (*arow = n); otherwise
+// *arow = -1, and -2 for an open item that cannot take the token.
+__device__ __forceinline__ int resolve_open(int tok_begin, int tok_end, int n, bool append, int* arow) {
+  const int cap = -tok_end;
+  if (append && n >= tok_begin && n < cap) {
+    *arow = n;
+    return n + 1;
+  }
+  *arow = append ? -2 : -1;
+  return min(max(n, tok_begin + 1), cap);
+}
+
 }  // namespace tgd

@@ -21,6 +21,15 @@ int32_t check_geometry(const tg_geometry* g);
 // (a negative one would turn the running maximum into a minimum).
 int32_t check_softcap(float softcap, float sm_scale);
 
+// What the decode calls share: the shapes they take, their arguments (ws_ptr of
+// ws_bytes bytes standing for the workspace), and the merge of the split units'
+// partials as a launch of its own: in one chain per unit where the plan has few
+// pieces a unit, which the kernels may then merge themselves.
+int32_t check_decode_shape(const tg_geometry* g, int dtype);
+int32_t check_decode_args(const tg_decode_args* a, const void* ws_ptr, size_t ws_bytes);
+bool decode_merges_in_one_chain(const tg_decode_args* a);
+int32_t launch_decode_merge(const tg_decode_args* a, const float* part_o, const float* part_lse, void* hip_stream);
+
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // True when every pointer given is 16-byte aligned (NULL counts as aligned):

@@ -38,6 +38,8 @@ TG_COMPRESS_MAX_CHUNK, TG_COMPRESS_MAX_ROWS, TG_COMPRESS_ONE_LAUNCH_MAX_CHUNK = 
 TG_ROPE_PLAIN, TG_ROPE_LINEAR, TG_ROPE_NTK, TG_ROPE_BANDS, TG_ROPE_YARN = 0, 1, 2, 3, 4
 TG_ROPE_HALF, TG_ROPE_INTERLEAVED = 0, 1
 
+TG_MX_FP4, TG_MX_FP8 = 4, 8
+
 
 class TangramError(RuntimeError):
     def __init__(self, code, where, detail):
@@ -126,6 +128,17 @@ class tg_score_mod(C.Structure):
     _fields_ = [("softcap", C.c_float), ("chunk_tokens", C.c_void_p), ("key_begin", C.c_void_p), ("key_end", C.c_void_p)]
 
 
+class tg_mx_format(C.Structure):
+    _fields_ = [("k_format", C.c_int32), ("v_format", C.c_int32)]
+
+
+class tg_unpack_mx_args(C.Structure):
+    _fields_ = [("geom", tg_geometry), ("batch", C.c_int32), ("layer", C.c_int32), ("dtype", C.c_int32),
+                ("format", tg_mx_format), ("mx_pool", C.c_void_p), ("pt_pages", C.c_void_p), ("pt_offsets", C.c_void_p),
+                ("group_of", C.c_void_p), ("slot_of", C.c_void_p), ("begin", C.c_void_p), ("len", C.c_void_p),
+                ("kv_pool", C.c_void_p), ("dst_pages", C.c_void_p)]
+
+
 class tg_footprint(C.Structure):
     _fields_ = [("full_slots", C.c_int64), ("retained_slots", C.c_int64), ("monolithic_slots", C.c_int64),
                 ("ragged_slots", C.c_int64), ("ragged_pages", C.c_int64), ("page_tables", C.c_int64)]
@@ -185,6 +198,12 @@ _SIGS = {
     "tg_slot_map": (_i32, [C.POINTER(tg_slot_map_args), _P]),
     "tg_prefill_mod": (_i32, [C.POINTER(tg_prefill_args), C.POINTER(tg_score_mod), _P]),
     "tg_decode_capped": (_i32, [C.POINTER(tg_decode_args), _f32, _P]),
+    "tg_mx_page_bytes": (_sz, [_G, C.POINTER(tg_mx_format)]),
+    "tg_append_mx": (_i32, [C.POINTER(tg_append_args), C.POINTER(tg_mx_format), _P]),
+    "tg_compress_mx": (_i32, [C.POINTER(tg_compress_args), C.POINTER(tg_mx_format), _P]),
+    "tg_unpack_mx": (_i32, [C.POINTER(tg_unpack_mx_args), _P]),
+    "tg_decode_mx_bins": (_i32, [_G, _i32, C.POINTER(tg_mx_format), _i32, _i32, _i32, _P, _P]),
+    "tg_decode_mx": (_i32, [C.POINTER(tg_decode_args), C.POINTER(tg_mx_format), _f32, _P]),
     "tg_read_probe": (_i32, [_G, _i32, _P, _P, _P, _i64, _i32, _P, _P]),
 }
 for _name, (_res, _args) in _SIGS.items():
@@ -684,3 +703,56 @@ def tg_prefill_mod(args: tg_prefill_args, mod: tg_score_mod, stream=None):
 
 def tg_decode_capped(args: tg_decode_args, softcap, stream=None):
     _check(_lib.tg_decode_capped(C.byref(args), float(softcap), _stream(stream)), "tg_decode_capped")
+
+
+def make_mx_format(k_format=TG_MX_FP4, v_format=TG_MX_FP4) -> tg_mx_format:
+    return tg_mx_format(int(k_format), int(v_format))
+
+
+def tg_mx_page_bytes(geom, fmt: tg_mx_format) -> int:
+    """Bytes of one page of a group in a quantised pool."""
+    n = int(_lib.tg_mx_page_bytes(C.byref(_geom(geom)), C.byref(fmt)))
+    if n == 0:
+        raise TangramError(TG_ERR_INVALID_ARG, "tg_mx_page_bytes", tg_last_error())
+    return n
+
+
+def tg_append_mx(args: tg_append_args, fmt: tg_mx_format, stream=None):
+    """args as make_append_args packs them, kv_pool the quantised pool (uint8)."""
+    _check(_lib.tg_append_mx(C.byref(args), C.byref(fmt), _stream(stream)), "tg_append_mx")
+
+
+def tg_compress_mx(args: tg_compress_args, fmt: tg_mx_format, stream=None):
+    """args as make_compress_args packs them, kv_pool the quantised pool (uint8)."""
+    _check(_lib.tg_compress_mx(C.byref(args), C.byref(fmt), _stream(stream)), "tg_compress_mx")
+
+
+def make_unpack_mx_args(geom, batch, layer, dtype, fmt: tg_mx_format, mx_pool, pt_pages, pt_offsets, group_of, slot_of,
+                        length, kv_pool, begin=None, dst_pages=None) -> tg_unpack_mx_args:
+    """Packs a tg_unpack_mx_args from device tensors (kept alive by the caller): mx_pool uint8, length and begin int32
+    [B][L][H], kv_pool [pages][2][H_p][16][d] of dtype, dst_pages int32 with an entry for every one of pt_pages."""
+    g, B = _geom(geom), int(batch)
+    LH, tables = g.num_layers * g.num_kv_heads, B * g.num_layers * (g.num_kv_heads // max(1, g.heads_per_group))
+    return tg_unpack_mx_args(g, B, int(layer), int(dtype), fmt, _array("mx_pool", mx_pool, "uint8"),
+                             _array("pt_pages", pt_pages, "int32"), _array("pt_offsets", pt_offsets, "int64", tables + 1),
+                             _array("group_of", group_of, "int32", LH), _array("slot_of", slot_of, "int32", LH),
+                             _array("begin", begin, "int32", B * LH), _array("length", length, "int32", B * LH),
+                             _array("kv_pool", kv_pool, int(dtype)),
+                             _array("dst_pages", dst_pages, "int32", 0 if dst_pages is None else pt_pages.numel()))
+
+
+def tg_unpack_mx(args: tg_unpack_mx_args, stream=None):
+    _check(_lib.tg_unpack_mx(C.byref(args), _stream(stream)), "tg_unpack_mx")
+
+
+def tg_decode_mx_bins(geom, dtype, fmt: tg_mx_format, device=0, batch=0, layer=0, kv_len=None) -> int:
+    """Bins for a plan of these lengths (kv_len int32 [B][L][H], host), or the most that run at once."""
+    n = C.c_int32(0)
+    _check(_lib.tg_decode_mx_bins(C.byref(_geom(geom)), int(dtype), C.byref(fmt), int(device), int(batch), int(layer),
+                                  _ptr(None if kv_len is None else _host(kv_len, np.int32)), C.byref(n)), "tg_decode_mx_bins")
+    return n.value
+
+
+def tg_decode_mx(args: tg_decode_args, fmt: tg_mx_format, softcap=0.0, stream=None):
+    """args as make_decode_args packs them, kv_pool the quantised pool (uint8)."""
+    _check(_lib.tg_decode_mx(C.byref(args), C.byref(fmt), float(softcap), _stream(stream)), "tg_decode_mx")
