@@ -33,7 +33,6 @@ using namespace tgd;
 
 constexpr int kWaves = 4;
 constexpr int kBlock = 64 * kWaves;
-constexpr int KP = 2;          // pages of a step
 constexpr int kMaxGqa = 16;
 constexpr int kPad = 4;        // floats between the heads' accumulators in LDS
 
@@ -48,8 +47,6 @@ struct MxDecodeParams {
   int64_t page_bytes;
   int32_t slab_bytes;
   int32_t num_q_heads, num_kv_heads, n_bins, gqa;
-  const int32_t* unit_splits;
-  const int32_t* unit_partial_base;
   void* out;
   float* lse;
   float* part_o;               // [num_partials][gqa][d]
@@ -57,7 +54,6 @@ struct MxDecodeParams {
   uint64_t* timestamps;
   int32_t* live;               // live lengths of this layer, or NULL
   int32_t live_stride;
-  int32_t* merge_counters;     // of the in-launch merge, or NULL
   const u4* append_k;
   const u4* append_v;
   int32_t* append_full;
@@ -68,6 +64,17 @@ struct MxDecodeParams {
 __device__ __forceinline__ f32x4 mfma(const u4& a, const u4& b, const f32x4& c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0,
                                                  0);
+}
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+// A product over the tokens of one page (2 words of 4 tokens' pairs) or two.
+template <int PAGES>
+__device__ __forceinline__ f32x4 mfma_pv(const uint32_t* a, const uint32_t* b, const f32x4& c) {
+  if constexpr (PAGES == 2)
+    return mfma(u4{a[0], a[1], a[2], a[3]}, u4{b[0], b[1], b[2], b[3]}, c);
+  else
+    return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4, u2{a[0], a[1]}),
+                                                     __builtin_bit_cast(s16x4, u2{b[0], b[1]}), c, 0, 0, 0);
 }
 
 // Codes 2i and 2i + 1 of a lane as a pair of bf16.
@@ -124,33 +131,70 @@ __device__ __forceinline__ void store4<uint16_t>(uint16_t* dst, const f32x4& v) 
                                    uint32_t(f32_to_bf16(v[2])) | (uint32_t(f32_to_bf16(v[3])) << 16)};
 }
 
-__device__ __forceinline__ tg_work_item load_item(const TG_CONST tg_work_item* src) {
-  tg_work_item r;
-  r.pt_base = src->pt_base;
-  r.b = src->b;
-  r.kv_head = src->kv_head;
-  r.slot = src->slot;
-  r.tok_begin = src->tok_begin;
-  r.tok_end = src->tok_end;
-  r.out_idx = src->out_idx;
-  return r;
+// A wave's ring in LDS, by format.
+template <typename T, int D, int KB, int VB>
+struct Shape {
+  static constexpr int kPages = KB + VB == 16 && D == 128 ? 1 : 2;            // pages of a step
+  static constexpr int kSlab = mx_slab_bytes(D, KB, VB);
+  // a slab comes in whole kilobytes of 16 bytes a lane and a rest of 4 or 16 bytes a lane
+  static constexpr int kFull = kSlab / 1024, kRest = kSlab % 1024;
+  static constexpr bool kWideRest = kRest > 256;
+  static constexpr int kStagePage = kFull * 1024 + (kWideRest ? 1024 : 256);
+  static constexpr int kStage = kPages * kStagePage;
+  static constexpr int kDma = kPages * (kFull + 1);                           // loads a step
+  static constexpr int kRing = D == 64 ? (KB + VB == 8 ? 6 : 3) : kStage > 6000 ? 2 : 3;                         // steps in the ring
+  static constexpr int kRow = (D + kPad) * 4;                                 // a head's accumulator in LDS
+  // the ring, which takes the wave's last state in the end; the state that waves 1 to 3 may park on the way
+  static constexpr int state_bytes(int gqa) { return gqa * (kRow + 8); }
+  static constexpr int wave_bytes(int gqa) {
+    return (kRing * kStage > state_bytes(gqa) ? kRing * kStage : (state_bytes(gqa) + 15) / 16 * 16);
+  }
+  static constexpr size_t lds_bytes(int gqa) {
+    return kWaves * wave_bytes(gqa) + (kWaves - 1) * ((state_bytes(gqa) + 15) / 16 * 16);
+  }
+};
+
+// 16 or 4 bytes a lane from base + offset into LDS at lds + 16 (4) * lane, past the
+// caches' keeping: a step reads every byte of the cache once.
+__device__ __forceinline__ void dma16(const void* base, uint32_t offset, uint32_t lds) {
+  asm volatile("global_load_lds_dwordx4 %0, %1 nt sc1" ::"v"(offset), "s"(base), "{m0}"(lds) : "memory");
+}
+__device__ __forceinline__ void dma4(const void* base, uint32_t offset, uint32_t lds) {
+  asm volatile("global_load_lds_dword %0, %1 nt sc1" ::"v"(offset), "s"(base), "{m0}"(lds) : "memory");
+}
+template <int N>
+__device__ __forceinline__ void wait_vmcnt() {
+  static_assert(N >= 0 && N < 64, "vmcnt is 6 bits");
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ uint32_t lds_address(const void* ptr) {
+  return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) void*)ptr));
 }
 
-constexpr size_t lds_floats(int gqa, int d) { return (size_t)kWaves * gqa * (d + kPad + 2) + 4; }
+__device__ __forceinline__ int lane_of(int x, int j) { return __builtin_amdgcn_readlane(x, j); }
+__device__ __forceinline__ int64_t lane_of64(int64_t x, int j) {
+  return (int64_t)(((uint64_t)(uint32_t)lane_of((int32_t)(x >> 32), j) << 32) | (uint32_t)lane_of((int32_t)x, j));
+}
 
 template <typename T, int D, int KB, int VB>
-__global__ void __launch_bounds__(kBlock)
+__global__ void __launch_bounds__(kBlock, 2)
     tg_decode_mx_kernel(MxDecodeParams p, const tg_work_item* __restrict__ items_g, const int32_t* __restrict__ pt_g,
                         const int32_t* __restrict__ bin_offsets_g) {
+  using S = Shape<T, D, KB, VB>;
   constexpr int E = Row16<T>::kElems;
   constexpr int NPART = sizeof(T) == 4 ? 3 : 1;   // bf16 parts of q and P
+  constexpr int KP = S::kPages;
   constexpr int KW = D * KB / 128, VW = D * VB / 128;
   constexpr int NQ = D / 32, NV = D / 16;
+  constexpr int QC = D / 4 / E;                   // 16-byte chunks of q a lane
+  constexpr int LPR = D / E;                      // 16-byte chunks of a row of T
+  constexpr int R = S::kRing;
   constexpr MxParts at = mx_parts(D, KB, VB);
+  // V's operands are made beside the products of q.k, where registers allow it
+  constexpr bool kEarly = NPART == 1;
   constexpr float kSlack = 8.0f;
-  extern __shared__ float lds[];
+  extern __shared__ __align__(16) uint8_t lds[];
 
-  const TG_CONST tg_work_item* const items = (const TG_CONST tg_work_item*)items_g;
   const TG_CONST int32_t* const pt = (const TG_CONST int32_t*)pt_g;
   const TG_CONST int32_t* const bin_offsets = (const TG_CONST int32_t*)bin_offsets_g;
 
@@ -159,339 +203,427 @@ __global__ void __launch_bounds__(kBlock)
   const int col = lane & 15, rb = lane >> 4;
   const int G = p.gqa;
   const int hq = col < G ? col : col % G;
-  float* const sm_acc = lds;                                  // [wave][head][D + kPad]
-  float* const sm_m = lds + kWaves * G * (D + kPad);          // [wave][head]
-  float* const sm_l = sm_m + kWaves * G;
-  int* const sm_flag = reinterpret_cast<int*>(sm_l + kWaves * G);
+  const int park_bytes = (S::state_bytes(G) + 15) / 16 * 16, wave_bytes = S::wave_bytes(G);
+  uint8_t* const ring = lds + wave * wave_bytes;
+  uint8_t* const parks = lds + kWaves * wave_bytes;
+  const uint32_t ring_lds = lds_address(ring);
   const uint64_t t_start = __builtin_amdgcn_s_memrealtime();
   const int it_begin = bin_offsets[blockIdx.x], it_end = bin_offsets[blockIdx.x + 1];
+  if (it_begin >= it_end) {
+    if (p.timestamps && threadIdx.x == 0) p.timestamps[2 * blockIdx.x] = p.timestamps[2 * blockIdx.x + 1] = t_start;
+    return;
+  }
   const float cs = p.cap > 0.f ? kLog2e : p.scale * kLog2e;   // log2 units per unit of (capped) score
 
-  for (int it = it_begin; it < it_end; ++it) {
-    tg_work_item item = load_item(items + it);
-    int arow = -1;
-    if (item.tok_end < 0) {
-      const int n = p.live ? p.live[(int64_t)item.b * p.live_stride + item.kv_head] : -item.tok_end;
-      item.tok_end = __builtin_amdgcn_readfirstlane(
-          resolve_open(item.tok_begin, item.tok_end, n, p.append_k != nullptr, &arow));
-      arow = __builtin_amdgcn_readfirstlane(arow);
+  // the result of a head's dims c4 .. of an item: out, or this piece's partial
+  auto write4 = [&](int b, int h, int out_idx, int g, int e, const f32x4& O, float lse) {
+    if (out_idx < 0) {
+      const int64_t row = (int64_t)b * p.num_q_heads + h * G + g;
+      store4<T>(static_cast<T*>(p.out) + row * D + e, O);
+      if (p.lse && e == 0) p.lse[row] = lse;
+      return;
     }
-    const int ntok = item.tok_end - item.tok_begin;
-    const int np = (ntok + kMxPage - 1) / kMxPage;
-    const TG_CONST int32_t* const ids = pt + item.pt_base + item.tok_begin / kMxPage;
-    const uint8_t* const slabs = p.pool + (int64_t)item.slot * p.slab_bytes;
-    const int ns = (np - wave * KP + kWaves * KP - 1) / (kWaves * KP);   // this wave's steps; may be 0
+    const int64_t row = (int64_t)out_idx * G + g;
+    float* dst = p.part_o + row * D + e;
+    *reinterpret_cast<f32x4*>(dst) = O;
+    if (e == 0) p.part_lse[row] = lse;
+  };
+  // no score above -inf: zeros, and an lse that loses against any other piece's
+  auto lse_of = [&](float m, float l) { return l == 0.f ? -FLT_MAX : m * (cs * kLn2) + logf(l); };
 
-    // the wave that attends to the new token quantises and stores it first, and
-    // reads it back with its page
-    if (arow >= 0 && (np - 1) / KP % kWaves == wave) {
-      constexpr int LPR = D / E;
-      const int t = arow % kMxPage;
-      uint8_t* slab = p.pool + (int64_t)ids[np - 1] * p.page_bytes + (int64_t)item.slot * p.slab_bytes;
-      const int64_t row = ((int64_t)item.b * p.num_kv_heads + item.kv_head) * LPR + lane % LPR;
-      if (lane < 2 * LPR) {
-        const bool is_v = lane >= LPR;
-        float x[E];
-        uint32_t scale;
-        Row16<T>::unpack(is_v ? p.append_v[row] : p.append_k[row], x);
-        if (is_v) {
-          const u2 c = mx_quantise<E>(x, VB, &scale);
-          mx_store<E>(slab + at.v_codes, slab + at.v_scales, t, lane % LPR * E, D, VB, true, c, scale);
-        } else {
-          const u2 c = mx_quantise<E>(x, KB, &scale);
-          mx_store<E>(slab, slab + at.k_scales, t, lane * E, D, KB, false, c, scale);
-        }
-      }
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // this wave's loads of the page come behind the stores
-    }
-
-    u4 qv[NPART][NQ];
+  // The items of the bin, up to 64 at a time, one a lane.  Their pages laid end to
+  // end are cut into four equal ranges, one a wave: a wave runs its range by itself,
+  // and only an item that a cut goes through takes more than one of them.
+  for (int chunk = it_begin; chunk < it_end; chunk += 64) {
+    const int n_items = min(64, it_end - chunk);
+    int64_t h_first;         // of the item's page ids
+    int h_ntok, h_slot, h_b, h_head, h_out, h_arow = -1, h_end;   // arow: the entry that takes the new token, or < 0
     {
-      const T* q = static_cast<const T*>(p.q) +
-                   ((int64_t)item.b * p.num_q_heads + item.kv_head * G + hq) * D + rb * (D / 4);
+      const tg_work_item im = items_g[chunk + min(lane, n_items - 1)];
+      int end = im.tok_end;
+      if (end < 0) {
+        const int n = p.live ? p.live[(int64_t)im.b * p.live_stride + im.kv_head] : -end;
+        end = resolve_open(im.tok_begin, im.tok_end, n, p.append_k != nullptr, &h_arow);
+      }
+      h_first = im.pt_base + im.tok_begin / kMxPage;
+      h_ntok = end - im.tok_begin;
+      h_slot = im.slot;
+      h_b = im.b;
+      h_head = im.kv_head;
+      h_out = im.out_idx;
+      h_end = lane < n_items ? (h_ntok + kMxPage - 1) / kMxPage : 0;   // pages, then where they end
 #pragma unroll
-      for (int m = 0; m < NQ; ++m) {
+      for (int s = 1; s < 64; s *= 2) {
+        const int x = __shfl_up(h_end, s);
+        h_end += lane >= s ? x : 0;
+      }
+    }
+    const int pages = lane_of(h_end, 63);
+    auto cut = [&](int w) { return (int)((int64_t)pages * w >> 2); };
+    const int f0 = cut(wave), f1 = cut(wave + 1);
+    auto begin_of = [&](int it) { return it > 0 ? lane_of(h_end, it - 1) : 0; };
+    const int it0 = __builtin_ctzll(__ballot(h_end > f0) | (1ull << 63));   // the item of page f0
+    __syncthreads();   // every wave has the lengths; the last chunk's states have been read
+
+    // the loads run ahead of the products, over all items
+    int d_it = it0, d_page = f0 - begin_of(it0), d_left = f1 - f0;   // d_left: pages to request
+    int d_np = lane_of(h_end, it0) - begin_of(it0);
+    int64_t d_first = lane_of64(h_first, it0);
+    const uint8_t* d_slabs = p.pool + (int64_t)lane_of(h_slot, it0) * S::kSlab;
+    struct Ids {
+      int32_t v[KP];
+    } d_id = {};
+    auto page_ids = [&] {
+      const int last = min(d_np, d_page + d_left) - 1;
+#pragma unroll
+      for (int k = 0; k < KP; ++k) d_id.v[k] = pt[d_first + min(d_page + k, last)];
+    };
+    auto issue = [&](int slot) {   // one step, and on to the next
+#pragma unroll
+      for (int k = 0; k < KP; ++k) {
+        const uint8_t* slab = d_slabs + (int64_t)d_id.v[k] * p.page_bytes;
+        const uint32_t dst = ring_lds + slot * S::kStage + k * S::kStagePage;
+#pragma unroll
+        for (int j = 0; j < S::kFull; ++j) dma16(slab + j * 1024, lane * 16, dst + j * 1024);
+        if constexpr (S::kWideRest) dma16(slab + S::kFull * 1024, min(lane * 16, S::kRest - 16), dst + S::kFull * 1024);
+        else dma4(slab + S::kFull * 1024, min(lane * 4, S::kRest - 4), dst + S::kFull * 1024);
+      }
+      const int took = min(KP, min(d_np - d_page, d_left));
+      d_page += took;
+      d_left -= took;
+      if (d_left <= 0) return;
+      if (d_page >= d_np) {
+        ++d_it;
+        d_page = 0;
+        d_np = lane_of(h_end, d_it) - lane_of(h_end, d_it - 1);
+        d_first = lane_of64(h_first, d_it);
+        d_slabs = p.pool + (int64_t)lane_of(h_slot, d_it) * S::kSlab;
+      }
+      page_ids();
+    };
+    // an item's queries, and its new token's rows, as they lie in memory
+    u4 q_next[QC], tok_next = {};
+    auto load_q = [&](int it) {
+      const int b = lane_of(h_b, it), h = lane_of(h_head, it);
+      const u4* q = reinterpret_cast<const u4*>(static_cast<const T*>(p.q) +
+                                                ((int64_t)b * p.num_q_heads + h * G + hq) * D + rb * (D / 4));
+#pragma unroll
+      for (int i = 0; i < QC; ++i) q_next[i] = q[i];
+      if (p.append_k && lane < 2 * LPR) {
+        const int64_t row = ((int64_t)b * p.num_kv_heads + h) * LPR;
+        tok_next = lane < LPR ? p.append_k[row + lane] : p.append_v[row + lane - LPR];
+      }
+    };
+
+    int it = it0, done = 0;
+    float m = -INFINITY, l = 0.f;
+    f32x4 acc[NV];
+    if (f0 < f1) {
+      load_q(it0);
+      page_ids();
+#pragma unroll
+      for (int r = 0; r < R - 1; ++r)
+        if (d_left > 0) issue(r);
+    }
+    for (int at_page = f0; at_page < f1; ++it) {
+      const int first_page = at_page - begin_of(it);   // of the item
+      const int np = lane_of(h_end, it) - begin_of(it);
+      const int stop = min(np, first_page + f1 - at_page);
+      const int ntok = lane_of(h_ntok, it), arow = lane_of(h_arow, it);
+
+      u4 qv[NPART][NQ];
+      const u4 tok = tok_next;
+#pragma unroll
+      for (int c = 0; c < NQ; ++c) {
         if constexpr (NPART == 1) {
-          qv[0][m] = *reinterpret_cast<const u4*>(q + 8 * m);
+          qv[0][c] = q_next[c];
         } else {
+          float x[8];
+          Row16<float>::unpack(q_next[2 * c], x);
+          Row16<float>::unpack(q_next[2 * c + 1], x + 4);
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             uint32_t a[3], b[3];
-            split3(q[8 * m + 2 * i], a);
-            split3(q[8 * m + 2 * i + 1], b);
+            split3(x[2 * i], a);
+            split3(x[2 * i + 1], b);
 #pragma unroll
-            for (int s = 0; s < 3; ++s) qv[s][m][i] = join16(a[s], b[s]);
+            for (int s = 0; s < 3; ++s) qv[s][c][i] = join16(a[s], b[s]);
           }
         }
       }
-    }
+      if (at_page + stop - first_page < f1) load_q(it + 1);   // in use when this item is done
 
-    struct Tile {
-      uint32_t k[KP][KW], v[KP][VW], ks[KP], vs[KP];
-    };
-    auto load = [&](Tile& t, int step) {
+      m = -INFINITY;
+      l = 0.f;
 #pragma unroll
-      for (int k = 0; k < KP; ++k) {
-        const int page = min((step * kWaves + wave) * KP + k, np - 1);
-        const uint8_t* slab = slabs + (int64_t)ids[page] * p.page_bytes;
-        load_codes<KW>(slab, lane, t.k[k]);
-        load_codes<VW>(slab + at.v_codes, lane, t.v[k]);
-        t.ks[k] = slab[at.k_scales + (D == 128 ? rb : rb >> 1) * kMxPage + col];
-        t.vs[k] = *reinterpret_cast<const uint32_t*>(slab + at.v_scales + rb * (D / 8) + col / (512 / D) * 4);
-      }
-    };
+      for (int n = 0; n < NV; ++n) acc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    float m = -INFINITY, l = 0.f;
-    f32x4 acc[NV];
-#pragma unroll
-    for (int n = 0; n < NV; ++n) acc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
-
-    auto compute = [&](Tile& t, int step) {
-      const int left = ntok - (step * kWaves + wave) * KP * kMxPage;   // tokens from the step's first on
-      float sv[4 * KP];
-#pragma unroll
-      for (int k = 0; k < KP; ++k) {
-        f32x4 s = {0.f, 0.f, 0.f, 0.f};
-        const float ks = mx_scale(t.ks[k]);
-#pragma unroll
-        for (int c = 0; c < NQ; ++c) {
-          const u4 a = {pair<KB>(t.k[k], 4 * c, ks), pair<KB>(t.k[k], 4 * c + 1, ks), pair<KB>(t.k[k], 4 * c + 2, ks),
-                        pair<KB>(t.k[k], 4 * c + 3, ks)};
-#pragma unroll
-          for (int part = 0; part < NPART; ++part) s = mfma(a, qv[part][c], s);
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float x = s[i];
-          if (p.cap > 0.f) x = p.cap * tanh_f32(x * p.scale);
-          sv[4 * k + i] = k * kMxPage + 4 * rb + i < left ? x : -INFINITY;
-        }
-      }
-      float mx = sv[0];
-#pragma unroll
-      for (int i = 1; i < 4 * KP; ++i) mx = fmaxf(mx, sv[i]);
-      mx = swap32_max(swap16_max(mx));
-      const bool raise = (mx - m) * cs > kSlack;
-      if (__any(raise)) {
-        const float m_new = raise ? mx : m;
-        const float alpha = fast_exp2((m - m_new) * cs);   // 0 when m was -inf
-        l = raise ? l * alpha : l;
-#pragma unroll
-        for (int n = 0; n < NV; ++n)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) acc[n][r] = raise ? acc[n][r] * alpha : acc[n][r];
-        m = m_new;
-      }
-      const float mref = m > -INFINITY ? m : 0.f;   // every score -inf so far: weights 0
-      u4 pb[NPART];
-#pragma unroll
-      for (int i = 0; i < 4 * KP; ++i) sv[i] = fast_exp2((sv[i] - mref) * cs);
-      l += ((sv[0] + sv[1]) + (sv[2] + sv[3])) + ((sv[4] + sv[5]) + (sv[6] + sv[7]));
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if constexpr (NPART == 1) {
-          // bf16 outputs: P rounded to bf16, half a step of the output's own
-          pb[0][i] = uint32_t(f32_to_bf16(sv[2 * i])) | (uint32_t(f32_to_bf16(sv[2 * i + 1])) << 16);
+      for (int page = first_page; page < stop; page += KP, ++done) {
+        if (d_left > 0) {   // R - 1 steps stay in flight
+          issue((done + R - 1) % R);
+          wait_vmcnt<S::kDma * (R - 1)>();
         } else {
-          uint32_t a[3], b[3];
-          split3(sv[2 * i], a);
-          split3(sv[2 * i + 1], b);
-#pragma unroll
-          for (int s = 0; s < 3; ++s) pb[s][i] = join16(a[s], b[s]);
+          wait_vmcnt<0>();
         }
-      }
-      if (left < KP * kMxPage) {   // rows past the retained length may hold anything: codes 0, scale 1
-#pragma unroll
-        for (int k = 0; k < KP; ++k) {
-          const int keep = min(max(left - k * kMxPage - 4 * rb, 0), 4);   // of the lane's 4 tokens
-          const uint32_t mask = keep == 4 ? ~0u : (1u << (8 * keep)) - 1u;
-          t.vs[k] = (t.vs[k] & mask) | (0x7f7f7f7fu & ~mask);
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            if (r < keep) continue;
-            if constexpr (VW == 2) {
-              t.v[k][r / 2] &= r % 2 ? 0x0000ffffu : 0xffff0000u;
+        uint8_t* const stage = ring + done % R * S::kStage;
+        const int left = min(ntok - page * kMxPage, (stop - page) * kMxPage);   // tokens from the step's first on
+
+        // the new token, the item's last entry: quantised into its place in the pool, and in the stage
+        if (arow >= 0 && stop == np && page + KP >= np) {
+          const int t = arow % kMxPage, k = np - 1 - page;
+          uint8_t* slab = p.pool + (int64_t)pt[lane_of64(h_first, it) + np - 1] * p.page_bytes +
+                          (int64_t)lane_of(h_slot, it) * S::kSlab;
+          if (lane < 2 * LPR) {
+            const bool is_v = lane >= LPR;
+            const int e = lane % LPR * E;
+            float x[E];
+            uint32_t scale;
+            Row16<T>::unpack(tok, x);
+            uint8_t* const mine = stage + k * S::kStagePage;
+            if (is_v) {
+              const u2 c = mx_quantise<E>(x, VB, &scale);
+              mx_store<E>(slab + at.v_codes, slab + at.v_scales, t, e, D, VB, true, c, scale);
+              mx_store<E>(mine + at.v_codes, mine + at.v_scales, t, e, D, VB, true, c, scale);
             } else {
-#pragma unroll
-              for (int w = 0; w < VW / 4; ++w) t.v[k][r * (VW / 4) + w] = 0u;
+              const u2 c = mx_quantise<E>(x, KB, &scale);
+              mx_store<E>(slab, slab + at.k_scales, t, e, D, KB, false, c, scale);
+              mx_store<E>(mine, mine + at.k_scales, t, e, D, KB, false, c, scale);
             }
           }
+          __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+          __builtin_amdgcn_wave_barrier();
+          __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
         }
-      }
-      float vs[KP][4];
-#pragma unroll
-      for (int k = 0; k < KP; ++k)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) vs[k][r] = mx_scale((t.vs[k] >> (8 * r)) & 0xffu);
-#pragma unroll
-      for (int i = 0; i < NV / 2; ++i) {   // dims 2i and 2i + 1 of the lane's sixteenth
-        u4 a, b;
+
+        float sv[4 * KP];
 #pragma unroll
         for (int k = 0; k < KP; ++k) {
-          uint32_t w[4];
+          const uint8_t* slab = stage + k * S::kStagePage;
+          uint32_t kc[KW];
+          load_codes<KW>(slab, lane, kc);
+          const float ks = mx_scale(slab[at.k_scales + (D == 128 ? rb : rb >> 1) * kMxPage + col]);
+          f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int r = 0; r < 4; ++r) w[r] = pair<VB>(t.v[k], r * (D / 32) + i, vs[k][r]);
-          a[2 * k] = __builtin_amdgcn_perm(w[1], w[0], 0x05040100u);
-          a[2 * k + 1] = __builtin_amdgcn_perm(w[3], w[2], 0x05040100u);
-          b[2 * k] = __builtin_amdgcn_perm(w[1], w[0], 0x07060302u);
-          b[2 * k + 1] = __builtin_amdgcn_perm(w[3], w[2], 0x07060302u);
+          for (int c = 0; c < NQ; ++c) {
+            const u4 a = {pair<KB>(kc, 4 * c, ks), pair<KB>(kc, 4 * c + 1, ks), pair<KB>(kc, 4 * c + 2, ks),
+                          pair<KB>(kc, 4 * c + 3, ks)};
+#pragma unroll
+            for (int part = 0; part < NPART; ++part) s = mfma(a, qv[part][c], s);
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) sv[4 * k + i] = s[i];
         }
+        // V's operands: dims 2i and 2i + 1 of the lane's sixteenth, pairs of tokens
+        uint32_t vc[KP][VW], vw[KP];
+        float vs[KP][4];
+        auto load_v = [&] {
 #pragma unroll
-        for (int part = 0; part < NPART; ++part) {
-          acc[2 * i] = mfma(a, pb[part], acc[2 * i]);
-          acc[2 * i + 1] = mfma(b, pb[part], acc[2 * i + 1]);
-        }
-      }
-    };
-
-    Tile t0, t1;
-    if (ns > 0) load(t0, 0);
-    if (ns > 1) load(t1, 1);
-    for (int s = 0; s < ns; s += 2) {
-      compute(t0, s);
-      if (s + 2 < ns) load(t0, s + 2);
-      if (s + 1 < ns) {
-        compute(t1, s + 1);
-        if (s + 3 < ns) load(t1, s + 3);
-      }
-    }
-
-    // the waves' states through LDS (a wave without a step has m = -inf and weight 0)
-    l = swap32_sum(swap16_sum(l));
-    if (col < G) {
-      float* dst = sm_acc + (wave * G + col) * (D + kPad) + rb * (D / 4);
+          for (int k = 0; k < KP; ++k) {
+            const uint8_t* slab = stage + k * S::kStagePage;
+            load_codes<VW>(slab + at.v_codes, lane, vc[k]);
+            vw[k] = *reinterpret_cast<const uint32_t*>(slab + at.v_scales + rb * (D / 8) + col / (512 / D) * 4);
+          }
+          if (left < KP * kMxPage) {   // rows past the retained length may hold anything: codes 0, scale 1
 #pragma unroll
-      for (int r = 0; r < 4; ++r)
+            for (int k = 0; k < KP; ++k) {
+              const int keep = min(max(left - k * kMxPage - 4 * rb, 0), 4);   // of the lane's 4 tokens
+              const uint32_t mask = keep == 4 ? ~0u : (1u << (8 * keep)) - 1u;
+              vw[k] = (vw[k] & mask) | (0x7f7f7f7fu & ~mask);
 #pragma unroll
-        for (int n = 0; n < NV; n += 4)
-          *reinterpret_cast<f32x4*>(dst + r * NV + n) = f32x4{acc[n][r], acc[n + 1][r], acc[n + 2][r], acc[n + 3][r]};
-      if (rb == 0) {
-        sm_m[wave * G + col] = m;
-        sm_l[wave * G + col] = l;
-      }
-    }
-    __syncthreads();   // every wave has read the live length too
-    if (threadIdx.x == 0) {
-      if (arow >= 0) p.live[(int64_t)item.b * p.live_stride + item.kv_head] = arow + 1;
-      if (arow == -2 && p.append_full) *p.append_full = 1;
-    }
-    const bool merges = item.out_idx >= 0 && p.merge_counters;
-    for (int o = threadIdx.x; o < G * (D / 4); o += kBlock) {
-      const int g = o / (D / 4), c = o % (D / 4);
-      float M = sm_m[g];
+              for (int r = 0; r < 4; ++r) {
+                const bool drop = r >= keep;
+                if constexpr (VW == 2) {
+                  vc[k][r / 2] &= drop ? (r % 2 ? 0x0000ffffu : 0xffff0000u) : ~0u;
+                } else {
 #pragma unroll
-      for (int w = 1; w < kWaves; ++w) M = fmaxf(M, sm_m[w * G + g]);
-      float L = 0.f;
-      f32x4 A = {0.f, 0.f, 0.f, 0.f};
-      const float mref = M > -INFINITY ? M : 0.f;
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) {
-        const float f = fast_exp2((sm_m[w * G + g] - mref) * cs);
-        L = fmaf(sm_l[w * G + g], f, L);
-        const f32x4 x = *reinterpret_cast<const f32x4*>(sm_acc + (w * G + g) * (D + kPad) + 4 * c);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) A[i] = fmaf(x[i], f, A[i]);
-      }
-      // no score above -inf: zeros, and an lse that loses against any other piece's
-      const float div = L == 0.f ? 1.f : L;
-      const f32x4 O = {A[0] / div, A[1] / div, A[2] / div, A[3] / div};
-      const float lse = L == 0.f ? -FLT_MAX : M * (cs * kLn2) + logf(L);
-      if (item.out_idx < 0) {
-        const int64_t row = (int64_t)item.b * p.num_q_heads + item.kv_head * G + g;
-        store4<T>(static_cast<T*>(p.out) + row * D + 4 * c, O);
-        if (p.lse && c == 0) p.lse[row] = lse;
-      } else {
-        const int64_t row = (int64_t)item.out_idx * G + g;
-        float* dst = p.part_o + row * D + 4 * c;
-        if (merges) {
-          // read in this launch by the workgroup that merges the unit, maybe on another XCD
-          uint64_t* d64 = reinterpret_cast<uint64_t*>(dst);
-          const auto word = [](float lo, float hi) {
-            return (uint64_t)__float_as_uint(lo) | ((uint64_t)__float_as_uint(hi) << 32);
-          };
-          __hip_atomic_store(d64, word(O[0], O[1]), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-          __hip_atomic_store(d64 + 1, word(O[2], O[3]), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-          if (c == 0) __hip_atomic_store(p.part_lse + row, lse, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        } else {
-          *reinterpret_cast<f32x4*>(dst) = O;
-          if (c == 0) p.part_lse[row] = lse;
-        }
-      }
-    }
-    if (merges) {
-      // The piece that arrives last merges its unit, with the recurrence and in the
-      // order of the merge launch.  The partials were written with device-scope
-      // stores and are complete (the wait) before the arrival is counted; they are
-      // read with device-scope loads issued after the count came back.
-      const int u = item.b * p.num_kv_heads + item.kv_head;
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      __syncthreads();
-      const int splits = p.unit_splits[u];
-      if (threadIdx.x == 0)
-        *sm_flag = __hip_atomic_fetch_add(p.merge_counters + u, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      __syncthreads();
-      if (*sm_flag == splits - 1) {
-        const int base = p.unit_partial_base[u];
-        for (int o = threadIdx.x; o < G * (D / 4); o += kBlock) {
-          const int g = o / (D / 4), c = o % (D / 4);
-          float M = -INFINITY, L = 0.f;
-          f32x4 A = {0.f, 0.f, 0.f, 0.f};
-          constexpr int kBatch = 4;
-          for (int i0 = 0; i0 < splits; i0 += kBatch) {
-            float lv[kBatch];
-            f32x4 ov[kBatch];
-#pragma unroll
-            for (int j = 0; j < kBatch; ++j) {
-              const int64_t row = (int64_t)(base + min(i0 + j, splits - 1)) * G + g;
-              lv[j] = __hip_atomic_load(p.part_lse + row, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-              const uint64_t* src = reinterpret_cast<const uint64_t*>(p.part_o + row * D + 4 * c);
-              const uint64_t lo = __hip_atomic_load(src, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-              const uint64_t hi = __hip_atomic_load(src + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-              ov[j] = f32x4{__uint_as_float((uint32_t)lo), __uint_as_float((uint32_t)(lo >> 32)),
-                            __uint_as_float((uint32_t)hi), __uint_as_float((uint32_t)(hi >> 32))};
-            }
-#pragma unroll
-            for (int j = 0; j < kBatch; ++j) {
-              const bool use = i0 + j < splits;
-              const float mn = fmaxf(M, lv[j]);
-              const float a = __expf(M - mn), w = __expf(lv[j] - mn);
-              const float Ln = fmaf(L, a, w);
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const float An = fmaf(A[i], a, w * ov[j][i]);
-                A[i] = use ? An : A[i];
+                  for (int w = 0; w < VW / 4; ++w) vc[k][r * (VW / 4) + w] = drop ? 0u : vc[k][r * (VW / 4) + w];
+                }
               }
-              L = use ? Ln : L;
-              M = use ? mn : M;
             }
           }
-          const int64_t row = (int64_t)item.b * p.num_q_heads + item.kv_head * G + g;
-          store4<T>(static_cast<T*>(p.out) + row * D + 4 * c, f32x4{A[0] / L, A[1] / L, A[2] / L, A[3] / L});
-          if (p.lse && c == 0) p.lse[row] = M + logf(L);
+#pragma unroll
+          for (int k = 0; k < KP; ++k)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) vs[k][r] = mx_scale((vw[k] >> (8 * r)) & 0xffu);
+        };
+        auto v_operands = [&](int i, uint32_t* a, uint32_t* b) {
+#pragma unroll
+          for (int k = 0; k < KP; ++k) {
+            uint32_t w[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) w[r] = pair<VB>(vc[k], r * (D / 32) + i, vs[k][r]);
+            a[2 * k] = __builtin_amdgcn_perm(w[1], w[0], 0x05040100u);
+            a[2 * k + 1] = __builtin_amdgcn_perm(w[3], w[2], 0x05040100u);
+            b[2 * k] = __builtin_amdgcn_perm(w[1], w[0], 0x07060302u);
+            b[2 * k + 1] = __builtin_amdgcn_perm(w[3], w[2], 0x07060302u);
+          }
+        };
+        uint32_t va[NV / 2][2 * KP], vb[NV / 2][2 * KP];
+        if constexpr (kEarly) {
+          load_v();
+#pragma unroll
+          for (int i = 0; i < NV / 2; ++i) v_operands(i, va[i], vb[i]);
         }
-        if (threadIdx.x == 0) __hip_atomic_store(p.merge_counters + u, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+
+        if (p.cap > 0.f) {
+#pragma unroll
+          for (int i = 0; i < 4 * KP; ++i) sv[i] = p.cap * tanh_f32(sv[i] * p.scale);
+        }
+        if (left < KP * kMxPage) {
+#pragma unroll
+          for (int i = 0; i < 4 * KP; ++i) sv[i] = i / 4 * kMxPage + 4 * rb + i % 4 < left ? sv[i] : -INFINITY;
+        }
+        float mx = sv[0];
+#pragma unroll
+        for (int i = 1; i < 4 * KP; ++i) mx = fmaxf(mx, sv[i]);
+        mx = swap32_max(swap16_max(mx));
+        const bool raise = (mx - m) * cs > kSlack;
+        if (__any(raise)) {
+          const float m_new = raise ? mx : m;
+          const float alpha = raise ? fast_exp2((m - m_new) * cs) : 1.f;   // 0 when m was -inf
+          l *= alpha;
+          m = m_new;
+#pragma unroll
+          for (int n = 0; n < NV; ++n) acc[n] *= alpha;
+        }
+        const float mref = m > -INFINITY ? m : 0.f;   // every score -inf so far: weights 0
+#pragma unroll
+        for (int i = 0; i < 4 * KP; ++i) sv[i] = fast_exp2((sv[i] - mref) * cs);
+        float sum = (sv[0] + sv[1]) + (sv[2] + sv[3]);
+        if constexpr (KP == 2) sum += (sv[4] + sv[5]) + (sv[6] + sv[7]);
+        l += sum;
+        uint32_t pb[NPART][2 * KP];
+#pragma unroll
+        for (int i = 0; i < 2 * KP; ++i) {
+          if constexpr (NPART == 1) {
+            // bf16 outputs: P rounded to bf16, half a step of the output's own
+            pb[0][i] = uint32_t(f32_to_bf16(sv[2 * i])) | (uint32_t(f32_to_bf16(sv[2 * i + 1])) << 16);
+          } else {
+            uint32_t a[3], b[3];
+            split3(sv[2 * i], a);
+            split3(sv[2 * i + 1], b);
+#pragma unroll
+            for (int s = 0; s < 3; ++s) pb[s][i] = join16(a[s], b[s]);
+          }
+        }
+        if constexpr (!kEarly) load_v();
+#pragma unroll
+        for (int i = 0; i < NV / 2; ++i) {
+          uint32_t a[2 * KP], b[2 * KP];
+          if constexpr (!kEarly) v_operands(i, a, b);
+#pragma unroll
+          for (int part = 0; part < NPART; ++part) {
+            acc[2 * i] = mfma_pv<KP>(kEarly ? va[i] : a, pb[part], acc[2 * i]);
+            acc[2 * i + 1] = mfma_pv<KP>(kEarly ? vb[i] : b, pb[part], acc[2 * i + 1]);
+          }
+        }
+      }
+      at_page += stop - first_page;
+
+      l = swap32_sum(swap16_sum(l));
+      const bool whole = first_page == 0 && stop == np;
+      if (whole) {
+        if (col < G) {
+          const float inv = 1.f / (l == 0.f ? 1.f : l);
+          const float lse = lse_of(m, l);
+          const int b = lane_of(h_b, it), h = lane_of(h_head, it), out_idx = lane_of(h_out, it);
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int n = 0; n < NV; n += 4)
+              write4(b, h, out_idx, col, rb * (D / 4) + r * NV + n,
+                     f32x4{acc[n][r] * inv, acc[n + 1][r] * inv, acc[n + 2][r] * inv, acc[n + 3][r] * inv}, lse);
+        }
+      } else if (col < G) {
+        // a shared item's state: parked if the wave goes on, else where its ring was (no load is in flight then)
+        uint8_t* state = at_page < f1 ? parks + (wave - 1) * park_bytes : ring;
+        float* dst = reinterpret_cast<float*>(state) + col * (D + kPad) + rb * (D / 4);
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+          for (int n = 0; n < NV; n += 4)
+            *reinterpret_cast<f32x4*>(dst + r * NV + n) = f32x4{acc[n][r], acc[n + 1][r], acc[n + 2][r], acc[n + 3][r]};
+        if (rb == 0) {
+          float* ml = reinterpret_cast<float*>(state + G * S::kRow) + 2 * col;
+          ml[0] = m;
+          ml[1] = l;
+        }
       }
     }
-    __syncthreads();   // the states may be overwritten
+    __syncthreads();
+
+    // items that a cut goes through
+    for (int w0 = 1, last_it = -1; w0 < kWaves; ++w0) {
+      const int c = cut(w0);
+      if (c >= pages) break;
+      const int j = __builtin_ctzll(__ballot(h_end > c) | (1ull << 63));   // the item of page c
+      if (c == begin_of(j) || j == last_it) continue;
+      last_it = j;
+      const int lo = begin_of(j), hi = lane_of(h_end, j);
+      const int b = lane_of(h_b, j), h = lane_of(h_head, j), out_idx = lane_of(h_out, j);
+      for (int o = threadIdx.x; o < G * (D / 4); o += kBlock) {
+        const int g = o / (D / 4), e = o % (D / 4) * 4;
+        float M = -INFINITY, L = 0.f, ms[kWaves];
+        const uint8_t* state[kWaves];
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+          // where wave w left its part of the item: with its last item, or parked
+          state[w] = cut(w + 1) <= hi ? lds + w * wave_bytes : parks + (w - 1) * park_bytes;
+          ms[w] = -INFINITY;
+          if (cut(w) < hi && cut(w + 1) > lo && cut(w) < cut(w + 1)) {
+            ms[w] = reinterpret_cast<const float*>(state[w] + G * S::kRow)[2 * g];
+            M = fmaxf(M, ms[w]);
+          }
+        }
+        f32x4 A = {0.f, 0.f, 0.f, 0.f};
+        const float mref = M > -INFINITY ? M : 0.f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+          if (!(cut(w) < hi && cut(w + 1) > lo && cut(w) < cut(w + 1))) continue;
+          const float f = fast_exp2((ms[w] - mref) * cs);
+          L = fmaf(reinterpret_cast<const float*>(state[w] + G * S::kRow)[2 * g + 1], f, L);
+          const f32x4 x = *reinterpret_cast<const f32x4*>(state[w] + g * S::kRow + e * 4);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) A[i] = fmaf(x[i], f, A[i]);
+        }
+        const float inv = 1.f / (L == 0.f ? 1.f : L);
+        write4(b, h, out_idx, g, e, f32x4{A[0] * inv, A[1] * inv, A[2] * inv, A[3] * inv}, lse_of(M, L));
+      }
+    }
+    if (wave == 0 && lane < n_items) {   // every wave has read the lengths
+      if (h_arow >= 0) p.live[(int64_t)h_b * p.live_stride + h_head] = h_arow + 1;
+      if (h_arow == -2 && p.append_full) *p.append_full = 1;
+    }
   }
+
   if (p.timestamps && threadIdx.x == 0) {
     p.timestamps[2 * blockIdx.x] = t_start;
-    p.timestamps[2 * blockIdx.x + 1] = it_begin < it_end ? __builtin_amdgcn_s_memrealtime() : t_start;
+    p.timestamps[2 * blockIdx.x + 1] = __builtin_amdgcn_s_memrealtime();
   }
 }
 
 using MxDecodeFn = void (*)(MxDecodeParams, const tg_work_item*, const int32_t*, const int32_t*);
 
-template <typename T, int D>
-MxDecodeFn pick_bits(int kb, int vb) {
-  if (kb == 4) return vb == 4 ? &tg_decode_mx_kernel<T, D, 4, 4> : &tg_decode_mx_kernel<T, D, 4, 8>;
-  return vb == 4 ? &tg_decode_mx_kernel<T, D, 8, 4> : &tg_decode_mx_kernel<T, D, 8, 8>;
+struct Picked {
+  MxDecodeFn fn;
+  size_t lds;   // bytes of a workgroup
+};
+
+template <typename T, int D, int KB, int VB>
+Picked picked(int gqa) {
+  return {&tg_decode_mx_kernel<T, D, KB, VB>, Shape<T, D, KB, VB>::lds_bytes(gqa)};
 }
 
-MxDecodeFn pick_decode_mx(int dtype, int d, const tg_mx_format& f) {
-  const int kb = tg::mx_bits(f.k_format), vb = tg::mx_bits(f.v_format);
-  if (dtype == TG_F32) return d == 64 ? pick_bits<float, 64>(kb, vb) : pick_bits<float, 128>(kb, vb);
-  return d == 64 ? pick_bits<uint16_t, 64>(kb, vb) : pick_bits<uint16_t, 128>(kb, vb);
+template <typename T, int D>
+Picked pick_bits(int kb, int vb, int gqa) {
+  if (kb == 4) return vb == 4 ? picked<T, D, 4, 4>(gqa) : picked<T, D, 4, 8>(gqa);
+  return vb == 4 ? picked<T, D, 8, 4>(gqa) : picked<T, D, 8, 8>(gqa);
+}
+
+Picked pick_decode_mx(int dtype, const tg_geometry& g, const tg_mx_format& f) {
+  const int kb = tg::mx_bits(f.k_format), vb = tg::mx_bits(f.v_format), gqa = g.num_q_heads / g.num_kv_heads;
+  if (dtype == TG_F32) return g.head_dim == 64 ? pick_bits<float, 64>(kb, vb, gqa) : pick_bits<float, 128>(kb, vb, gqa);
+  return g.head_dim == 64 ? pick_bits<uint16_t, 64>(kb, vb, gqa) : pick_bits<uint16_t, 128>(kb, vb, gqa);
 }
 
 size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
@@ -516,19 +648,18 @@ int32_t tg_decode_mx_bins(const tg_geometry* geom, int32_t dtype, const tg_mx_fo
         pages += tg::ceil_div(n, kMxPage);
       }
   }
-  const int gqa = geom->num_q_heads / geom->num_kv_heads;
-  MxDecodeFn fn = pick_decode_mx(dtype, geom->head_dim, *format);
+  const Picked k = pick_decode_mx(dtype, *geom, *format);
   int cus = 0, per_cu = 0, prev = 0;
   if (hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, device) != hipSuccess)
     return tg::fail(TG_ERR_HIP, "hipDeviceGetAttribute failed for device %d", device);
   if (hipGetDevice(&prev) != hipSuccess) return tg::fail(TG_ERR_HIP, "hipGetDevice failed");
   if (prev != device && hipSetDevice(device) != hipSuccess) return tg::fail(TG_ERR_HIP, "hipSetDevice failed");
-  const hipError_t e = hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, reinterpret_cast<const void*>(fn), kBlock,
-                                                                    lds_floats(gqa, geom->head_dim) * sizeof(float));
+  const hipError_t e =
+      hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, reinterpret_cast<const void*>(k.fn), kBlock, k.lds);
   if (prev != device) (void)hipSetDevice(prev);
   if (e != hipSuccess) return tg::fail(TG_ERR_HIP, "occupancy query failed: %s", hipGetErrorString(e));
   const int64_t most = (int64_t)per_cu * cus;
-  const int64_t want = kv_len ? tg::ceil_div(pages, kWaves * KP) : most;
+  const int64_t want = kv_len ? tg::ceil_div(pages, kWaves * 2) : most;
   *n_bins = (int32_t)(want < most ? want : most);
   return TG_OK;
 }
@@ -554,8 +685,6 @@ int32_t tg_decode_mx(const tg_decode_args* a, const tg_mx_format* format, float 
   p.num_kv_heads = g.num_kv_heads;
   p.n_bins = a->n_bins;
   p.gqa = gqa;
-  p.unit_splits = a->unit_splits;
-  p.unit_partial_base = a->unit_partial_base;
   p.out = a->out;
   p.lse = a->lse;
   p.part_o = reinterpret_cast<float*>(ws);
@@ -569,15 +698,13 @@ int32_t tg_decode_mx(const tg_decode_args* a, const tg_mx_format* format, float 
   p.cap = softcap;
   p.scale = a->sm_scale != 0.f ? a->sm_scale : 1.0f / std::sqrt((float)d);
   if (softcap > 0.f) p.scale /= softcap;
-  const bool merges = a->merge_counters && a->num_partials > 0 && tg::decode_merges_in_one_chain(a);
-  p.merge_counters = merges ? a->merge_counters : nullptr;
   if (a->num_items == 0) return TG_OK;
-  hipLaunchKernelGGL(pick_decode_mx(a->dtype, d, *format), dim3(a->n_bins), dim3(kBlock),
-                     lds_floats(gqa, d) * sizeof(float), static_cast<hipStream_t>(hip_stream), p, a->items, a->pt_pages,
-                     a->bin_offsets);
+  const Picked k = pick_decode_mx(a->dtype, g, *format);
+  hipLaunchKernelGGL(k.fn, dim3(a->n_bins), dim3(kBlock), k.lds, static_cast<hipStream_t>(hip_stream), p, a->items,
+                     a->pt_pages, a->bin_offsets);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return tg::fail(TG_ERR_HIP, "decode launch failed: %s", hipGetErrorString(e));
-  if (a->num_partials > 0 && !merges) return tg::launch_decode_merge(a, p.part_o, p.part_lse, hip_stream);
+  if (a->num_partials > 0) return tg::launch_decode_merge(a, p.part_o, p.part_lse, hip_stream);
   return TG_OK;
 }
 
