@@ -41,18 +41,19 @@ __host__ __device__ constexpr MxParts mx_parts(int d, int kb, int vb) {
 }
 
 // Byte of element e of token t among the codes of its part.  Elements that
-// follow e up to the end of its run (mx_run) have the bytes behind it.
+// follow e up to the end of its run (mx_run) have the bytes behind it.  d and
+// bits are powers of two: shifts, as a division costs more than the quantiser.
 __device__ __forceinline__ int mx_code_at(int t, int e, int d, int bits, bool is_v) {
-  const int lane = is_v ? (t >> 2) * 16 + e / (d >> 4) : e / (d >> 2) * 16 + t;
-  const int el = is_v ? (t & 3) * (d >> 4) + e % (d >> 4) : e % (d >> 2);
-  const int byte = el * bits >> 3;
-  const int chunk = min(16, d * bits >> 5);
-  return byte / chunk * 64 * chunk + lane * chunk + byte % chunk;
+  const int ld = d == 128 ? 7 : 6, pack = bits == 4 ? 1 : 0;   // log2 of d, of codes in a byte
+  const int lane = is_v ? (t >> 2) * 16 + (e >> (ld - 4)) : (e >> (ld - 2)) * 16 + t;
+  const int el = is_v ? ((t & 3) << (ld - 4)) + (e & ((1 << (ld - 4)) - 1)) : e & ((1 << (ld - 2)) - 1);
+  const int byte = el >> pack, chunk = min(4, ld - 2 - pack);  // log2 of a chunk's bytes
+  return ((byte >> chunk) << (chunk + 6)) + (lane << chunk) + (byte & ((1 << chunk) - 1));
 }
 // Elements of a row that lie in consecutive bytes: at least this many, aligned.
-__device__ __forceinline__ int mx_run(int d, bool is_v) { return is_v ? min(8, d >> 4) : 8; }
+__device__ __forceinline__ int mx_run(int d, bool is_v) { return is_v && d == 64 ? 4 : 8; }
 __device__ __forceinline__ int mx_scale_at(int t, int group, int d, bool is_v) {
-  return is_v ? (t >> 2) * 4 * (d / kMxGroup) + group * 4 + (t & 3) : group * kMxPage + t;
+  return is_v ? (t >> 2) * (d == 128 ? 16 : 8) + group * 4 + (t & 3) : group * kMxPage + t;
 }
 
 // The 16 bytes of a row that a lane holds, as fp32.

@@ -63,14 +63,14 @@ struct UnpackParams {
   const uint8_t* pool;
   u4* rows;
   const int32_t* pt_pages;
-  const int32_t* dst_pages;
+  const int32_t* dst_pages;   // = pt_pages where there are none
   const int64_t* pt_offsets;
   const int32_t* group_of;
   const int32_t* slot_of;
   const int32_t* begin;   // [B][L][H] or NULL
   const int32_t* len;     // [B][L][H]
   int32_t L, H, G, Hp, layer;
-  int32_t waves;          // waves that share a unit
+  int64_t units;
 };
 
 // 16 bytes of a row from its codes
@@ -88,50 +88,135 @@ __device__ __forceinline__ u4 row16(const u2& c, float s) {
   }
 }
 
-// A wave takes a page of one head at a time: every lane 16 bytes of a row, so that
-// the stores, most of the bytes, are whole rows in order.
+constexpr int kUnits = 1024;    // (request, head) units shared out at once
+constexpr int kUnpackWgs = 512;
+
+// The lengths are on the device and differ a lot between heads, so the pages are
+// shared out here: every workgroup lays the units' pages end to end (a sum over
+// the units in LDS) and every wave takes an equal range of them, up to 64 pages at
+// a time, one a lane for what is looked up per page.  A lane reads and writes 16
+// bytes of a row, so that the stores, most of the bytes, are whole rows in order;
+// a page's codes are requested before the page before it is stored.
 template <typename T, int D, int KB, int VB>
 __global__ __launch_bounds__(kThreads) void tg_unpack_mx_kernel(UnpackParams p) {
   constexpr int E = Row16<T>::kElems;
   constexpr int LPR = D / E;                 // lanes per row
   constexpr int RPP = 64 / LPR;              // rows at once
   constexpr int NR = kMxPage / RPP;
+  constexpr int kSlab = mx_slab_bytes(D, KB, VB);
+  constexpr int kPer = kUnits / kThreads;    // units of a thread
   constexpr MxParts at = mx_parts(D, KB, VB);
+  __shared__ int64_t sm_end[kUnits];         // pages up to and with the unit's
+  __shared__ int64_t sm_first[kUnits];       // of the unit's page ids, from its first entry read
+  __shared__ int32_t sm_lo[kUnits], sm_hi[kUnits];
+  __shared__ int64_t sm_wave[kThreads / 64];
+
   const int lane = threadIdx.x & 63;
-  const int64_t w = (int64_t)blockIdx.x * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t unit = w / p.waves;
-  const int first = (int)(w % p.waves);
-  const int64_t b = unit / p.H;
-  const int h = (int)(unit % p.H);
-  const int64_t lh = (int64_t)p.layer * p.H + h, blh = (b * p.L + p.layer) * p.H + h;
-  const TablePages table = table_of(p.pt_offsets, (b * p.L + p.layer) * p.G, p.group_of[lh], p.G);
-  const int64_t cap = table.pages * kMxPage;
-  const int64_t lo = p.begin ? max(p.begin[blh], 0) : 0, hi = min((int64_t)p.len[blh], cap);
-  const int slot = p.slot_of[lh];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t w = (int64_t)blockIdx.x * (kThreads / 64) + wave, waves = (int64_t)gridDim.x * (kThreads / 64);
   const int sub = lane % LPR, r0 = lane / LPR;
-  for (int64_t pg = lo / kMxPage + first; pg * kMxPage < hi; pg += p.waves) {
-    const uint8_t* slab = p.pool + ((int64_t)p.pt_pages[table.base + pg] * p.Hp + slot) * mx_slab_bytes(D, KB, VB);
-    u2 kc[NR], vc[NR];
-    uint32_t ks[NR], vs[NR];
+
+  for (int64_t u0 = 0; u0 < p.units; u0 += kUnits) {
+    const int n = (int)min((int64_t)kUnits, p.units - u0);
+    int64_t mine[kPer], sum = 0;
 #pragma unroll
-    for (int i = 0; i < NR; ++i) {
-      const int t = i * RPP + r0;
-      kc[i] = mx_load<E>(slab, t, sub * E, D, KB, false);
-      vc[i] = mx_load<E>(slab + at.v_codes, t, sub * E, D, VB, true);
-      ks[i] = slab[at.k_scales + mx_scale_at(t, sub * E / kMxGroup, D, false)];
-      vs[i] = slab[at.v_scales + mx_scale_at(t, sub * E / kMxGroup, D, true)];
+    for (int i = 0; i < kPer; ++i) {
+      const int k = threadIdx.x * kPer + i;
+      int64_t pages = 0;
+      if (k < n) {
+        const int64_t b = (uint32_t)(u0 + k) / (uint32_t)p.H;
+        const int h = (int)((uint32_t)(u0 + k) % (uint32_t)p.H);
+        const int64_t blh = (b * p.L + p.layer) * p.H + h;
+        const TablePages table =
+            table_of(p.pt_offsets, (b * p.L + p.layer) * p.G, p.group_of[(int64_t)p.layer * p.H + h], p.G);
+        const int32_t lo = p.begin ? max(p.begin[blh], 0) : 0;
+        const int32_t hi = (int32_t)min((int64_t)p.len[blh], table.pages * kMxPage);
+        sm_lo[k] = lo;
+        sm_hi[k] = hi;
+        sm_first[k] = table.base + lo / kMxPage;
+        pages = hi > lo ? (hi - 1) / kMxPage - lo / kMxPage + 1 : 0;
+      }
+      sum += pages;
+      mine[i] = sum;
     }
-    const int64_t dst = (p.dst_pages ? p.dst_pages : p.pt_pages)[table.base + pg];
-    u4* kr = p.rows + ((dst * 2 * p.Hp + slot) * kMxPage) * LPR + lane;
-    u4* vr = kr + (int64_t)p.Hp * kMxPage * LPR;
+    int64_t before = sum;   // of the threads up to and with this one, in its wave
 #pragma unroll
-    for (int i = 0; i < NR; ++i) {
-      const int64_t entry = pg * kMxPage + i * RPP + r0;
-      if (entry >= lo && entry < hi) {
-        kr[i * 64] = row16<T, KB>(kc[i], mx_scale(ks[i]));
-        vr[i * 64] = row16<T, VB>(vc[i], mx_scale(vs[i]));
+    for (int s = 1; s < 64; s *= 2) {
+      const int64_t x = __shfl_up(before, s);
+      before += lane >= s ? x : 0;
+    }
+    if (lane == 63) sm_wave[wave] = before;
+    __syncthreads();
+    before -= sum;
+    for (int i = 0; i < wave; ++i) before += sm_wave[i];
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) sm_end[threadIdx.x * kPer + i] = before + mine[i];
+    __syncthreads();
+
+    const int64_t total = sm_end[kUnits - 1];
+    const int64_t f1 = total * (w + 1) / waves;
+    for (int64_t f = total * w / waves; f < f1; f += 64) {
+      const int count = (int)min((int64_t)64, f1 - f);
+      // of page f + lane: its slab, its rows in the other pool, the rows to write
+      int64_t src = 0, dst = 0;
+      int32_t from = 0, to = 0;
+      if (lane < count) {
+        int u = 0;
+#pragma unroll
+        for (int s = kUnits / 2; s > 0; s /= 2) u += sm_end[u + s - 1] <= f + lane ? s : 0;
+        const int64_t at_page = f + lane - (u > 0 ? sm_end[u - 1] : 0);
+        const int h = (int)((uint32_t)(u0 + u) % (uint32_t)p.H);
+        const int slot = p.slot_of[(int64_t)p.layer * p.H + h];
+        const int64_t id = sm_first[u] + at_page;
+        const int32_t row = (int32_t)(sm_lo[u] / kMxPage + at_page) * kMxPage;
+        src = ((int64_t)p.pt_pages[id] * p.Hp + slot) * kSlab;
+        dst = ((int64_t)p.dst_pages[id] * 2 * p.Hp + slot) * kMxPage;
+        from = sm_lo[u] - row;
+        to = sm_hi[u] - row;
+      }
+      auto of64 = [](int64_t x, int j) {
+        return (int64_t)(((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int32_t)(x >> 32), j) << 32) |
+                         (uint32_t)__builtin_amdgcn_readlane((int32_t)x, j));
+      };
+      struct Page {
+        u2 kc[NR], vc[NR];
+        uint32_t ks[NR], vs[NR];
+      };
+      auto load = [&](Page& g, int j) {
+        const uint8_t* slab = p.pool + of64(src, j);
+#pragma unroll
+        for (int i = 0; i < NR; ++i) {
+          const int t = i * RPP + r0;
+          g.kc[i] = mx_load<E>(slab, t, sub * E, D, KB, false);
+          g.vc[i] = mx_load<E>(slab + at.v_codes, t, sub * E, D, VB, true);
+          g.ks[i] = slab[at.k_scales + mx_scale_at(t, sub * E / kMxGroup, D, false)];
+          g.vs[i] = slab[at.v_scales + mx_scale_at(t, sub * E / kMxGroup, D, true)];
+        }
+      };
+      auto store = [&](const Page& g, int j) {
+        u4* kr = p.rows + of64(dst, j) * LPR + lane;
+        u4* vr = kr + (int64_t)p.Hp * kMxPage * LPR;
+        const int lo = __builtin_amdgcn_readlane(from, j), hi = __builtin_amdgcn_readlane(to, j);
+#pragma unroll
+        for (int i = 0; i < NR; ++i) {
+          const int t = i * RPP + r0;
+          if (t >= lo && t < hi) {
+            __builtin_nontemporal_store(row16<T, KB>(g.kc[i], mx_scale(g.ks[i])), kr + i * 64);
+            __builtin_nontemporal_store(row16<T, VB>(g.vc[i], mx_scale(g.vs[i])), vr + i * 64);
+          }
+        }
+      };
+      Page a, b;
+      load(a, 0);
+      for (int j = 0; j < count; j += 2) {
+        if (j + 1 < count) load(b, j + 1);
+        store(a, j);
+        if (j + 1 >= count) break;
+        if (j + 2 < count) load(a, j + 2);
+        store(b, j + 1);
       }
     }
+    if (u0 + kUnits < p.units) __syncthreads();   // the sums may be written again
   }
 }
 
@@ -209,7 +294,7 @@ int32_t tg_unpack_mx(const tg_unpack_mx_args* a, void* hip_stream) {
   p.pool = static_cast<const uint8_t*>(a->mx_pool);
   p.rows = static_cast<u4*>(a->kv_pool);
   p.pt_pages = a->pt_pages;
-  p.dst_pages = a->dst_pages;
+  p.dst_pages = a->dst_pages ? a->dst_pages : a->pt_pages;
   p.pt_offsets = a->pt_offsets;
   p.group_of = a->group_of;
   p.slot_of = a->slot_of;
@@ -220,15 +305,12 @@ int32_t tg_unpack_mx(const tg_unpack_mx_args* a, void* hip_stream) {
   p.Hp = g.heads_per_group;
   p.G = g.num_kv_heads / g.heads_per_group;
   p.layer = a->layer;
-  const int64_t units = (int64_t)a->batch * g.num_kv_heads;
-  // the lengths are on the device: every unit gets the same number of waves
-  p.waves = (int32_t)(4 * tg::ceil_div(2048, units) < 16 ? 16 : 4 * tg::ceil_div(2048, units));
-  const int64_t blocks = units * p.waves / 4;
-  if (blocks > INT32_MAX) return tg::fail(TG_ERR_INVALID_ARG, "batch too large");
+  p.units = (int64_t)a->batch * g.num_kv_heads;
+  if (p.units > INT32_MAX) return tg::fail(TG_ERR_INVALID_ARG, "batch too large");
   const int kb = tg::mx_bits(a->format.k_format), vb = tg::mx_bits(a->format.v_format);
   UnpackFn fn = a->dtype == TG_F32 ? (g.head_dim == 64 ? pick_unpack<float, 64>(kb, vb) : pick_unpack<float, 128>(kb, vb))
                                    : (g.head_dim == 64 ? pick_unpack<uint16_t, 64>(kb, vb) : pick_unpack<uint16_t, 128>(kb, vb));
-  hipLaunchKernelGGL(fn, dim3((unsigned)blocks), dim3(kThreads), 0, static_cast<hipStream_t>(hip_stream), p);
+  hipLaunchKernelGGL(fn, dim3(kUnpackWgs), dim3(kThreads), 0, static_cast<hipStream_t>(hip_stream), p);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return tg::fail(TG_ERR_HIP, "unpack launch failed: %s", hipGetErrorString(e));
   return TG_OK;
