@@ -242,6 +242,10 @@ __global__ __launch_bounds__(kSelThreads) void tg_compress_select_kernel(SelectP
   }
 }
 
+// Waves of an item in the one-launch form.
+template <typename Row>
+constexpr int kItemWaves = std::is_same_v<Row, Raw> ? 1 : 2;
+
 // Copies the K and V rows of ranks [r0, r0 + rows) of one unit: rank j's
 // chunk index is tok(j); it goes to the head's entry cursor + j.  Called by a
 // whole workgroup, kUnroll rows in flight per thread.  Bound by HBM.
@@ -286,12 +290,9 @@ __device__ __forceinline__ void copy_rows(const CopyParams& p, const tg_compress
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u) {
         const int j = base + u * rpp + rsel;
-        float x[E];
         uint32_t ks, vs;
-        tgd::Row16<T>::unpack(kk[u], x);
-        const tgd::u2 kc = tgd::mx_quantise<E>(x, p.kb, &ks);
-        tgd::Row16<T>::unpack(vv[u], x);
-        const tgd::u2 vc = tgd::mx_quantise<E>(x, p.vb, &vs);
+        const tgd::u2 kc = tgd::mx_quantise<T>(kk[u], p.kb, &ks);
+        const tgd::u2 vc = tgd::mx_quantise<T>(vv[u], p.vb, &vs);
         if (j < rows) {   // the lanes of a row together
           const int t = (it.cursor + r0 + j) % tgd::kMxPage;
           uint8_t* slab = pool + ((int64_t)page[u] * p.Hp + it.slot) * tgd::mx_slab_bytes(d, p.kb, p.vb);
@@ -340,11 +341,15 @@ __global__ __launch_bounds__(kThreads) void tg_compress_copy_kernel(CopyParams p
 // workgroups spread the items over every CU (measured at chunk 512: 7.9 us,
 // against 8.1, 9.3 and 12.1 us with 4, 8 and 16 items per workgroup).
 template <typename Row, int KPL>
-__global__ __launch_bounds__(64) void tg_compress_wave_kernel(SelectParams sp, CopyParams p, int32_t n_items) {
+__global__ __launch_bounds__(64 * kItemWaves<Row>) void tg_compress_wave_kernel(SelectParams sp, CopyParams p, int32_t n_items) {
   constexpr int kSpill = kFusedMaxChunk;        // per-lane dummy entries for branch-free stores
-  __shared__ __align__(16) uint32_t hist[kBins];
-  __shared__ int32_t kept_lds[kFusedMaxChunk + 64];
-  const int lane = threadIdx.x;
+  constexpr int NW = kItemWaves<Row>;
+  __shared__ __align__(16) uint32_t hist_all[NW][kBins];
+  __shared__ int32_t kept_all[NW][kFusedMaxChunk + 64];
+  const int lane = threadIdx.x & 63;
+  const int wave = NW > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
+  uint32_t* const hist = hist_all[wave];
+  int32_t* const kept_lds = kept_all[wave];
   const int item = blockIdx.x;
   if (item >= n_items) return;
   const tg_compress_item it = load_item((const TG_CONST tg_compress_item*)p.items + item);
@@ -429,8 +434,10 @@ __global__ __launch_bounds__(64) void tg_compress_wave_kernel(SelectParams sp, C
   }
   const int r0 = max(it.rank_begin, 0);
   const int r1 = min(min(it.rank_end, min(count, min(it.count, p.C))), r0 + TG_COMPRESS_MAX_ROWS);
-  copy_rows<Row, 8, true>(p, it, r0, r1 - r0, [&](int j) { return kl[r0 + j]; }, lane, 64);
-  if (it.rank_begin == 0) {
+  // each wave has ranked the chunk for itself and takes its share of the ranks
+  const int a0 = r0 + max(r1 - r0, 0) * wave / NW, a1 = r0 + max(r1 - r0, 0) * (wave + 1) / NW;
+  copy_rows<Row, 8 / NW, true>(p, it, a0, a1 - a0, [&](int j) { return kl[a0 + j]; }, lane, 64);
+  if (it.rank_begin == 0 && wave == 0) {
     int32_t* out = sp.kept + unit * p.C;
     for (int r = lane; r < count; r += 64) out[r] = kl[r];
   }
@@ -441,7 +448,7 @@ template <typename Row>
 int32_t launch(const tg_compress_args* a, const SelectParams& s, const CopyParams& c, hipStream_t stream) {
   if (a->chunk_len <= kFusedMaxChunk) {
     const int kpl = (a->chunk_len + 63) / 64;
-    const dim3 grid((unsigned)a->num_items), block(64);
+    const dim3 grid((unsigned)a->num_items), block(64 * kItemWaves<Row>);
     if (kpl <= 1) hipLaunchKernelGGL((tg_compress_wave_kernel<Row, 1>), grid, block, 0, stream, s, c, a->num_items);
     else if (kpl <= 2) hipLaunchKernelGGL((tg_compress_wave_kernel<Row, 2>), grid, block, 0, stream, s, c, a->num_items);
     else if (kpl <= 4) hipLaunchKernelGGL((tg_compress_wave_kernel<Row, 4>), grid, block, 0, stream, s, c, a->num_items);

@@ -376,16 +376,14 @@ __global__ void __launch_bounds__(kBlock, 2)
           if (lane < 2 * LPR) {
             const bool is_v = lane >= LPR;
             const int e = lane % LPR * E;
-            float x[E];
             uint32_t scale;
-            Row16<T>::unpack(tok, x);
             uint8_t* const mine = stage + k * S::kStagePage;
             if (is_v) {
-              const u2 c = mx_quantise<E>(x, VB, &scale);
+              const u2 c = mx_quantise<T>(tok, VB, &scale);
               mx_store<E>(slab + at.v_codes, slab + at.v_scales, t, e, D, VB, true, c, scale);
               mx_store<E>(mine + at.v_codes, mine + at.v_scales, t, e, D, VB, true, c, scale);
             } else {
-              const u2 c = mx_quantise<E>(x, KB, &scale);
+              const u2 c = mx_quantise<T>(tok, KB, &scale);
               mx_store<E>(slab, slab + at.k_scales, t, e, D, KB, false, c, scale);
               mx_store<E>(mine, mine + at.k_scales, t, e, D, KB, false, c, scale);
             }

@@ -56,18 +56,54 @@ __device__ __forceinline__ int mx_scale_at(int t, int group, int d, bool is_v) {
   return is_v ? (t >> 2) * (d == 128 ? 16 : 8) + group * 4 + (t & 3) : group * kMxPage + t;
 }
 
-// The 16 bytes of a row that a lane holds, as fp32.
+// The 16 bytes of a row that a lane holds: the bits of the largest magnitude among
+// them as fp32 (as integers NaN is above infinity, and both above every number),
+// and the conversions of 4 elements, word 2 i or 4 i on, with scale s.
 template <typename T>
 struct Row16;
 template <>
 struct Row16<uint16_t> {
+  typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
   static constexpr int kElems = 8;
-  __device__ __forceinline__ static void unpack(const u4& v, float* f) {
+  // by value: a bit cast of a vector's element in place takes the first one
+  __device__ __forceinline__ static bf16x2 words(u4 v, int i) {
+    const uint32_t w = v[i];
+    return __builtin_bit_cast(bf16x2, w);
+  }
+  __device__ __forceinline__ static uint32_t top(const u4& v) {
+    u16x2 m = __builtin_bit_cast(u16x2, v[0] & 0x7fff7fffu);
+#pragma unroll
+    for (int i = 1; i < 4; ++i) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, v[i] & 0x7fff7fffu));
+    return (uint32_t)max(m.x, m.y) << 16;
+  }
+  __device__ __forceinline__ static uint32_t fp4(const u4& v, float s) {
+    uint32_t c = 0;
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, words(v, 0), s, 0);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, words(v, 1), s, 1);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, words(v, 2), s, 2);
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, words(v, 3), s, 3);
+  }
+  __device__ __forceinline__ static u2 fp8(const u4& v, float s) {
+    u2 r;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      s16x2 c = {0, 0};
+      c = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(c, words(v, 2 * i), s, false);
+      c = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(c, words(v, 2 * i + 1), s, true);
+      r[i] = __builtin_bit_cast(uint32_t, c);
+    }
+    return r;
+  }
+  // magnitudes above bits `most` of fp32 become those (a bf16 number)
+  __device__ __forceinline__ static u4 clamp(const u4& v, uint32_t most) {
+    u4 r;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      f[2 * i] = bf16_lo(v[i]);
-      f[2 * i + 1] = bf16_hi(v[i]);
+      const u16x2 m = __builtin_elementwise_min(__builtin_bit_cast(u16x2, v[i] & 0x7fff7fffu),
+                                                u16x2{(uint16_t)(most >> 16), (uint16_t)(most >> 16)});
+      r[i] = __builtin_bit_cast(uint32_t, m) | (v[i] & 0x80008000u);
     }
+    return r;
   }
 };
 template <>
@@ -77,6 +113,29 @@ struct Row16<float> {
 #pragma unroll
     for (int i = 0; i < 4; ++i) f[i] = __uint_as_float(v[i]);
   }
+  __device__ __forceinline__ static uint32_t top(const u4& v) {
+    return max(max(v[0] & 0x7fffffffu, v[1] & 0x7fffffffu), max(v[2] & 0x7fffffffu, v[3] & 0x7fffffffu));
+  }
+  __device__ __forceinline__ static uint32_t fp4(const u4& v, float s) {
+    float x[4];
+    unpack(v, x);
+    const uint32_t c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, x[0], x[1], s, 0);
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[2], x[3], s, 1);
+  }
+  __device__ __forceinline__ static u2 fp8(const u4& v, float s) {
+    float x[4];
+    unpack(v, x);
+    s16x2 c = {0, 0};
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(c, x[0], x[1], s, false);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(c, x[2], x[3], s, true);
+    return u2{__builtin_bit_cast(uint32_t, c), 0u};
+  }
+  __device__ __forceinline__ static u4 clamp(const u4& v, uint32_t most) {
+    u4 r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r[i] = min(v[i] & 0x7fffffffu, most) | (v[i] & 0x80000000u);
+    return r;
+  }
 };
 
 template <int CTRL>
@@ -84,54 +143,37 @@ __device__ __forceinline__ uint32_t dpp_max_u32(uint32_t x) {
   return max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, false));
 }
 
-// Codes of a lane's E elements (the lanes of a group of 32 lie side by side and
-// call this together): the scale is 2^e, e the least integer with max|x| <= top
-// 2^e, top 7 (4 bits) or 464 (8 bits), the midpoint between the largest value and
-// the step that would follow; an element is x / 2^e to the nearest, ties to even,
-// at most the largest.  All of it is exact but the one rounding of the element,
-// so it depends on nothing but the input.  A group with a NaN or an infinity gets
-// scale byte 255 and codes 0, which stand for NaN.
-// Returns the codes, E * bits / 8 bytes, low bytes first, and *scale, e + 127.
-template <int E>
-__device__ __forceinline__ u2 mx_quantise(const float* x, int bits, uint32_t* scale) {
-  uint32_t top = 0;
-#pragma unroll
-  for (int i = 0; i < E; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);   // as integers: NaN above infinity
+// Codes of the elements that a lane holds (the lanes of a group of 32 lie side by
+// side and call this together): the scale is 2^e, e the least integer with max|x|
+// <= top 2^e, top 7 (4 bits) or 464 (8 bits), the midpoint between the largest
+// value and the step that would follow; an element is x / 2^e to the nearest, ties
+// to even, at most the largest.  All of it is exact but the one rounding of the
+// element, so it depends on nothing but the input.  A group with a NaN or an
+// infinity gets scale byte 255 and codes 0, which stand for NaN.
+// Returns the codes, low bytes first, and *scale, e + 127.
+template <typename T>
+__device__ __forceinline__ u2 mx_quantise(u4 x, int bits, uint32_t* scale) {
+  uint32_t top = Row16<T>::top(x);
   top = dpp_max_u32<kQuadXor1>(top);
   top = dpp_max_u32<kQuadXor2>(top);
-  if constexpr (E == 4) top = dpp_max_u32<kRowHalfMirror>(top);
-  const int expo = (int)(top >> 23), frac = (int)(top & 0x7fffffu);
+  if constexpr (sizeof(T) == 4) top = dpp_max_u32<kRowHalfMirror>(top);
+  // the exponent of top * 2^-2 (4 bits, 7 = 1.75 * 2^2) or top * 2^-8 (464 = 1.8125 * 2^8), one more past
+  // 1.75 or 1.8125; within bounds that keep every value a normal bf16 number
+  const int up = bits == 4 ? 0x1fffff : 0x17ffff, shift = bits == 4 ? 2 : 8;
+  const int e = min(max((int)((top + up) >> 23) - shift, bits == 4 ? 2 : 10), bits == 4 ? 252 : 246);
+  const float s = __uint_as_float((uint32_t)e << 23);
   const bool finite = top < 0x7f800000u;
+  *scale = finite ? (uint32_t)e : 255u;
   u2 r = {0u, 0u};
   if (bits == 4) {
-    // 7 = 1.75 * 2^2; within [-125, 125] every value is a normal bf16 number
-    const int e = min(max(expo - 2 + (frac > 0x600000), 2), 252);
-    const float s = __uint_as_float((uint32_t)e << 23);
-    uint32_t c = 0;
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[0], x[1], s, 0);
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[2], x[3], s, 1);
-    if constexpr (E == 8) {
-      c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[4], x[5], s, 2);
-      c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[6], x[7], s, 3);
-    }
-    r.x = finite ? c : 0u;
-    *scale = finite ? (uint32_t)e : 255u;
+    r.x = finite ? Row16<T>::fp4(x, s) : 0u;
   } else {
-    // 464 = 1.8125 * 2^8; [-117, 119]
-    const int e = min(max(expo - 8 + (frac > 0x680000), 10), 246);
-    const float s = __uint_as_float((uint32_t)e << 23);
-    const float most = 448.f * s;   // the conversion makes NaN of what rounds past 448
-    float y[E];
-#pragma unroll
-    for (int i = 0; i < E; ++i) y[i] = fminf(fmaxf(x[i], -most), most);
-#pragma unroll
-    for (int w = 0; w < E / 4; ++w) {
-      s16x2 c = {0, 0};
-      c = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(c, y[4 * w], y[4 * w + 1], s, false);
-      c = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(c, y[4 * w + 2], y[4 * w + 3], s, true);
-      r[w] = finite ? __builtin_bit_cast(uint32_t, c) : 0u;
-    }
-    *scale = finite ? (uint32_t)e : 255u;
+    // past 464 * 2^119 alone is a value left that the conversion would make NaN of
+    constexpr uint32_t kMost = (246u << 23) + (8u << 23) + 0x600000u;   // 448 * 2^119
+    if (top > kMost) x = Row16<T>::clamp(x, kMost);
+    r = Row16<T>::fp8(x, s);
+    r.x = finite ? r.x : 0u;
+    r.y = finite ? r.y : 0u;
   }
   return r;
 }

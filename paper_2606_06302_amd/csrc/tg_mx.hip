@@ -47,13 +47,10 @@ __global__ __launch_bounds__(kThreads) void tg_append_mx_kernel(AppendParams p) 
   const int64_t page = p.pt_pages[table.base + n / kMxPage];
   uint8_t* slab = p.pool + (page * p.Hp + p.slot_of[lh]) * mx_slab_bytes(p.d, p.kb, p.vb);
   const MxParts at = mx_parts(p.d, p.kb, p.vb);
-  float x[E];
   uint32_t scale;
-  Row16<T>::unpack(kv, x);
-  u2 c = mx_quantise<E>(x, p.kb, &scale);
+  u2 c = mx_quantise<T>(kv, p.kb, &scale);
   mx_store<E>(slab, slab + at.k_scales, n % kMxPage, sub * E, p.d, p.kb, false, c, scale);
-  Row16<T>::unpack(vv, x);
-  c = mx_quantise<E>(x, p.vb, &scale);
+  c = mx_quantise<T>(vv, p.vb, &scale);
   mx_store<E>(slab + at.v_codes, slab + at.v_scales, n % kMxPage, sub * E, p.d, p.vb, true, c, scale);
   // every lane of the unit has read n (same wave, same load)
   if (sub == 0) *live = n + 1;
