@@ -33,6 +33,8 @@
 
 namespace {
 
+using tgd::wave_inclusive_sum;
+
 constexpr int kThreads = 256;           // copy launch
 constexpr int kBins = 256;              // one radix digit of 8 bits (short chunks)
 constexpr int kUnroll = 4;           // rows in flight per thread in the copy launch
@@ -91,25 +93,6 @@ __device__ __forceinline__ tg_compress_item load_item(const TG_CONST tg_compress
   r.rank_begin = src->rank_begin;
   r.rank_end = src->rank_end;
   return r;
-}
-
-// DPP lane movement with zero fill (row_mask selects the 16-lane rows updated).
-template <int CTRL, int ROW_MASK>
-__device__ __forceinline__ int dpp_add_src(int x) {
-  return __builtin_amdgcn_update_dpp(0, x, CTRL, ROW_MASK, 0xF, true);
-}
-
-// Inclusive prefix sum over the 64 lanes of a wave: shifts by 1, 2, 4 and 8
-// inside each 16-lane row, then row 0's total into row 1 and row 2's into row
-// 3 (row_bcast:15), then rows 0-1's total into rows 2 and 3 (row_bcast:31).
-__device__ __forceinline__ int wave_inclusive_sum(int x) {
-  x += dpp_add_src<0x111, 0xF>(x);
-  x += dpp_add_src<0x112, 0xF>(x);
-  x += dpp_add_src<0x114, 0xF>(x);
-  x += dpp_add_src<0x118, 0xF>(x);
-  x += dpp_add_src<0x142, 0xA>(x);
-  x += dpp_add_src<0x143, 0xC>(x);
-  return x;
 }
 
 // Number of set bits of `mask` at lanes below the calling lane.

@@ -121,14 +121,34 @@ __device__ __forceinline__ void split3(float x, uint32_t* part) {
 }
 __device__ __forceinline__ uint32_t join16(uint32_t lo, uint32_t hi) { return __builtin_amdgcn_perm(hi, lo, 0x07060302u); }
 
+// Two fp32 values as bf16, to the nearest even.
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{lo, hi}), bf16x2));
+}
+// Byte R of a word of scales as the scale, in one instruction.
+template <int R>
+__device__ __forceinline__ float byte_scale(uint32_t w) {
+  uint32_t s;
+  const uint32_t shift = 23;
+  if constexpr (R == 0)
+    asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_0" : "=v"(s) : "v"(shift), "v"(w));
+  else if constexpr (R == 1)
+    asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_1" : "=v"(s) : "v"(shift), "v"(w));
+  else if constexpr (R == 2)
+    asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_2" : "=v"(s) : "v"(shift), "v"(w));
+  else
+    asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_3" : "=v"(s) : "v"(shift), "v"(w));
+  return __uint_as_float(s);
+}
+
 template <typename T>
 __device__ __forceinline__ void store4(T* dst, const f32x4& v);
 template <>
 __device__ __forceinline__ void store4<float>(float* dst, const f32x4& v) { *reinterpret_cast<f32x4*>(dst) = v; }
 template <>
 __device__ __forceinline__ void store4<uint16_t>(uint16_t* dst, const f32x4& v) {
-  *reinterpret_cast<u2*>(dst) = u2{uint32_t(f32_to_bf16(v[0])) | (uint32_t(f32_to_bf16(v[1])) << 16),
-                                   uint32_t(f32_to_bf16(v[2])) | (uint32_t(f32_to_bf16(v[3])) << 16)};
+  *reinterpret_cast<u2*>(dst) = u2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
 }
 
 // A wave's ring in LDS, by format.
@@ -252,19 +272,13 @@ __global__ void __launch_bounds__(kBlock, 2)
       h_head = im.kv_head;
       h_out = im.out_idx;
       h_end = lane < n_items ? (h_ntok + kMxPage - 1) / kMxPage : 0;   // pages, then where they end
-#pragma unroll
-      for (int s = 1; s < 64; s *= 2) {
-        const int x = __shfl_up(h_end, s);
-        h_end += lane >= s ? x : 0;
-      }
+      h_end = wave_inclusive_sum(h_end);
     }
     const int pages = lane_of(h_end, 63);
     auto cut = [&](int w) { return (int)((int64_t)pages * w >> 2); };
     const int f0 = cut(wave), f1 = cut(wave + 1);
     auto begin_of = [&](int it) { return it > 0 ? lane_of(h_end, it - 1) : 0; };
     const int it0 = __builtin_ctzll(__ballot(h_end > f0) | (1ull << 63));   // the item of page f0
-    __syncthreads();   // every wave has the lengths; the last chunk's states have been read
-
     // the loads run ahead of the products, over all items
     int d_it = it0, d_page = f0 - begin_of(it0), d_left = f1 - f0;   // d_left: pages to request
     int d_np = lane_of(h_end, it0) - begin_of(it0);
@@ -278,11 +292,11 @@ __global__ void __launch_bounds__(kBlock, 2)
 #pragma unroll
       for (int k = 0; k < KP; ++k) d_id.v[k] = pt[d_first + min(d_page + k, last)];
     };
-    auto issue = [&](int slot) {   // one step, and on to the next
+    auto issue = [&](int to) {   // one step, and on to the next
 #pragma unroll
       for (int k = 0; k < KP; ++k) {
         const uint8_t* slab = d_slabs + (int64_t)d_id.v[k] * p.page_bytes;
-        const uint32_t dst = ring_lds + slot * S::kStage + k * S::kStagePage;
+        const uint32_t dst = ring_lds + to * S::kStage + k * S::kStagePage;
 #pragma unroll
         for (int j = 0; j < S::kFull; ++j) dma16(slab + j * 1024, lane * 16, dst + j * 1024);
         if constexpr (S::kWideRest) dma16(slab + S::kFull * 1024, min(lane * 16, S::kRest - 16), dst + S::kFull * 1024);
@@ -315,7 +329,7 @@ __global__ void __launch_bounds__(kBlock, 2)
       }
     };
 
-    int it = it0, done = 0;
+    int it = it0, slot = 0;   // slot: of the ring, of the step computed next
     float m = -INFINITY, l = 0.f;
     f32x4 acc[NV];
     if (f0 < f1) {
@@ -358,14 +372,14 @@ __global__ void __launch_bounds__(kBlock, 2)
 #pragma unroll
       for (int n = 0; n < NV; ++n) acc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-      for (int page = first_page; page < stop; page += KP, ++done) {
+      for (int page = first_page; page < stop; page += KP, slot = slot + 1 < R ? slot + 1 : 0) {
         if (d_left > 0) {   // R - 1 steps stay in flight
-          issue((done + R - 1) % R);
+          issue(slot > 0 ? slot - 1 : R - 1);
           wait_vmcnt<S::kDma * (R - 1)>();
         } else {
           wait_vmcnt<0>();
         }
-        uint8_t* const stage = ring + done % R * S::kStage;
+        uint8_t* const stage = ring + slot * S::kStage;
         const int left = min(ntok - page * kMxPage, (stop - page) * kMxPage);   // tokens from the step's first on
 
         // the new token, the item's last entry: quantised into its place in the pool, and in the stage
@@ -393,57 +407,63 @@ __global__ void __launch_bounds__(kBlock, 2)
           __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
         }
 
-        float sv[4 * KP];
+        // every read of the step goes out before its first product
+        uint32_t kc[KP][KW], vc[KP][VW], vw[KP];
+        float ks[KP];
 #pragma unroll
         for (int k = 0; k < KP; ++k) {
           const uint8_t* slab = stage + k * S::kStagePage;
-          uint32_t kc[KW];
-          load_codes<KW>(slab, lane, kc);
-          const float ks = mx_scale(slab[at.k_scales + (D == 128 ? rb : rb >> 1) * kMxPage + col]);
-          f32x4 s = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int c = 0; c < NQ; ++c) {
-            const u4 a = {pair<KB>(kc, 4 * c, ks), pair<KB>(kc, 4 * c + 1, ks), pair<KB>(kc, 4 * c + 2, ks),
-                          pair<KB>(kc, 4 * c + 3, ks)};
-#pragma unroll
-            for (int part = 0; part < NPART; ++part) s = mfma(a, qv[part][c], s);
-          }
-#pragma unroll
-          for (int i = 0; i < 4; ++i) sv[4 * k + i] = s[i];
+          load_codes<KW>(slab, lane, kc[k]);
+          ks[k] = mx_scale(slab[at.k_scales + (D == 128 ? rb : rb >> 1) * kMxPage + col]);
         }
-        // V's operands: dims 2i and 2i + 1 of the lane's sixteenth, pairs of tokens
-        uint32_t vc[KP][VW], vw[KP];
-        float vs[KP][4];
-        auto load_v = [&] {
+#pragma unroll
+        for (int k = 0; k < KP; ++k) {
+          const uint8_t* slab = stage + k * S::kStagePage;
+          load_codes<VW>(slab + at.v_codes, lane, vc[k]);
+          vw[k] = *reinterpret_cast<const uint32_t*>(slab + at.v_scales + rb * (D / 8) + col / (512 / D) * 4);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        if (left < KP * kMxPage) {   // rows past the retained length may hold anything: codes 0, scale 1
 #pragma unroll
           for (int k = 0; k < KP; ++k) {
-            const uint8_t* slab = stage + k * S::kStagePage;
-            load_codes<VW>(slab + at.v_codes, lane, vc[k]);
-            vw[k] = *reinterpret_cast<const uint32_t*>(slab + at.v_scales + rb * (D / 8) + col / (512 / D) * 4);
-          }
-          if (left < KP * kMxPage) {   // rows past the retained length may hold anything: codes 0, scale 1
+            const int keep = min(max(left - k * kMxPage - 4 * rb, 0), 4);   // of the lane's 4 tokens
+            const uint32_t mask = keep == 4 ? ~0u : (1u << (8 * keep)) - 1u;
+            vw[k] = (vw[k] & mask) | (0x7f7f7f7fu & ~mask);
 #pragma unroll
-            for (int k = 0; k < KP; ++k) {
-              const int keep = min(max(left - k * kMxPage - 4 * rb, 0), 4);   // of the lane's 4 tokens
-              const uint32_t mask = keep == 4 ? ~0u : (1u << (8 * keep)) - 1u;
-              vw[k] = (vw[k] & mask) | (0x7f7f7f7fu & ~mask);
+            for (int r = 0; r < 4; ++r) {
+              const bool drop = r >= keep;
+              if constexpr (VW == 2) {
+                vc[k][r / 2] &= drop ? (r % 2 ? 0x0000ffffu : 0xffff0000u) : ~0u;
+              } else {
 #pragma unroll
-              for (int r = 0; r < 4; ++r) {
-                const bool drop = r >= keep;
-                if constexpr (VW == 2) {
-                  vc[k][r / 2] &= drop ? (r % 2 ? 0x0000ffffu : 0xffff0000u) : ~0u;
-                } else {
-#pragma unroll
-                  for (int w = 0; w < VW / 4; ++w) vc[k][r * (VW / 4) + w] = drop ? 0u : vc[k][r * (VW / 4) + w];
-                }
+                for (int w = 0; w < VW / 4; ++w) vc[k][r * (VW / 4) + w] = drop ? 0u : vc[k][r * (VW / 4) + w];
               }
             }
           }
+        }
+
+        f32x4 s[KP];
 #pragma unroll
-          for (int k = 0; k < KP; ++k)
+        for (int k = 0; k < KP; ++k) s[k] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int r = 0; r < 4; ++r) vs[k][r] = mx_scale((vw[k] >> (8 * r)) & 0xffu);
-        };
+        for (int c = 0; c < NQ; ++c)
+#pragma unroll
+          for (int k = 0; k < KP; ++k) {
+            const u4 a = {pair<KB>(kc[k], 4 * c, ks[k]), pair<KB>(kc[k], 4 * c + 1, ks[k]),
+                          pair<KB>(kc[k], 4 * c + 2, ks[k]), pair<KB>(kc[k], 4 * c + 3, ks[k])};
+#pragma unroll
+            for (int part = 0; part < NPART; ++part) s[k] = mfma(a, qv[part][c], s[k]);
+          }
+
+        // V's operands: dims 2i and 2i + 1 of the lane's sixteenth, pairs of tokens
+        float vs[KP][4];
+#pragma unroll
+        for (int k = 0; k < KP; ++k) {
+          vs[k][0] = byte_scale<0>(vw[k]);
+          vs[k][1] = byte_scale<1>(vw[k]);
+          vs[k][2] = byte_scale<2>(vw[k]);
+          vs[k][3] = byte_scale<3>(vw[k]);
+        }
         auto v_operands = [&](int i, uint32_t* a, uint32_t* b) {
 #pragma unroll
           for (int k = 0; k < KP; ++k) {
@@ -458,11 +478,16 @@ __global__ void __launch_bounds__(kBlock, 2)
         };
         uint32_t va[NV / 2][2 * KP], vb[NV / 2][2 * KP];
         if constexpr (kEarly) {
-          load_v();
 #pragma unroll
-          for (int i = 0; i < NV / 2; ++i) v_operands(i, va[i], vb[i]);
+          for (int i = 0; i < NV / 2; ++i) {
+            v_operands(i, va[i], vb[i]);
+#pragma unroll
+            for (int j = 0; j < 2 * KP; ++j) asm volatile("" : "+v"(va[i][j]), "+v"(vb[i][j]));   // here, not behind the branches
+          }
         }
-
+        float sv[4 * KP];
+#pragma unroll
+        for (int i = 0; i < 4 * KP; ++i) sv[i] = s[i / 4][i % 4];
         if (p.cap > 0.f) {
 #pragma unroll
           for (int i = 0; i < 4 * KP; ++i) sv[i] = p.cap * tanh_f32(sv[i] * p.scale);
@@ -486,7 +511,11 @@ __global__ void __launch_bounds__(kBlock, 2)
         }
         const float mref = m > -INFINITY ? m : 0.f;   // every score -inf so far: weights 0
 #pragma unroll
-        for (int i = 0; i < 4 * KP; ++i) sv[i] = fast_exp2((sv[i] - mref) * cs);
+        for (int i = 0; i < 4 * KP; ++i) {
+          // fp32: relative to m itself and not to a rounded m cs, as the states are weighted by m
+          if constexpr (NPART == 1) sv[i] = fast_exp2(fmaf(sv[i], cs, -mref * cs));
+          else sv[i] = fast_exp2((sv[i] - mref) * cs);
+        }
         float sum = (sv[0] + sv[1]) + (sv[2] + sv[3]);
         if constexpr (KP == 2) sum += (sv[4] + sv[5]) + (sv[6] + sv[7]);
         l += sum;
@@ -495,7 +524,7 @@ __global__ void __launch_bounds__(kBlock, 2)
         for (int i = 0; i < 2 * KP; ++i) {
           if constexpr (NPART == 1) {
             // bf16 outputs: P rounded to bf16, half a step of the output's own
-            pb[0][i] = uint32_t(f32_to_bf16(sv[2 * i])) | (uint32_t(f32_to_bf16(sv[2 * i + 1])) << 16);
+            pb[0][i] = pack_bf16(sv[2 * i], sv[2 * i + 1]);
           } else {
             uint32_t a[3], b[3];
             split3(sv[2 * i], a);
@@ -504,7 +533,6 @@ __global__ void __launch_bounds__(kBlock, 2)
             for (int s = 0; s < 3; ++s) pb[s][i] = join16(a[s], b[s]);
           }
         }
-        if constexpr (!kEarly) load_v();
 #pragma unroll
         for (int i = 0; i < NV / 2; ++i) {
           uint32_t a[2 * KP], b[2 * KP];
@@ -592,6 +620,7 @@ __global__ void __launch_bounds__(kBlock, 2)
       if (h_arow >= 0) p.live[(int64_t)h_b * p.live_stride + h_head] = h_arow + 1;
       if (h_arow == -2 && p.append_full) *p.append_full = 1;
     }
+    if (chunk + 64 < it_end) __syncthreads();   // the states have been read
   }
 
   if (p.timestamps && threadIdx.x == 0) {

@@ -81,6 +81,25 @@ __device__ __forceinline__ float rows_max(float x) {
   return swap32_max(x);
 }
 
+// DPP lane movement with zero fill (row_mask selects the 16-lane rows updated).
+template <int CTRL, int ROW_MASK>
+__device__ __forceinline__ int dpp_add_src(int x) {
+  return __builtin_amdgcn_update_dpp(0, x, CTRL, ROW_MASK, 0xF, true);
+}
+
+// Inclusive prefix sum over the 64 lanes of a wave: shifts by 1, 2, 4 and 8
+// inside each 16-lane row, then row 0's total into row 1 and row 2's into row
+// 3 (row_bcast:15), then rows 0-1's total into rows 2 and 3 (row_bcast:31).
+__device__ __forceinline__ int wave_inclusive_sum(int x) {
+  x += dpp_add_src<0x111, 0xF>(x);
+  x += dpp_add_src<0x112, 0xF>(x);
+  x += dpp_add_src<0x114, 0xF>(x);
+  x += dpp_add_src<0x118, 0xF>(x);
+  x += dpp_add_src<0x142, 0xA>(x);
+  x += dpp_add_src<0x143, 0xC>(x);
+  return x;
+}
+
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // tanh.  Up to 5/8 an odd polynomial fitted for the smallest relative error
