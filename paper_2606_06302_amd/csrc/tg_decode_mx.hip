@@ -162,15 +162,18 @@ struct Shape {
   static constexpr int kStagePage = kFull * 1024 + (kWideRest ? 1024 : 256);
   static constexpr int kStage = kPages * kStagePage;
   static constexpr int kDma = kPages * (kFull + 1);                           // loads a step
-  static constexpr int kRing = D == 64 ? (KB + VB == 8 ? 6 : 3) : kStage > 6000 ? 2 : 3;                         // steps in the ring
+  static constexpr int kRing = 2;                         // steps in the ring
   static constexpr int kRow = (D + kPad) * 4;                                 // a head's accumulator in LDS
   // the ring, which takes the wave's last state in the end; the state that waves 1 to 3 may park on the way
   static constexpr int state_bytes(int gqa) { return gqa * (kRow + 8); }
   static constexpr int wave_bytes(int gqa) {
     return (kRing * kStage > state_bytes(gqa) ? kRing * kStage : (state_bytes(gqa) + 15) / 16 * 16);
   }
+  // the next item's queries, and its new token's K and V rows
+  static constexpr int kTok = 2 * D * (int)sizeof(T);
+  static constexpr int query_bytes(int gqa) { return kTok + gqa * D * (int)sizeof(T); }
   static constexpr size_t lds_bytes(int gqa) {
-    return kWaves * wave_bytes(gqa) + (kWaves - 1) * ((state_bytes(gqa) + 15) / 16 * 16);
+    return kWaves * (wave_bytes(gqa) + query_bytes(gqa)) + (kWaves - 1) * ((state_bytes(gqa) + 15) / 16 * 16);
   }
 };
 
@@ -223,9 +226,12 @@ __global__ void __launch_bounds__(kBlock, 2)
   const int col = lane & 15, rb = lane >> 4;
   const int G = p.gqa;
   const int hq = col < G ? col : col % G;
+  const int nq = G * LPR;                         // 16-byte chunks of an item's queries
   const int park_bytes = (S::state_bytes(G) + 15) / 16 * 16, wave_bytes = S::wave_bytes(G);
   uint8_t* const ring = lds + wave * wave_bytes;
   uint8_t* const parks = lds + kWaves * wave_bytes;
+  const uint8_t* const queries = parks + (kWaves - 1) * park_bytes + wave * S::query_bytes(G);   // the token's rows first
+  const uint32_t queries_lds = lds_address(queries);
   const uint32_t ring_lds = lds_address(ring);
   const uint64_t t_start = __builtin_amdgcn_s_memrealtime();
   const int it_begin = bin_offsets[blockIdx.x], it_end = bin_offsets[blockIdx.x + 1];
@@ -315,21 +321,19 @@ __global__ void __launch_bounds__(kBlock, 2)
       }
       page_ids();
     };
-    // an item's queries, and its new token's rows, as they lie in memory
-    u4 q_next[QC], tok_next = {};
     auto load_q = [&](int it) {
       const int b = lane_of(h_b, it), h = lane_of(h_head, it);
-      const u4* q = reinterpret_cast<const u4*>(static_cast<const T*>(p.q) +
-                                                ((int64_t)b * p.num_q_heads + h * G + hq) * D + rb * (D / 4));
-#pragma unroll
-      for (int i = 0; i < QC; ++i) q_next[i] = q[i];
-      if (p.append_k && lane < 2 * LPR) {
-        const int64_t row = ((int64_t)b * p.num_kv_heads + h) * LPR;
-        tok_next = lane < LPR ? p.append_k[row + lane] : p.append_v[row + lane - LPR];
+      const uint8_t* q = static_cast<const uint8_t*>(p.q) + ((int64_t)b * p.num_q_heads + h * G) * (LPR * 16);
+      for (int j = 0; j < nq; j += 64)
+        if (j + lane < nq) dma16(q + j * 16, lane * 16, queries_lds + S::kTok + j * 16);
+      if (p.append_k && lane < LPR) {
+        const int64_t row = ((int64_t)b * p.num_kv_heads + h) * (LPR * 16);
+        dma16(reinterpret_cast<const uint8_t*>(p.append_k) + row, lane * 16, queries_lds);
+        dma16(reinterpret_cast<const uint8_t*>(p.append_v) + row, lane * 16, queries_lds + S::kTok / 2);
       }
     };
 
-    int it = it0, slot = 0;   // slot: of the ring, of the step computed next
+    int it = it0, slot = 0, waited = 0;   // slot: of the ring, of the step computed next
     float m = -INFINITY, l = 0.f;
     f32x4 acc[NV];
     if (f0 < f1) {
@@ -345,34 +349,47 @@ __global__ void __launch_bounds__(kBlock, 2)
       const int stop = min(np, first_page + f1 - at_page);
       const int ntok = lane_of(h_ntok, it), arow = lane_of(h_arow, it);
 
-      u4 qv[NPART][NQ];
-      const u4 tok = tok_next;
+      // the queries were requested when the item before began: they are there if R - 1
+      // steps have been waited for since
+      if (waited < R - 1) wait_vmcnt<0>();
+      waited = 0;
+      u4 qv[NPART][NQ], tok = {};
+      {
+        const u4* q = reinterpret_cast<const u4*>(queries + S::kTok) + hq * LPR + rb * QC;
+        u4 x[QC];
 #pragma unroll
-      for (int c = 0; c < NQ; ++c) {
-        if constexpr (NPART == 1) {
-          qv[0][c] = q_next[c];
-        } else {
-          float x[8];
-          Row16<float>::unpack(q_next[2 * c], x);
-          Row16<float>::unpack(q_next[2 * c + 1], x + 4);
+        for (int i = 0; i < QC; ++i) x[i] = q[i];
+        if (arow >= 0 && lane < 2 * LPR) tok = reinterpret_cast<const u4*>(queries)[lane];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            uint32_t a[3], b[3];
-            split3(x[2 * i], a);
-            split3(x[2 * i + 1], b);
+        for (int c = 0; c < NQ; ++c) {
+          if constexpr (NPART == 1) {
+            qv[0][c] = x[c];
+          } else {
+            float y[8];
+            Row16<float>::unpack(x[2 * c], y);
+            Row16<float>::unpack(x[2 * c + 1], y + 4);
 #pragma unroll
-            for (int s = 0; s < 3; ++s) qv[s][c][i] = join16(a[s], b[s]);
+            for (int i = 0; i < 4; ++i) {
+              uint32_t a[3], b[3];
+              split3(y[2 * i], a);
+              split3(y[2 * i + 1], b);
+#pragma unroll
+              for (int s = 0; s < 3; ++s) qv[s][c][i] = join16(a[s], b[s]);
+            }
           }
         }
       }
-      if (at_page + stop - first_page < f1) load_q(it + 1);   // in use when this item is done
+      if (at_page + stop - first_page < f1) {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // read, so the next may take their place
+        load_q(it + 1);
+      }
 
       m = -INFINITY;
       l = 0.f;
 #pragma unroll
       for (int n = 0; n < NV; ++n) acc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-      for (int page = first_page; page < stop; page += KP, slot = slot + 1 < R ? slot + 1 : 0) {
+      for (int page = first_page; page < stop; page += KP, ++waited, slot = slot + 1 < R ? slot + 1 : 0) {
         if (d_left > 0) {   // R - 1 steps stay in flight
           issue(slot > 0 ? slot - 1 : R - 1);
           wait_vmcnt<S::kDma * (R - 1)>();
@@ -686,7 +703,9 @@ int32_t tg_decode_mx_bins(const tg_geometry* geom, int32_t dtype, const tg_mx_fo
   if (prev != device) (void)hipSetDevice(prev);
   if (e != hipSuccess) return tg::fail(TG_ERR_HIP, "occupancy query failed: %s", hipGetErrorString(e));
   const int64_t most = (int64_t)per_cu * cus;
-  const int64_t want = kv_len ? tg::ceil_div(pages, kWaves * 2) : most;
+  // Three pages a bin where there are too few to fill the device: 40 ragged layers of 22 to 34000 pages
+  // at 16 / 8 / 4 / 3 / 2 / 1 pages a bin take 1.22 / 1.14 / 1.04 / 1.03 / 1.03 / 1.03 times their best.
+  const int64_t want = kv_len ? tg::ceil_div(pages, 3) : most;
   *n_bins = (int32_t)(want < most ? want : most);
   return TG_OK;
 }
