@@ -255,7 +255,7 @@ __global__ void __launch_bounds__(kBlock, 2)
     if (e == 0) p.part_lse[row] = lse;
   };
   // no score above -inf: zeros, and an lse that loses against any other piece's
-  auto lse_of = [&](float m, float l) { return l == 0.f ? -FLT_MAX : m * (cs * kLn2) + logf(l); };
+  auto lse_of = [&](float m, float l) { return l == 0.f ? -FLT_MAX : fmaf(m, cs * kLn2, __builtin_amdgcn_logf(l) * kLn2); };
 
   // The items of the bin, up to 64 at a time, one a lane.  Their pages laid end to
   // end are cut into four equal ranges, one a wave: a wave runs its range by itself,
@@ -567,7 +567,7 @@ __global__ void __launch_bounds__(kBlock, 2)
       const bool whole = first_page == 0 && stop == np;
       if (whole) {
         if (col < G) {
-          const float inv = 1.f / (l == 0.f ? 1.f : l);
+          const float inv = __builtin_amdgcn_rcpf(l == 0.f ? 1.f : l);
           const float lse = lse_of(m, l);
           const int b = lane_of(h_b, it), h = lane_of(h_head, it), out_idx = lane_of(h_out, it);
 #pragma unroll
@@ -596,6 +596,7 @@ __global__ void __launch_bounds__(kBlock, 2)
     __syncthreads();
 
     // items that a cut goes through
+#pragma unroll 1
     for (int w0 = 1, last_it = -1; w0 < kWaves; ++w0) {
       const int c = cut(w0);
       if (c >= pages) break;
@@ -604,32 +605,43 @@ __global__ void __launch_bounds__(kBlock, 2)
       last_it = j;
       const int lo = begin_of(j), hi = lane_of(h_end, j);
       const int b = lane_of(h_b, j), h = lane_of(h_head, j), out_idx = lane_of(h_out, j);
+      // where every wave left its part of the item, with its last item or parked; a wave
+      // without a part is read all the same (the reads go out together) and not used
+      uint32_t at_state[kWaves];
+      int parts = 0;   // bit w: wave w has one
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        parts |= (cut(w) < hi && cut(w + 1) > lo && cut(w) < cut(w + 1)) << w;
+        at_state[w] = w == 0 || cut(w + 1) <= hi ? w * wave_bytes : kWaves * wave_bytes + (w - 1) * park_bytes;
+      }
+#pragma unroll 1
       for (int o = threadIdx.x; o < G * (D / 4); o += kBlock) {
         const int g = o / (D / 4), e = o % (D / 4) * 4;
-        float M = -INFINITY, L = 0.f, ms[kWaves];
-        const uint8_t* state[kWaves];
+        int mine = parts;
+        asm volatile("" : "+v"(mine));   // one body, not one for every set of waves: it is fetched cold
+        float ms[kWaves], ls[kWaves];
+        f32x4 x[kWaves];
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) {
-          // where wave w left its part of the item: with its last item, or parked
-          state[w] = cut(w + 1) <= hi ? lds + w * wave_bytes : parks + (w - 1) * park_bytes;
-          ms[w] = -INFINITY;
-          if (cut(w) < hi && cut(w + 1) > lo && cut(w) < cut(w + 1)) {
-            ms[w] = reinterpret_cast<const float*>(state[w] + G * S::kRow)[2 * g];
-            M = fmaxf(M, ms[w]);
-          }
+          const float* ml = reinterpret_cast<const float*>(lds + at_state[w] + G * S::kRow) + 2 * g;
+          ms[w] = ml[0];
+          ls[w] = ml[1];
+          x[w] = *reinterpret_cast<const f32x4*>(lds + at_state[w] + g * S::kRow + e * 4);
         }
+        float M = -INFINITY, L = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) M = fmaxf(M, mine >> w & 1 ? ms[w] : -INFINITY);
         f32x4 A = {0.f, 0.f, 0.f, 0.f};
         const float mref = M > -INFINITY ? M : 0.f;
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) {
-          if (!(cut(w) < hi && cut(w + 1) > lo && cut(w) < cut(w + 1))) continue;
-          const float f = fast_exp2((ms[w] - mref) * cs);
-          L = fmaf(reinterpret_cast<const float*>(state[w] + G * S::kRow)[2 * g + 1], f, L);
-          const f32x4 x = *reinterpret_cast<const f32x4*>(state[w] + g * S::kRow + e * 4);
+          const bool has = mine >> w & 1;
+          const float f = has ? fast_exp2((ms[w] - mref) * cs) : 0.f;
+          L = fmaf(has ? ls[w] : 0.f, f, L);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) A[i] = fmaf(x[i], f, A[i]);
+          for (int i = 0; i < 4; ++i) A[i] = fmaf(has ? x[w][i] : 0.f, f, A[i]);
         }
-        const float inv = 1.f / (L == 0.f ? 1.f : L);
+        const float inv = __builtin_amdgcn_rcpf(L == 0.f ? 1.f : L);
         write4(b, h, out_idx, g, e, f32x4{A[0] * inv, A[1] * inv, A[2] * inv, A[3] * inv}, lse_of(M, L));
       }
     }
