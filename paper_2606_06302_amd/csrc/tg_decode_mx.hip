@@ -1,25 +1,43 @@
 // Ragged paged split-KV decode attention over a quantised cache (tg_decode_mx).
 //
-// The plans, work items, partials and merge are tg_decode's; a bin is run by a
-// workgroup, whose waves take the item's pages KP at a time in turn, each with an
-// online-softmax state of its own, merged through LDS at the item's end.
+// The plans, work items, partials and merge launch are tg_decode's; a bin is run by
+// a workgroup of four waves.  The pages of its items, laid end to end, are cut into
+// four equal ranges, and every wave runs its range by itself with an online softmax
+// of its own; the waves meet once, at the end, where the up to three items that a
+// cut goes through are joined through LDS.  What an item needs (page ids, lengths,
+// heads) is held a lane an item, so that no load stands between one item and the
+// next.
 //
-// The slab of a page (tg_mx.h) lies as the lanes of a wave take it, so a page is
-// four loads a lane straight into registers: K codes, V codes and a scale word of
-// each.  gfx950 turns two codes into two bf16 numbers with their power-of-two
+// Data movement.  A page's slab (tg_mx.h) goes as it lies into a stage of the
+// wave's ring in LDS with gfx950's global_load_lds (no registers, one wait counted
+// by hand); one step is in flight while the one before is computed.
+//
+// Arithmetic.  gfx950 turns two codes into two bf16 numbers with their power-of-two
 // scale in one full-rate instruction, exactly, and the products run on them with
 // the query heads of the KV head as the 16 columns (columns past G repeat a real
 // head and are never stored):
 //   * S^T[16 tok][16 heads] = K q^T, D/32 x v_mfma_f32_16x16x32_bf16.  The lanes
 //     of quarter j hold dims j D/4 .. of a row, so the k index runs through the
 //     dims in that order, in K and in q alike.
-//   * online softmax over the step's 16 KP tokens; the 4 lanes of a column are
-//     combined with the permlane swaps, and the maximum is raised only when a step
-//     exceeds it by more than 2^8 in weight.
-//   * O^T[16 dims][16 heads] += V^T P^T, D/16 products 32 tokens deep: tokens
-//     4j .. 4j + 3 of two pages for lane group j, which is where S^T leaves them.
-//     The V operand pairs tokens, its codes pair dims: one byte permute each.
+//   * online softmax over the step's tokens; the 4 lanes of a column are combined
+//     with the permlane swaps, and the maximum is raised only when a step exceeds
+//     it by more than 2^8 in weight.
+//   * O^T[16 dims][16 heads] += V^T P^T, D/16 products 32 (or 16) tokens deep:
+//     tokens 4j .. 4j + 3 of a page for lane group j, which is where S^T leaves
+//     them.  The codes pair dims, the operand pairs tokens: one byte permute each.
 // With fp32 queries, q and P go in as three bf16 parts that hold their 24 bits.
+//
+// Bound by memory where there is enough of it: 64 requests, 189971 pages of 8-bit
+// rows (802 MB) 131 us, 6.1 TB/s; 95142 pages of 4-bit rows (207 MB, much of it in
+// the last-level cache) 47 us.  A step of two 4-bit pages (4352 bytes) takes a SIMD
+// about 1400 cycles with two waves on it (190 vector instructions and 16 matrix
+// products each), 7.5 TB/s over the chip, so the compute is not far behind.  A call
+// has about 3.5 us of latency in it (bin, items, page ids, rows, result, one after
+// the other) and 4 for the merge launch: 32 requests of 8192 tokens (94 MB) 24 us.
+// Measured on the way there: two barriers an item and headers loaded item by item
+// 28 us, the waves' ranges 25.7, every read of a step ahead of its products 24.6;
+// a merge inside the launch (counters, device-scope stores) 2 to 5 us more than the
+// merge launch; 8 waves a workgroup and half the bins 27.
 #include <hip/hip_runtime.h>
 
 #include <cfloat>
@@ -45,8 +63,7 @@ struct MxDecodeParams {
   const void* q;
   uint8_t* pool;
   int64_t page_bytes;
-  int32_t slab_bytes;
-  int32_t num_q_heads, num_kv_heads, n_bins, gqa;
+  int32_t num_q_heads, num_kv_heads, gqa;
   void* out;
   float* lse;
   float* part_o;               // [num_partials][gqa][d]
@@ -151,30 +168,27 @@ __device__ __forceinline__ void store4<uint16_t>(uint16_t* dst, const f32x4& v) 
   *reinterpret_cast<u2*>(dst) = u2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
 }
 
-// A wave's ring in LDS, by format.
-template <typename T, int D, int KB, int VB>
+// A wave's ring in LDS, by format: two steps of two pages, of one where two would
+// take a CU's third workgroup (8-bit rows of 128 dims).
+template <int D, int KB, int VB>
 struct Shape {
-  static constexpr int kPages = KB + VB == 16 && D == 128 ? 1 : 2;            // pages of a step
+  static constexpr int kPages = KB + VB == 16 && D == 128 ? 1 : 2;   // of a step
   static constexpr int kSlab = mx_slab_bytes(D, KB, VB);
-  // a slab comes in whole kilobytes of 16 bytes a lane and a rest of 4 or 16 bytes a lane
+  // a slab comes in whole kilobytes of 16 bytes a lane and a rest of 4 or 16
   static constexpr int kFull = kSlab / 1024, kRest = kSlab % 1024;
   static constexpr bool kWideRest = kRest > 256;
-  static constexpr int kStagePage = kFull * 1024 + (kWideRest ? 1024 : 256);
-  static constexpr int kStage = kPages * kStagePage;
-  static constexpr int kDma = kPages * (kFull + 1);                           // loads a step
-  static constexpr int kRing = 2;                         // steps in the ring
-  static constexpr int kRow = (D + kPad) * 4;                                 // a head's accumulator in LDS
-  // the ring, which takes the wave's last state in the end; the state that waves 1 to 3 may park on the way
-  static constexpr int state_bytes(int gqa) { return gqa * (kRow + 8); }
-  static constexpr int wave_bytes(int gqa) {
-    return (kRing * kStage > state_bytes(gqa) ? kRing * kStage : (state_bytes(gqa) + 15) / 16 * 16);
+  static constexpr int kStage = kPages * kSlab;
+  static constexpr int kDma = kPages * (kFull + 1);                  // loads of a step
+  static constexpr int kRing = 2;                                    // steps
+  static constexpr int kRow = (D + kPad) * 4;                        // a head's accumulator in LDS
+  // A wave's state of an item that it shares: accumulators, then (m, l) of every
+  // head.  The last one takes the place of the ring; waves 1 to 3 may park one on
+  // the way.
+  __host__ __device__ static constexpr int state_bytes(int gqa) { return (gqa * (kRow + 8) + 15) / 16 * 16; }
+  __host__ __device__ static constexpr int wave_bytes(int gqa) {
+    return kRing * kStage > state_bytes(gqa) ? kRing * kStage : state_bytes(gqa);
   }
-  // the next item's queries, and its new token's K and V rows
-  static constexpr int kTok = 2 * D * (int)sizeof(T);
-  static constexpr int query_bytes(int gqa) { return kTok + gqa * D * (int)sizeof(T); }
-  static constexpr size_t lds_bytes(int gqa) {
-    return kWaves * (wave_bytes(gqa) + query_bytes(gqa)) + (kWaves - 1) * ((state_bytes(gqa) + 15) / 16 * 16);
-  }
+  static constexpr size_t lds_bytes(int gqa) { return kWaves * wave_bytes(gqa) + (kWaves - 1) * state_bytes(gqa); }
 };
 
 // 16 or 4 bytes a lane from base + offset into LDS at lds + 16 (4) * lane, past the
@@ -200,10 +214,10 @@ __device__ __forceinline__ int64_t lane_of64(int64_t x, int j) {
 }
 
 template <typename T, int D, int KB, int VB>
-__global__ void __launch_bounds__(kBlock, 2)
+__global__ void __launch_bounds__(kBlock, sizeof(T) == 2 && !(D == 128 && KB == 4 && VB == 8) ? 3 : 2)
     tg_decode_mx_kernel(MxDecodeParams p, const tg_work_item* __restrict__ items_g, const int32_t* __restrict__ pt_g,
                         const int32_t* __restrict__ bin_offsets_g) {
-  using S = Shape<T, D, KB, VB>;
+  using S = Shape<D, KB, VB>;
   constexpr int E = Row16<T>::kElems;
   constexpr int NPART = sizeof(T) == 4 ? 3 : 1;   // bf16 parts of q and P
   constexpr int KP = S::kPages;
@@ -226,12 +240,9 @@ __global__ void __launch_bounds__(kBlock, 2)
   const int col = lane & 15, rb = lane >> 4;
   const int G = p.gqa;
   const int hq = col < G ? col : col % G;
-  const int nq = G * LPR;                         // 16-byte chunks of an item's queries
-  const int park_bytes = (S::state_bytes(G) + 15) / 16 * 16, wave_bytes = S::wave_bytes(G);
+  const int park_bytes = S::state_bytes(G), wave_bytes = S::wave_bytes(G);
   uint8_t* const ring = lds + wave * wave_bytes;
   uint8_t* const parks = lds + kWaves * wave_bytes;
-  const uint8_t* const queries = parks + (kWaves - 1) * park_bytes + wave * S::query_bytes(G);   // the token's rows first
-  const uint32_t queries_lds = lds_address(queries);
   const uint32_t ring_lds = lds_address(ring);
   const uint64_t t_start = __builtin_amdgcn_s_memrealtime();
   const int it_begin = bin_offsets[blockIdx.x], it_end = bin_offsets[blockIdx.x + 1];
@@ -241,7 +252,7 @@ __global__ void __launch_bounds__(kBlock, 2)
   }
   const float cs = p.cap > 0.f ? kLog2e : p.scale * kLog2e;   // log2 units per unit of (capped) score
 
-  // the result of a head's dims c4 .. of an item: out, or this piece's partial
+  // four dims of a head's result of an item: the output, or this piece's partial
   auto write4 = [&](int b, int h, int out_idx, int g, int e, const f32x4& O, float lse) {
     if (out_idx < 0) {
       const int64_t row = (int64_t)b * p.num_q_heads + h * G + g;
@@ -257,9 +268,7 @@ __global__ void __launch_bounds__(kBlock, 2)
   // no score above -inf: zeros, and an lse that loses against any other piece's
   auto lse_of = [&](float m, float l) { return l == 0.f ? -FLT_MAX : fmaf(m, cs * kLn2, __builtin_amdgcn_logf(l) * kLn2); };
 
-  // The items of the bin, up to 64 at a time, one a lane.  Their pages laid end to
-  // end are cut into four equal ranges, one a wave: a wave runs its range by itself,
-  // and only an item that a cut goes through takes more than one of them.
+  // the items of the bin, up to 64 at a time, one a lane
   for (int chunk = it_begin; chunk < it_end; chunk += 64) {
     const int n_items = min(64, it_end - chunk);
     int64_t h_first;         // of the item's page ids
@@ -285,6 +294,7 @@ __global__ void __launch_bounds__(kBlock, 2)
     const int f0 = cut(wave), f1 = cut(wave + 1);
     auto begin_of = [&](int it) { return it > 0 ? lane_of(h_end, it - 1) : 0; };
     const int it0 = __builtin_ctzll(__ballot(h_end > f0) | (1ull << 63));   // the item of page f0
+
     // the loads run ahead of the products, over all items
     int d_it = it0, d_page = f0 - begin_of(it0), d_left = f1 - f0;   // d_left: pages to request
     int d_np = lane_of(h_end, it0) - begin_of(it0);
@@ -302,11 +312,14 @@ __global__ void __launch_bounds__(kBlock, 2)
 #pragma unroll
       for (int k = 0; k < KP; ++k) {
         const uint8_t* slab = d_slabs + (int64_t)d_id.v[k] * p.page_bytes;
-        const uint32_t dst = ring_lds + to * S::kStage + k * S::kStagePage;
+        const uint32_t dst = ring_lds + to * S::kStage + k * S::kSlab;
 #pragma unroll
         for (int j = 0; j < S::kFull; ++j) dma16(slab + j * 1024, lane * 16, dst + j * 1024);
-        if constexpr (S::kWideRest) dma16(slab + S::kFull * 1024, min(lane * 16, S::kRest - 16), dst + S::kFull * 1024);
-        else dma4(slab + S::kFull * 1024, min(lane * 4, S::kRest - 4), dst + S::kFull * 1024);
+        if constexpr (S::kWideRest) {
+          if (lane < S::kRest / 16) dma16(slab + S::kFull * 1024, lane * 16, dst + S::kFull * 1024);
+        } else {
+          if (lane < S::kRest / 4) dma4(slab + S::kFull * 1024, lane * 4, dst + S::kFull * 1024);
+        }
       }
       const int took = min(KP, min(d_np - d_page, d_left));
       d_page += took;
@@ -321,23 +334,10 @@ __global__ void __launch_bounds__(kBlock, 2)
       }
       page_ids();
     };
-    auto load_q = [&](int it) {
-      const int b = lane_of(h_b, it), h = lane_of(h_head, it);
-      const uint8_t* q = static_cast<const uint8_t*>(p.q) + ((int64_t)b * p.num_q_heads + h * G) * (LPR * 16);
-      for (int j = 0; j < nq; j += 64)
-        if (j + lane < nq) dma16(q + j * 16, lane * 16, queries_lds + S::kTok + j * 16);
-      if (p.append_k && lane < LPR) {
-        const int64_t row = ((int64_t)b * p.num_kv_heads + h) * (LPR * 16);
-        dma16(reinterpret_cast<const uint8_t*>(p.append_k) + row, lane * 16, queries_lds);
-        dma16(reinterpret_cast<const uint8_t*>(p.append_v) + row, lane * 16, queries_lds + S::kTok / 2);
-      }
-    };
-
-    int it = it0, slot = 0, waited = 0;   // slot: of the ring, of the step computed next
+    int it = it0, slot = 0;   // slot: of the ring, of the step computed next
     float m = -INFINITY, l = 0.f;
     f32x4 acc[NV];
     if (f0 < f1) {
-      load_q(it0);
       page_ids();
 #pragma unroll
       for (int r = 0; r < R - 1; ++r)
@@ -349,17 +349,19 @@ __global__ void __launch_bounds__(kBlock, 2)
       const int stop = min(np, first_page + f1 - at_page);
       const int ntok = lane_of(h_ntok, it), arow = lane_of(h_arow, it);
 
-      // the queries were requested when the item before began: they are there if R - 1
-      // steps have been waited for since
-      if (waited < R - 1) wait_vmcnt<0>();
-      waited = 0;
+      // waiting for the queries waits for the step in flight too, which is needed next
+      // (queries fetched an item ahead, through LDS, took the same time)
       u4 qv[NPART][NQ], tok = {};
       {
-        const u4* q = reinterpret_cast<const u4*>(queries + S::kTok) + hq * LPR + rb * QC;
+        const int b = lane_of(h_b, it), h = lane_of(h_head, it);
+        const u4* q = static_cast<const u4*>(p.q) + ((int64_t)b * p.num_q_heads + h * G + hq) * LPR + rb * QC;
         u4 x[QC];
 #pragma unroll
         for (int i = 0; i < QC; ++i) x[i] = q[i];
-        if (arow >= 0 && lane < 2 * LPR) tok = reinterpret_cast<const u4*>(queries)[lane];
+        if (arow >= 0 && lane < 2 * LPR) {
+          const int64_t row = ((int64_t)b * p.num_kv_heads + h) * LPR;
+          tok = lane < LPR ? p.append_k[row + lane] : p.append_v[row + lane - LPR];
+        }
 #pragma unroll
         for (int c = 0; c < NQ; ++c) {
           if constexpr (NPART == 1) {
@@ -379,17 +381,12 @@ __global__ void __launch_bounds__(kBlock, 2)
           }
         }
       }
-      if (at_page + stop - first_page < f1) {
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // read, so the next may take their place
-        load_q(it + 1);
-      }
-
       m = -INFINITY;
       l = 0.f;
 #pragma unroll
       for (int n = 0; n < NV; ++n) acc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-      for (int page = first_page; page < stop; page += KP, ++waited, slot = slot + 1 < R ? slot + 1 : 0) {
+      for (int page = first_page; page < stop; page += KP, slot = slot + 1 < R ? slot + 1 : 0) {
         if (d_left > 0) {   // R - 1 steps stay in flight
           issue(slot > 0 ? slot - 1 : R - 1);
           wait_vmcnt<S::kDma * (R - 1)>();
@@ -408,7 +405,7 @@ __global__ void __launch_bounds__(kBlock, 2)
             const bool is_v = lane >= LPR;
             const int e = lane % LPR * E;
             uint32_t scale;
-            uint8_t* const mine = stage + k * S::kStagePage;
+            uint8_t* const mine = stage + k * S::kSlab;
             if (is_v) {
               const u2 c = mx_quantise<T>(tok, VB, &scale);
               mx_store<E>(slab + at.v_codes, slab + at.v_scales, t, e, D, VB, true, c, scale);
@@ -429,13 +426,13 @@ __global__ void __launch_bounds__(kBlock, 2)
         float ks[KP];
 #pragma unroll
         for (int k = 0; k < KP; ++k) {
-          const uint8_t* slab = stage + k * S::kStagePage;
+          const uint8_t* slab = stage + k * S::kSlab;
           load_codes<KW>(slab, lane, kc[k]);
           ks[k] = mx_scale(slab[at.k_scales + (D == 128 ? rb : rb >> 1) * kMxPage + col]);
         }
 #pragma unroll
         for (int k = 0; k < KP; ++k) {
-          const uint8_t* slab = stage + k * S::kStagePage;
+          const uint8_t* slab = stage + k * S::kSlab;
           load_codes<VW>(slab + at.v_codes, lane, vc[k]);
           vw[k] = *reinterpret_cast<const uint32_t*>(slab + at.v_scales + rb * (D / 8) + col / (512 / D) * 4);
         }
@@ -578,7 +575,8 @@ __global__ void __launch_bounds__(kBlock, 2)
                      f32x4{acc[n][r] * inv, acc[n + 1][r] * inv, acc[n + 2][r] * inv, acc[n + 3][r] * inv}, lse);
         }
       } else if (col < G) {
-        // a shared item's state: parked if the wave goes on, else where its ring was (no load is in flight then)
+        // a shared item's state: parked if the wave goes on (its first item then, so it is
+        // not wave 0), else where its ring was (no load is in flight then)
         uint8_t* state = at_page < f1 ? parks + (wave - 1) * park_bytes : ring;
         float* dst = reinterpret_cast<float*>(state) + col * (D + kPad) + rb * (D / 4);
 #pragma unroll
@@ -667,7 +665,7 @@ struct Picked {
 
 template <typename T, int D, int KB, int VB>
 Picked picked(int gqa) {
-  return {&tg_decode_mx_kernel<T, D, KB, VB>, Shape<T, D, KB, VB>::lds_bytes(gqa)};
+  return {&tg_decode_mx_kernel<T, D, KB, VB>, Shape<D, KB, VB>::lds_bytes(gqa)};
 }
 
 template <typename T, int D>
@@ -714,11 +712,15 @@ int32_t tg_decode_mx_bins(const tg_geometry* geom, int32_t dtype, const tg_mx_fo
       hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, reinterpret_cast<const void*>(k.fn), kBlock, k.lds);
   if (prev != device) (void)hipSetDevice(prev);
   if (e != hipSuccess) return tg::fail(TG_ERR_HIP, "occupancy query failed: %s", hipGetErrorString(e));
-  const int64_t most = (int64_t)per_cu * cus;
-  // Three pages a bin where there are too few to fill the device: 40 ragged layers of 22 to 34000 pages
-  // at 16 / 8 / 4 / 3 / 2 / 1 pages a bin take 1.22 / 1.14 / 1.04 / 1.03 / 1.03 / 1.03 times their best.
-  const int64_t want = kv_len ? tg::ceil_div(pages, 3) : most;
-  *n_bins = (int32_t)(want < most ? want : most);
+  // Two workgroups a CU, of three pages a bin at least: 40 ragged layers of 22 to 34000 pages at 16 / 8 / 4 / 3
+  // / 2 / 1 pages a bin take 1.20 / 1.13 / 1.05 / 1.03 / 1.04 / 1.04 times their best.  Three a CU for much
+  // work, where they fit together (95142 pages in 4 bits 47.4 us against 53.9, 25774 in 8 bits 26.4 against 29.6,
+  // 10713 in 4 bits 16.4 against 14.9) or, with more of it, one after another (85208 pages with 8-bit keys 53.9
+  // against 59.1, 45885 39.8 against 38.4); more than that is behind everywhere.
+  const int64_t three = 3 * (int64_t)cus, two = (per_cu < 2 ? per_cu : 2) * (int64_t)cus;
+  const bool many = kv_len && pages >= (per_cu >= 3 ? 32 : 96) * three;
+  const int64_t few = kv_len ? tg::ceil_div(pages, 3) : two;
+  *n_bins = (int32_t)(many ? three : few < two ? few : two);
   return TG_OK;
 }
 
@@ -737,11 +739,9 @@ int32_t tg_decode_mx(const tg_decode_args* a, const tg_mx_format* format, float 
   MxDecodeParams p;
   p.q = a->q;
   p.pool = static_cast<uint8_t*>(a->kv_pool);
-  p.slab_bytes = mx_slab_bytes(d, tg::mx_bits(format->k_format), tg::mx_bits(format->v_format));
-  p.page_bytes = (int64_t)g.heads_per_group * p.slab_bytes;
+  p.page_bytes = (int64_t)tg_mx_page_bytes(&g, format);
   p.num_q_heads = g.num_q_heads;
   p.num_kv_heads = g.num_kv_heads;
-  p.n_bins = a->n_bins;
   p.gqa = gqa;
   p.out = a->out;
   p.lse = a->lse;
