@@ -977,9 +977,9 @@ typedef struct {
 
 int32_t tg_unpack_mx(const tg_unpack_mx_args* args, void* hip_stream);
 
-/* 13d. Bins that a plan for these lengths should have (host): as many workgroups
- * as the kernel runs at once on `device`, fewer where the layer's pages are too few
- * to share.  kv_len [B][L][H] (host), with batch and layer; NULL: the most.
+/* 13d. Bins that a plan for these lengths should have (host): two workgroups a CU
+ * of `device`, fewer where the layer's pages are too few to share, three for very
+ * much work.  kv_len [B][L][H] (host), with batch and layer; NULL: two a CU.
  * n_bins out.  Errors: TG_ERR_INVALID_ARG, TG_ERR_UNSUPPORTED, TG_ERR_HIP. */
 int32_t tg_decode_mx_bins(const tg_geometry* geom, int32_t dtype, const tg_mx_format* format, int32_t device,
                           int32_t batch, int32_t layer, const int32_t* kv_len, int32_t* n_bins);
@@ -990,8 +990,8 @@ int32_t tg_decode_mx_bins(const tg_geometry* geom, int32_t dtype, const tg_mx_fo
  * cap as tg_decode_capped's.  sm_scale must be finite and >= 0.
  *   append_k, append_v: the token is quantised into its entry first and attended to
  *     as stored: one call gives what tg_append_mx and tg_decode_mx give, bit for bit.
- *   merge_counters: any dtype and head_dim; the results are the same without, bit
- *     for bit.
+ *   merge_counters: not used; the partials of split units are always joined by a
+ *     launch of their own.
  * Scores that overflow to -inf have no weight; a head with no other scores gives
  * zeros and an lse of -FLT_MAX.
  * Supported: dtype TG_F32 or TG_BF16, gqa 1..16. */

@@ -713,12 +713,12 @@ int32_t tg_decode_mx_bins(const tg_geometry* geom, int32_t dtype, const tg_mx_fo
   if (prev != device) (void)hipSetDevice(prev);
   if (e != hipSuccess) return tg::fail(TG_ERR_HIP, "occupancy query failed: %s", hipGetErrorString(e));
   // Two workgroups a CU, of three pages a bin at least: 40 ragged layers of 22 to 34000 pages at 16 / 8 / 4 / 3
-  // / 2 / 1 pages a bin take 1.20 / 1.13 / 1.05 / 1.03 / 1.04 / 1.04 times their best.  Three a CU for much
-  // work, where they fit together (95142 pages in 4 bits 47.4 us against 53.9, 25774 in 8 bits 26.4 against 29.6,
-  // 10713 in 4 bits 16.4 against 14.9) or, with more of it, one after another (85208 pages with 8-bit keys 53.9
-  // against 59.1, 45885 39.8 against 38.4); more than that is behind everywhere.
+  // / 2 / 1 pages a bin take 1.20 / 1.13 / 1.05 / 1.03 / 1.04 / 1.04 times their best.  Three a CU, where they fit
+  // together, for 80 pages a bin and more (32 requests of 8 heads, 768 bins against 512: 59069 pages in 4 bits 32.4
+  // us against 31.3, 65595 32.7 against 35.1, 88759 38.3 against 40.1; in 8 bits 47.6 against 47.3, 50.7 against
+  // 52.3, 64.2 against 66.8); more than that is behind everywhere.
   const int64_t three = 3 * (int64_t)cus, two = (per_cu < 2 ? per_cu : 2) * (int64_t)cus;
-  const bool many = kv_len && pages >= (per_cu >= 3 ? 32 : 96) * three;
+  const bool many = kv_len && per_cu >= 3 && pages >= 80 * three;
   const int64_t few = kv_len ? tg::ceil_div(pages, 3) : two;
   *n_bins = (int32_t)(many ? three : few < two ? few : two);
   return TG_OK;

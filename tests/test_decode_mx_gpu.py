@@ -44,7 +44,7 @@ def test_decode(bits, dtype, d, gqa):
 @pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f32", 64), ("bf16", 64), ("f32", 128)])
 @pytest.mark.parametrize("bins", [1, 7, 64, 1024])
 def test_partitions_and_merges(dtype, d, bins):
-    """Any number of bins, and the in-launch merge bit for bit as the merge launch."""
+    """Any number of bins; arrival counters change nothing."""
     c = Cache([40, 700, 2500, 3], H=2, gqa=3, d=d, Hp=1, bits=(8, 4), seed=bins)
     q = queries(c, dtype)
     out, lse, plan = c.decode(q, dtype, bins=bins)
