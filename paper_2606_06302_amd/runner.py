@@ -111,20 +111,43 @@ class DeviceTables:
         return out
 
 
+def random_mx_pool(geom, fmt, pages, device="cuda", seed=0):
+    """A quantised pool of random rows: normal-sized values with evenly spread codes, no NaN among them."""
+    gen = torch.Generator(device=device).manual_seed(seed)
+    bits = [4 if f == tg.TG_MX_FP4 else 8 for f in (fmt.k_format, fmt.v_format)]
+    d, P, slab = geom.head_dim, geom.page_size, tg.tg_mx_page_bytes(geom, fmt) // geom.heads_per_group
+    pool = torch.randint(0, 256, (pages * geom.heads_per_group, slab), generator=gen, dtype=torch.uint8, device=device)
+    at = 0
+    for b in bits:
+        if b == 8:      # the lowest exponent bit cleared: no code of NaN
+            pool[:, at:at + P * d].bitwise_and_(0xf7)
+        at += P * d * b // 8
+    for i, b in enumerate(bits):
+        lo = at + i * P * d // 32
+        pool[:, lo:lo + P * d // 32] = 125 if b == 4 else 119
+    return pool.view(pages, geom.heads_per_group, slab)
+
+
 class DecodeSession:
     """Pool, queries, outputs and per-layer plans of one decode workload.  softcap not 0: the scores are capped
-    (tg_decode_capped)."""
+    (tg_decode_capped).  mx: the tg_mx_format of a quantised cache; the pool is then bytes ([pages][H_p][slab], random
+    rows where none is given), attended to with tg_decode_mx and appended to with tg_append_mx."""
 
     def __init__(self, wl, tables: Tables = None, mode=tg.TG_PLAN_AOT, n_bins=None, split_target=None,
                  fill="device", pool=None, q=None, want_lse=True, device="cuda", layers=None, open_end=False,
-                 fused_merge=False, softcap=0.0):
+                 fused_merge=False, softcap=0.0, mx=None):
         from workloads import S_POOL, S_Q, device_normal_, host_pool, host_q_decode, page_elems
         g = wl.geom
         self.wl, self.device = wl, device
         self.t = tables if tables is not None else Tables(wl, device=device)
         self.dtype = TORCH_DTYPE[wl.dtype]
         self.tg_dtype = TG_DTYPE[wl.dtype]
-        if n_bins is None:
+        self.mx = mx
+        if n_bins is None and mx is not None:     # one number for all layers: that of the longest
+            n_bins = max(tg.tg_decode_mx_bins(g, self.tg_dtype, mx, torch.device(device).index or 0, wl.batch, l,
+                                              self.t.kv_len)
+                         for l in (range(g.num_layers) if layers is None else layers))
+        elif n_bins is None:
             n_bins = tg.tg_decode_max_ctas(g, self.tg_dtype, torch.device(device).index or 0)
         if split_target is None:
             split_target = 2 * n_bins   # measured best on the 64-layer step (bins x {1,2,4,8})
@@ -141,13 +164,19 @@ class DecodeSession:
         # pool
         if pool is not None:
             self.pool = pool
+        elif mx is not None:
+            self.pool = random_mx_pool(g, mx, self.t.pool_pages, device)
         elif fill == "host":
             host = host_pool(wl, self.t.pool_pages)
             self.pool = torch.from_numpy(host).to(self.dtype).to(device)
         else:
             self.pool = torch.empty(self.t.pool_pages * page_elems(g), dtype=self.dtype, device=device)
             device_normal_(self.pool, wl, S_POOL, wl.kv_scale)
-        self.pool = self.pool.view(self.t.pool_pages, 2, g.heads_per_group, g.page_size, g.head_dim)
+        if mx is not None:
+            assert self.pool.dtype == torch.uint8 and self.pool.is_contiguous() and \
+                self.pool.numel() >= self.t.pool_pages * tg.tg_mx_page_bytes(g, mx), "a quantised pool is bytes, tg_mx_page_bytes a page"
+        else:
+            self.pool = self.pool.view(self.t.pool_pages, 2, g.heads_per_group, g.page_size, g.head_dim)
         if q is not None:
             self.q = q
         elif fill == "host":
@@ -200,6 +229,8 @@ class DecodeSession:
 
     def workers_per_wg(self):
         """Bins (workers) per workgroup of the decode kernel the library picks for this session."""
+        if self.mx is not None:
+            return 1
         return tg.tg_decode_bins_per_workgroup(self.wl.geom, self.tg_dtype, self.n_bins)
 
     def calibrate_xcd_weights(self, stream=None, classes=8, per_layer=False):
@@ -276,17 +307,27 @@ class DecodeSession:
             self.append_decode_args[l] = a
 
     def append_layer(self, l, stream=None):
-        tg.tg_append(self.append_args[l], stream)
+        if self.mx is not None:
+            tg.tg_append_mx(self.append_args[l], self.mx, stream)
+        else:
+            tg.tg_append(self.append_args[l], stream)
 
     def enable_projection(self, spec, rows, positions):
         """The step's queries, keys and values come as projection rows ([L][B][(Hq + 2H) * d], queries first, then keys,
         then values) with the tokens' positions [B] int32: run_projected_step normalises, rotates and stores them
-        (tg_rope_append into self.q and the cache), then attends."""
+        (tg_rope_append into self.q and the cache), then attends.  With a quantised cache they go through self.q,
+        self.k_tok and self.v_tok (tg_rope), and the attention stores them."""
         assert self.open_end, "appending needs open-ended plans and live lengths"
         g, B = self.wl.geom, self.wl.batch
         self.rows, self.positions, self.spec = rows, positions, spec
-        self._append_tables()
         q, k = g.num_q_heads * g.head_dim, g.num_kv_heads * g.head_dim
+        if self.mx is not None:
+            self.enable_append(fused=True)
+            self.rope_args = {l: tg.make_rope_args(g, B, 1, self.tg_dtype, spec, rows[l][:, :q], rows[l][:, q:q + k],
+                                                   rows[l][:, q + k:], self.q[l], self.k_tok[l], self.v_tok[l],
+                                                   positions=positions) for l in self.layers}
+            return
+        self._append_tables()
         self.rope_append_args = {l: tg.make_rope_append_args(
             g, B, l, self.tg_dtype, spec, rows[l][:, :q], rows[l][:, q:q + k], rows[l][:, q + k:], positions, self.q[l],
             self.pool, self.t.d_pt_pages, self.d_offsets, self.d_group_of, self.d_slot_of, self.live_len, self.full)
@@ -294,11 +335,17 @@ class DecodeSession:
 
     def run_projected_step(self, stream=None):
         for l in self.layers:
+            if self.mx is not None:
+                tg.tg_rope(self.rope_args[l], stream)
+                self._decode(self.append_decode_args[l], stream)
+                continue
             tg.tg_rope_append(self.rope_append_args[l], stream)
             self._decode(self.dplans[l].args, stream)
 
     def _decode(self, args, stream):
-        if self.softcap != 0:   # tg_decode_capped refuses what is no cap
+        if self.mx is not None:
+            tg.tg_decode_mx(args, self.mx, self.softcap, stream)
+        elif self.softcap != 0:   # tg_decode_capped refuses what is no cap
             tg.tg_decode_capped(args, self.softcap, stream)
         else:
             tg.tg_decode(args, stream)
@@ -309,7 +356,7 @@ class DecodeSession:
             if self.fused_append:
                 self._decode(self.append_decode_args[l], stream)
             else:
-                tg.tg_append(self.append_args[l], stream)
+                self.append_layer(l, stream)
                 self._decode(self.dplans[l].args, stream)
 
     def run_layer(self, l, stream=None):
@@ -414,10 +461,12 @@ class PrefillSession:
     launch (a uint8 tensor of at least tg_prefill_workspace_bytes, up to 60 MB), shared by sessions whose calls run
     one after another on a stream, as a model's layers do; the session allocates its own where none, or too small a
     one, is given.  mod: a tg_score_mod (make_score_mod) of capped scores, masks and short chunks, whose tensors the
-    caller keeps."""
+    caller keeps.  mx: the tg_mx_format of a quantised cache, mx_pool its pool; every run then reads the layer's history
+    back first (tg_unpack_mx) into pool, [layer_pages][2][H_p][P][d], which sessions that run one after another can share
+    (the session allocates its own where none is given)."""
 
     def __init__(self, wl, tables: Tables = None, layer=0, fill="device", pool=None, device="cuda", schedule=True,
-                 hist_len=None, workspace=None, mod=None):
+                 hist_len=None, workspace=None, mod=None, mx=None, mx_pool=None):
         from workloads import S_K, S_POOL, S_Q, S_V, device_normal_, host_pool, host_prefill_inputs, page_elems
         g = wl.geom
         assert wl.chunk_len >= 1, "prefill workloads need a chunk length"
@@ -428,6 +477,15 @@ class PrefillSession:
         self.hist = self.t.kv_len if hist_len is None else np.ascontiguousarray(hist_len, dtype=np.int32)
         self.dtype = TORCH_DTYPE[wl.dtype]
         B, C = wl.batch, wl.chunk_len
+        self.mx, self.mx_pool = mx, mx_pool
+        pages, pool_pages = self.t.d_pt_pages, self.t.pool_pages
+        if mx is not None:
+            assert mx_pool is not None, "a quantised history has a pool"
+            ids, pool_pages = self._layer_pages()
+            self.d_layer_pages = pages = to_device(ids, device)
+            if pool is None:
+                pool = torch.zeros(pool_pages * page_elems(g), dtype=self.dtype, device=device)
+            pool = pool.view(-1)[:pool_pages * page_elems(g)]
         if pool is not None:
             self.pool = pool
         elif fill == "host":
@@ -435,7 +493,7 @@ class PrefillSession:
         else:
             self.pool = torch.empty(self.t.pool_pages * page_elems(g), dtype=self.dtype, device=device)
             device_normal_(self.pool, wl, S_POOL, wl.kv_scale)
-        self.pool = self.pool.view(self.t.pool_pages, 2, g.heads_per_group, g.page_size, g.head_dim)
+        self.pool = self.pool.view(pool_pages, 2, g.heads_per_group, g.page_size, g.head_dim)
         if fill == "host":
             q, k, v = host_prefill_inputs(wl)
             self.q, self.k_new, self.v_new = (torch.from_numpy(x).to(self.dtype).to(device) for x in (q, k, v))
@@ -455,8 +513,12 @@ class PrefillSession:
         self.order = tg.tg_prefill_schedule(g, B, C, layer, self.hist) if schedule else None
         self.d_order = to_device(self.order, device) if schedule else None
         self.args = tg.make_prefill_args(g, B, C, layer, TG_DTYPE[wl.dtype], self.q, self.k_new, self.v_new,
-                                         self.pool, self.t.d_pt_pages, self.d_offsets, self.d_kv_len,
+                                         self.pool, pages, self.d_offsets, self.d_kv_len,
                                          self.d_group_of, self.d_slot_of, self.out, block_order=self.d_order)
+        if mx is not None:
+            self.unpack_args = tg.make_unpack_mx_args(g, B, layer, TG_DTYPE[wl.dtype], mx, mx_pool, self.t.d_pt_pages,
+                                                      self.d_offsets, self.d_group_of, self.d_slot_of, self.d_kv_len,
+                                                      self.pool, dst_pages=pages)
         # scheduled ahead of time: partials of the key-split launch where it pays
         pays = schedule and tg.tg_prefill_split_pays(g, B, C, layer, self.hist)
         ws_bytes = tg.tg_prefill_workspace_bytes(self.args) if pays else 0
@@ -466,7 +528,20 @@ class PrefillSession:
             self.workspace = workspace if fits else torch.empty(ws_bytes, dtype=torch.uint8, device=device)
             self.args.workspace, self.args.workspace_bytes = self.workspace.data_ptr(), ws_bytes
 
+    def _layer_pages(self):
+        """A page array whose ids of the layer's tables count up from 0, and how many there are."""
+        g, off = self.wl.geom, self.t.pt_offsets
+        G = g.num_kv_heads // g.heads_per_group
+        ids, n = np.zeros(len(self.t.pt_pages), np.int32), 0
+        for b in range(self.wl.batch):
+            lo, hi = (int(off[(b * g.num_layers + self.layer) * G + i]) for i in (0, G))
+            ids[lo:hi] = np.arange(n, n + hi - lo)
+            n += hi - lo
+        return ids, max(1, n)
+
     def run(self, stream=None):
+        if self.mx is not None:
+            tg.tg_unpack_mx(self.unpack_args, stream)
         if self.mod is not None:
             tg.tg_prefill_mod(self.args, self.mod, stream)
         else:
@@ -498,15 +573,16 @@ class CompressSession:
     chunk_len rows are valid.  k_new, v_new [B][C][H][d] and scores [B][H][C]
     are device tensors (drawn from the workload's seeded streams when None).
     The counts and work items come from tg_compress_plan (host, before the
-    step); run() enqueues tg_compress."""
+    step); run() enqueues tg_compress, or with mx, the tg_mx_format of a
+    quantised pool, tg_compress_mx."""
 
     def __init__(self, wl, tables: Tables, pool, chunk_start, chunk_tokens, layer=0, sel_ratio="reserved",
-                 rows_per_item=32, k_new=None, v_new=None, scores=None, device="cuda"):
+                 rows_per_item=32, k_new=None, v_new=None, scores=None, device="cuda", mx=None):
         from workloads import S_K, S_V, device_normal_, host_scores
         g = wl.geom
         B, C, H = wl.batch, wl.chunk_len, g.num_kv_heads
         self.wl, self.t, self.layer, self.device = wl, tables, layer, device
-        self.pool = pool
+        self.pool, self.mx = pool, mx
         self.dtype = TORCH_DTYPE[wl.dtype]
         self.chunk_start = np.asarray(chunk_start, dtype=np.int32)
         self.chunk_tokens = np.asarray(chunk_tokens, dtype=np.int32)
@@ -533,14 +609,18 @@ class CompressSession:
                                           self.d_chunk_tokens, self.d_keep_count, self.kept)
 
     def run(self, stream=None):
-        tg.tg_compress(self.args, stream)
+        if self.mx is not None:
+            tg.tg_compress_mx(self.args, self.mx, stream)
+        else:
+            tg.tg_compress(self.args, stream)
 
     def traffic_bytes(self) -> int:
         """Algorithmic HBM bytes of one call: the kept K and V rows read from the chunk and
         written to the pages, the valid scores read once, and the kept indices written once
         (and read back by the copy)."""
         g = self.wl.geom
-        esz = 4 if self.wl.dtype == "f32" else 2
+        row = 2 * g.head_dim * (4 if self.wl.dtype == "f32" else 2)
+        stored = row if self.mx is None else tg.tg_mx_page_bytes(g, self.mx) // (g.heads_per_group * g.page_size)
         kept = int(self.plan["keep_count"].sum())
         scores = int(self.chunk_tokens.astype(np.int64).sum()) * g.num_kv_heads * 4
-        return kept * 2 * g.head_dim * esz * 2 + scores + kept * 4 * 2
+        return kept * (row + stored) + scores + kept * 4 * 2

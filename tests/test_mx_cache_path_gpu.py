@@ -1,0 +1,239 @@
+"""The calls around a quantised cache together, as a served layer uses them: chunks attended to over the read-back history,
+compressed into the cache, then decode steps that store their own token; and the sessions that make these calls.  Every
+stage against a 64-bit form of its own inputs, the stored bytes against the reference's."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from gpu_helpers import say
+from workloads import Geometry, custom
+
+pytestmark = pytest.mark.gpu
+
+if torch.cuda.is_available():
+    from mx_helpers import DTYPE, Cache, TG, check_decode, f64, fmt
+    from oracle import mx
+    from paper_2606_06302_amd import tangram as tg
+    from paper_2606_06302_amd.device import to_device
+    from paper_2606_06302_amd.runner import CompressSession, DecodeSession, PrefillSession, Tables
+    from test_projection_to_cache_gpu import rotated
+    from test_score_mod_gpu import attend
+
+
+@pytest.fixture(autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+
+
+class Bytes:
+    """The reference's copy of a pool under a session's tables."""
+
+    def __init__(self, tables, geom, bits, host):
+        self.t, self.g, self.places, self.host = tables, geom, mx.Places(geom.head_dim, *bits), host
+
+    def slabs(self, b, l, h, n):
+        G = self.g.num_kv_heads // self.g.heads_per_group
+        lo = int(self.t.pt_offsets[(b * self.g.num_layers + l) * G + self.t.group_of[l, h]])
+        return self.t.pt_pages[lo:lo + (n + 15) // 16], int(self.t.slot_of[l, h])
+
+    def rows(self, b, l, h, n):
+        page, slot = self.slabs(b, l, h, n)
+        return [x[:n] for x in self.places.rows(self.host[page, slot])]
+
+    def store(self, b, l, h, entry, k, v):
+        page, slot = self.slabs(b, l, h, entry + 1)
+        self.places.store(self.host[page[-1], slot], entry % 16, k, v)
+
+
+@pytest.mark.parametrize("d,gqa,bits", [(128, 4, (4, 4)), (64, 5, (8, 4)), (128, 1, (8, 8)), (64, 2, (4, 8))])
+def test_chunks_to_decode_steps(d, gqa, bits):
+    """Tolerances: out is off by half a step of bf16, 2^-8, and by what its weights are off by times sum p |v|: their own
+    half step, 2^-8, and 1e-3 for the fp32 work."""
+    H, Hp, B, C, L, steps = 4, 2, 3, 48, 2, 4
+    g = Geometry(L, H, H * gqa, d, 16, Hp)
+    tokens = np.array([[48, 31, 48], [48, 1, 20], [7, 48, 48]])
+    wl = custom(91 + d, g, B, "bf16", tokens.sum(0).astype(np.int32), chunk_len=C)
+    t = Tables(wl, headroom=np.full(B, steps, np.int32))
+    fm = fmt(bits)
+    per = tg.tg_mx_page_bytes(g, fm)
+    pool = torch.full((t.pool_pages, Hp, per // Hp), 255, dtype=torch.uint8, device="cuda")
+    ref = Bytes(t, g, bits, pool.cpu().numpy())
+    scratch = torch.full((t.pool_pages * 2 * Hp * 16 * d,), float("nan"), dtype=torch.bfloat16, device="cuda")
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    randn = lambda *s: torch.randn(*s, generator=gen, device="cuda").bfloat16()
+    scale = 1 / math.sqrt(d)
+
+    def check(got, q, keys, vals, seen, what):
+        o, w = attend(q, keys, vals, seen, scale, 0.0)
+        assert np.all(np.abs(got - o) <= 2.0 ** -8 * np.abs(o) + (2.0 ** -8 + 1e-3) * w), what
+
+    stored = np.zeros((B, L, H), np.int32)
+    start = np.zeros(B, np.int32)
+    for chunk in range(3):
+        n = tokens[chunk].astype(np.int32)
+        d_n = to_device(n, "cuda")
+        nxt = stored.copy()
+        for l in range(L):
+            # the layer's history read back into pages that the layers share, attention over it and the chunk
+            s = PrefillSession(wl, tables=t, layer=l, pool=scratch, hist_len=stored, mx=fm, mx_pool=pool,
+                               mod=tg.make_score_mod(0.0, d_n))
+            s.q.copy_(randn(*s.q.shape)), s.k_new.copy_(randn(*s.k_new.shape)), s.v_new.copy_(randn(*s.v_new.shape))
+            s.run()
+            c = CompressSession(wl, t, pool, start, n, layer=l, k_new=s.k_new, v_new=s.v_new,
+                                scores=torch.randn(B, H, C, generator=gen, device="cuda"), mx=fm)
+            c.run()
+            torch.cuda.synchronize()
+            q, k, v, out, kept = f64(s.q), f64(s.k_new), f64(s.v_new), f64(s.out), c.kept.cpu().numpy()
+            for b, h in np.ndindex(B, H):
+                m, i = int(stored[b, l, h]), slice(0, n[b])
+                keys, vals = ref.rows(b, l, h, m)
+                keys, vals = np.concatenate([keys, k[b, i, h]]), np.concatenate([vals, v[b, i, h]])
+                seen = np.ones((n[b], m + n[b]), bool)
+                seen[:, m:] = np.tri(n[b], dtype=bool)
+                for j in range(h * gqa, (h + 1) * gqa):
+                    check(out[b, i, j], q[b, i, j], keys, vals, seen, (chunk, l, b, j))
+            for b, h in np.ndindex(B, H):
+                for e in range(int(c.plan["keep_count"][b, h])):
+                    ref.store(b, l, h, int(stored[b, l, h]) + e, k[b, kept[b, h, e], h], v[b, kept[b, h, e], h])
+            nxt[:, l] += c.plan["keep_count"].astype(np.int32)
+            got = pool.cpu().numpy()
+            assert np.array_equal(got, ref.host), np.argwhere(got != ref.host)[:4].tolist()
+        stored, start = nxt, start + n
+    assert np.array_equal(stored, t.kv_len)
+
+    # decode steps, one session storing its token in the attention, one before it, from the same bytes
+    make = lambda pool: DecodeSession(wl, tables=t, mode=tg.TG_PLAN_AOT_FILL, pool=pool, open_end=True, mx=fm)
+    ds, apart = make(pool), make(pool.clone())
+    ds.enable_append(fused=True), apart.enable_append(ds.k_tok, ds.v_tok)
+    for step in range(steps):
+        ds.k_tok.copy_(randn(*ds.k_tok.shape)), ds.v_tok.copy_(randn(*ds.v_tok.shape)), ds.q.copy_(randn(*ds.q.shape))
+        apart.q.copy_(ds.q)
+        ds.run_decode_step(), apart.run_decode_step()
+        torch.cuda.synchronize()
+        k, v, q, out = f64(ds.k_tok), f64(ds.v_tok), f64(ds.q), f64(ds.out)
+        for l, b, h in np.ndindex(L, B, H):
+            ref.store(b, l, h, int(stored[b, l, h]) + step, k[l, b, h], v[l, b, h])
+            m = int(stored[b, l, h]) + step + 1
+            keys, vals = ref.rows(b, l, h, m)
+            heads = slice(h * gqa, (h + 1) * gqa)
+            check(out[l, b, heads], q[l, b, heads], keys, vals, np.ones((gqa, m), bool), (step, l, b, h))
+        assert np.array_equal(pool.cpu().numpy(), ref.host)
+        assert torch.equal(pool, apart.pool) and torch.equal(ds.out, apart.out) and torch.equal(ds.lse, apart.lse)
+        assert np.array_equal(ds.live_len.cpu().numpy(), stored + step + 1) and torch.equal(ds.live_len, apart.live_len)
+    assert int(ds.full) == 0 and int(apart.full) == 0
+    say(f"{bits} d{d}: three chunks of {L} layers and {steps} steps, {int(ds.live_len.sum())} entries")
+
+
+def test_steps_from_projection_rows():
+    """run_projected_step and the same rows rotated apart and appended: the same cache and outputs; replayed from a graph
+    with eager steps between."""
+    B, g, d, steps = 3, Geometry(2, 4, 16, 128, 16, 2), 128, 8
+    wl = custom(72, g, B, "bf16", (30, 400))
+    t = Tables(wl, headroom=np.full(B, steps + 2, np.int32))
+    fm = fmt((8, 4))
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    randn = lambda *s: torch.randn(*s, generator=gen, device="cuda").bfloat16()
+    turns = torch.from_numpy(tg.tg_rope_freqs(d, 10000.0)[0].view(np.int64)).cuda()
+    w = (1 + 0.1 * randn(d)).bfloat16()
+    spec = tg.make_rope_spec(tg.TG_ROPE_HALF, d, turns, 1.0, True, 1e-6, 0.0, w, w)
+    a, b = (DecodeSession(wl, tables=t, mode=tg.TG_PLAN_AOT_FILL, open_end=True, mx=fm, softcap=20.0) for _ in range(2))
+    assert torch.equal(a.pool, b.pool) and a.pool.data_ptr() != b.pool.data_ptr()
+    rows, positions = randn(2, B, (16 + 8) * d), torch.arange(B, dtype=torch.int32, device="cuda") * 1000
+    a.enable_projection(spec, rows, positions)
+    kt, vt = torch.zeros(2, B, 4, d, dtype=torch.bfloat16, device="cuda"), torch.zeros(2, B, 4, d, dtype=torch.bfloat16, device="cuda")
+    b.enable_append(kt, vt)
+    ropes = [tg.make_rope_args(g, B, 1, tg.TG_BF16, spec, rows[l][:, :16 * d], rows[l][:, 16 * d:20 * d], rows[l][:, 20 * d:],
+                               b.q[l], kt[l], vt[l], positions=positions) for l in range(2)]
+    graph, stream = None, torch.cuda.Stream()
+    for i in range(steps):
+        rows.copy_(randn(*rows.shape))
+        torch.cuda.synchronize()
+        if i == 2:
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=stream):
+                a.run_projected_step(stream)
+        if i >= 2 and i % 3:
+            graph.replay()
+        else:
+            a.run_projected_step()
+        for r in ropes:
+            tg.tg_rope(r)
+        b.run_decode_step()
+        torch.cuda.synchronize()
+        assert torch.equal(a.q, b.q) and torch.equal(a.pool, b.pool) and torch.equal(a.live_len, b.live_len)
+        assert torch.equal(a.out, b.out) and torch.equal(a.lse, b.lse)
+        x = f64(rows[1]).reshape(B, -1, d)
+        theta = turns.cpu().numpy().view(np.uint64).astype(np.float64) / 2.0 ** 64 * 2 * math.pi
+        want = rotated(x[:, 16:20], f64(w), positions.cpu().numpy().astype(np.float64), theta, 1.0)
+        assert np.all(np.abs(f64(a.k_tok[1]) - want) <= 2.0 ** -8 * np.abs(want) + 1e-4)
+        positions.add_(1)
+    assert int(a.full) == 0 and torch.equal(a.live_len.cpu(), torch.from_numpy(t.kv_len) + steps)
+
+
+@pytest.mark.parametrize("bins", [1, 2, 5])
+def test_bins_of_many_items(bins):
+    """More items a bin than a wave has lanes, with and without their token's append."""
+    lens = list(range(1, 48))
+    c, e = (Cache(lens, H=4, gqa=2, d=128, Hp=2, bits=(4, 8), headroom=2, seed=3) for _ in range(2))
+    assert c.B * c.H > 128
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    rand = lambda *s: torch.randn(*s, generator=gen, device="cuda").bfloat16()
+    live, live2 = (to_device(c.kv_len, "cuda") for _ in range(2))
+    q, k, v = rand(c.B, 8, 128), rand(c.B, 4, 128), rand(c.B, 4, 128)
+    out, lse, _ = c.decode(q, "bf16", bins=bins)
+    check_decode(c, q, out, lse, "bf16", what=f"bins {bins}")
+    full = torch.zeros(1, dtype=torch.int32, device="cuda")
+    out, lse, _ = c.decode(q, "bf16", bins=bins, open_end=True, live=live, k_tok=k, v_tok=v, full=full)
+    tg.tg_append_mx(tg.make_append_args(e.geom, e.B, 0, tg.TG_BF16, k, v, e.pool, *e.tables, live2), e.fmt)
+    out2, lse2, _ = e.decode(q, "bf16", bins=bins, open_end=True, live=live2)
+    assert int(full) == 0 and torch.equal(live, live2) and torch.equal(c.pool, e.pool)
+    assert torch.equal(out, out2) and torch.equal(lse, lse2)
+    check_decode(c, q, out, lse, "bf16", lens=c.kv_len[:, 0] + 1, host=c.pool.cpu().numpy(), what=f"bins {bins}, append")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_unpack_of_many_heads(dtype):
+    """More (request, head) units than are shared out at once, some of them empty."""
+    rng = np.random.default_rng(2)
+    c = Cache(rng.integers(1, 60, 280), H=8, gqa=1, d=64, Hp=2, bits=(8, 4), seed=2)
+    length = c.kv_len.copy()
+    length[rng.random(length.shape) < 0.3] = 0
+    assert length.size > 2048
+    rows = torch.full((c.pool_pages, 2, 2, 16, 64), 77.0, dtype=DTYPE[dtype], device="cuda")
+    want = f64(rows)
+    d_length = to_device(length, "cuda")
+    tg.tg_unpack_mx(tg.make_unpack_mx_args(c.geom, c.B, 0, TG[dtype], c.fmt, c.pool, *c.tables, d_length, rows))
+    for b, h in np.ndindex(c.B, 8):
+        n = int(length[b, 0, h])
+        page, slot = c.slabs(b, 0, h, n)
+        if n:
+            for i, x in enumerate(c.rows(b, 0, h, n)):
+                for j, p in enumerate(page):
+                    m = min(16, n - 16 * j)
+                    want[p, i, slot, :m] = x[16 * j:16 * j + m]
+    assert np.array_equal(f64(rows), want)
+
+
+def test_two_streams():
+    """Calls of two caches at once, each with its own workspace, as each by itself."""
+    caches = [Cache([900, 40, 3000], H=4, gqa=4, d=128, Hp=2, bits=b, seed=9) for b in ((4, 4), (8, 8))]
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    q = torch.randn(3, 16, 128, generator=gen, device="cuda").bfloat16()
+    alone, keep, streams = [], [{}, {}], [torch.cuda.Stream() for _ in caches]
+    for c, kp in zip(caches, keep):
+        out, lse, _ = c.decode(q, "bf16", bins=100)
+        alone.append((out.clone(), lse.clone()))
+        c.decode(q, "bf16", bins=100, keep=kp)
+    torch.cuda.synchronize()
+    for kp in keep:
+        kp["out"].zero_()
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for c, kp, s in zip(caches, keep, streams):
+            tg.tg_decode_mx(kp["args"], c.fmt, 0.0, s)
+    torch.cuda.synchronize()
+    for (out, lse), kp in zip(alone, keep):
+        assert torch.equal(out, kp["out"]) and torch.equal(lse, kp["lse"])
