@@ -297,14 +297,19 @@ class DecodeSession:
 
     def _bind_append(self):
         # decode args that also append (kept apart from the plain ones, which run_step uses)
-        self.append_decode_args = {}
-        if not getattr(self, "fused_append", False):
-            return
+        fused = getattr(self, "fused_append", False)
+        self.append_decode_args = self._appending(self.k_tok, self.v_tok) if fused else {}
+        if self.mx is not None and getattr(self, "rope_args", None):
+            self.projected_args = self._appending(*self.rope_kv)
+
+    def _appending(self, k, v):
+        res = {}
         for l in self.layers:
             a = tg.tg_decode_args.from_buffer_copy(self.dplans[l].args)
-            a.append_k, a.append_v = self.k_tok[l].data_ptr(), self.v_tok[l].data_ptr()
+            a.append_k, a.append_v = k[l].data_ptr(), v[l].data_ptr()
             a.append_full = self.full.data_ptr()
-            self.append_decode_args[l] = a
+            res[l] = a
+        return res
 
     def append_layer(self, l, stream=None):
         if self.mx is not None:
@@ -315,19 +320,20 @@ class DecodeSession:
     def enable_projection(self, spec, rows, positions):
         """The step's queries, keys and values come as projection rows ([L][B][(Hq + 2H) * d], queries first, then keys,
         then values) with the tokens' positions [B] int32: run_projected_step normalises, rotates and stores them
-        (tg_rope_append into self.q and the cache), then attends.  With a quantised cache they go through self.q,
-        self.k_tok and self.v_tok (tg_rope), and the attention stores them."""
+        (tg_rope_append into self.q and the cache), then attends.  With a quantised cache the rotated keys and the
+        values go through a buffer of their own (tg_rope), from which the attention stores them."""
         assert self.open_end, "appending needs open-ended plans and live lengths"
         g, B = self.wl.geom, self.wl.batch
         self.rows, self.positions, self.spec = rows, positions, spec
         q, k = g.num_q_heads * g.head_dim, g.num_kv_heads * g.head_dim
-        if self.mx is not None:
-            self.enable_append(fused=True)
-            self.rope_args = {l: tg.make_rope_args(g, B, 1, self.tg_dtype, spec, rows[l][:, :q], rows[l][:, q:q + k],
-                                                   rows[l][:, q + k:], self.q[l], self.k_tok[l], self.v_tok[l],
-                                                   positions=positions) for l in self.layers}
-            return
         self._append_tables()
+        if self.mx is not None:
+            self.rope_kv = torch.zeros(2, g.num_layers, B, g.num_kv_heads, g.head_dim, dtype=self.dtype, device=self.device)
+            self.rope_args = {l: tg.make_rope_args(g, B, 1, self.tg_dtype, spec, rows[l][:, :q], rows[l][:, q:q + k],
+                                                   rows[l][:, q + k:], self.q[l], *self.rope_kv[:, l],
+                                                   positions=positions) for l in self.layers}
+            self._bind_append()
+            return
         self.rope_append_args = {l: tg.make_rope_append_args(
             g, B, l, self.tg_dtype, spec, rows[l][:, :q], rows[l][:, q:q + k], rows[l][:, q + k:], positions, self.q[l],
             self.pool, self.t.d_pt_pages, self.d_offsets, self.d_group_of, self.d_slot_of, self.live_len, self.full)
@@ -337,7 +343,7 @@ class DecodeSession:
         for l in self.layers:
             if self.mx is not None:
                 tg.tg_rope(self.rope_args[l], stream)
-                self._decode(self.append_decode_args[l], stream)
+                self._decode(self.projected_args[l], stream)
                 continue
             tg.tg_rope_append(self.rope_append_args[l], stream)
             self._decode(self.dplans[l].args, stream)

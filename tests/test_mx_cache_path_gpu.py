@@ -168,9 +168,52 @@ def test_steps_from_projection_rows():
         x = f64(rows[1]).reshape(B, -1, d)
         theta = turns.cpu().numpy().view(np.uint64).astype(np.float64) / 2.0 ** 64 * 2 * math.pi
         want = rotated(x[:, 16:20], f64(w), positions.cpu().numpy().astype(np.float64), theta, 1.0)
-        assert np.all(np.abs(f64(a.k_tok[1]) - want) <= 2.0 ** -8 * np.abs(want) + 1e-4)
+        assert np.all(np.abs(f64(a.rope_kv[0, 1]) - want) <= 2.0 ** -8 * np.abs(want) + 1e-4)
         positions.add_(1)
     assert int(a.full) == 0 and torch.equal(a.live_len.cpu(), torch.from_numpy(t.kv_len) + steps)
+
+
+@pytest.mark.parametrize("fused", [False, True])
+def test_steps_that_append_and_steps_that_project_alternate(fused):
+    """Whichever was enabled first, each with buffers of its own, and after the plans were rebuilt."""
+    B, g, d, steps = 3, Geometry(2, 4, 16, 128, 16, 2), 128, 8
+    wl = custom(72, g, B, "bf16", (30, 400))
+    t = Tables(wl, headroom=np.full(B, 16, np.int32))
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    randn = lambda *s: torch.randn(*s, generator=gen, device="cuda").bfloat16()
+    k, v, rows = randn(steps, 2, B, 4, d), randn(steps, 2, B, 4, d), randn(steps, 2, B, (16 + 8) * d)
+    turns = torch.from_numpy(tg.tg_rope_freqs(d, 10000.0)[0].view(np.int64)).cuda()
+    spec = tg.make_rope_spec(tg.TG_ROPE_HALF, d, turns)
+    results = []
+    for first in ("append", "project"):
+        s = DecodeSession(wl, tables=t, mode=tg.TG_PLAN_AOT_FILL, n_bins=32, open_end=True, mx=fmt((4, 4)))
+        kt, vt, rt = torch.zeros_like(k[0]), torch.zeros_like(v[0]), torch.zeros_like(rows[0])
+        positions = torch.arange(B, dtype=torch.int32, device="cuda") * 1000
+        for what in ("append", "project") if first == "append" else ("project", "append"):
+            s.enable_append(kt, vt, fused=fused) if what == "append" else s.enable_projection(spec, rt, positions)
+        outs = []
+        for i in range(steps):
+            if i == 4:
+                s.set_bin_weights(np.arange(1, 33, dtype=np.int32))
+            s.q.copy_(0.1 * i + torch.linspace(-1, 1, s.q.numel(), device="cuda").view_as(s.q))
+            if i % 2:
+                kt.copy_(k[i]), vt.copy_(v[i])
+                s.run_decode_step()
+            else:
+                rt.copy_(rows[i])
+                s.run_projected_step()
+            outs.append(s.out.clone())
+        torch.cuda.synchronize()
+        assert int(s.full) == 0 and torch.equal(s.live_len.cpu(), torch.from_numpy(t.kv_len) + steps)
+        # the tokens of the steps, as their rows quantise
+        ref = Bytes(t, g, (4, 4), s.pool.cpu().numpy())
+        have = ref.host.copy()
+        for l, b, h, i in np.ndindex(2, B, 4, steps):
+            if i % 2:
+                ref.store(b, l, h, int(t.kv_len[b, l, h]) + i, f64(k[i, l, b, h]), f64(v[i, l, b, h]))
+        assert np.array_equal(have, ref.host)
+        results.append((s.pool, *outs))
+    assert all(torch.equal(a, b) for a, b in zip(*results))
 
 
 @pytest.mark.parametrize("bins", [1, 2, 5])
