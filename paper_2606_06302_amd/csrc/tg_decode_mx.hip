@@ -193,12 +193,14 @@ struct Shape {
 };
 
 // 16 or 4 bytes a lane from base + offset into LDS at lds + 16 (4) * lane, past the
-// caches' keeping: a step reads every byte of the cache once.
+// caches' keeping: a step reads every byte of the cache once.  M0 is read one wait
+// state after its write at the earliest, which neither the hardware nor, in inline
+// assembly, the compiler sees to: hence the s_nop.
 __device__ __forceinline__ void dma16(const void* base, uint32_t offset, uint32_t lds) {
-  asm volatile("global_load_lds_dwordx4 %0, %1 nt sc1" ::"v"(offset), "s"(base), "{m0}"(lds) : "memory");
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt sc1" ::"v"(offset), "s"(base), "{m0}"(lds) : "memory");
 }
 __device__ __forceinline__ void dma4(const void* base, uint32_t offset, uint32_t lds) {
-  asm volatile("global_load_lds_dword %0, %1 nt sc1" ::"v"(offset), "s"(base), "{m0}"(lds) : "memory");
+  asm volatile("s_nop 0\n\tglobal_load_lds_dword %0, %1 nt sc1" ::"v"(offset), "s"(base), "{m0}"(lds) : "memory");
 }
 template <int N>
 __device__ __forceinline__ void wait_vmcnt() {

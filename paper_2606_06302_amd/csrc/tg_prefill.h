@@ -67,9 +67,11 @@ __device__ __forceinline__ uint32_t lds_address(const void* ptr) {
 
 // 16 bytes per lane from global memory (a wave-uniform base plus 16 * chunk
 // bytes per lane) into LDS at m0_base + 16 * lane.  The scalar base keeps
-// 64-bit addresses out of the vector registers.
+// 64-bit addresses out of the vector registers.  M0 is read one wait state after
+// its write at the earliest, which neither the hardware nor, in inline assembly,
+// the compiler sees to: hence the s_nop.
 __device__ __forceinline__ void lds_dma16(const u4* base, uint32_t chunk, uint32_t m0_base) {
-  asm volatile("global_load_lds_dwordx4 %0, %1" ::"v"(chunk * 16), "s"(base), "{m0}"(m0_base) : "memory");
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(chunk * 16), "s"(base), "{m0}"(m0_base) : "memory");
 }
 
 template <int N>
