@@ -992,6 +992,9 @@ int32_t tg_decode_mx_bins(const tg_geometry* geom, int32_t dtype, const tg_mx_fo
  *     as stored: one call gives what tg_append_mx and tg_decode_mx give, bit for bit.
  *   merge_counters: not used; the partials of split units are always joined by a
  *     launch of their own.
+ * Scores and their sums are held in fp32; a weight goes into its product with V with
+ * 24 bits in fp32 calls and 16 (off by 2^-16 of it at most) in bf16 ones, at both head
+ * sizes.
  * Scores that overflow to -inf have no weight; a head with no other scores gives
  * zeros and an lse of -FLT_MAX.
  * Supported: dtype TG_F32 or TG_BF16, gqa 1..16. */

@@ -25,7 +25,12 @@
 //   * O^T[16 dims][16 heads] += V^T P^T, D/16 products 32 (or 16) tokens deep:
 //     tokens 4j .. 4j + 3 of a page for lane group j, which is where S^T leaves
 //     them.  The codes pair dims, the operand pairs tokens: one byte permute each.
-// With fp32 queries, q and P go in as three bf16 parts that hold their 24 bits.
+// With fp32 queries, q and P go in as three bf16 parts that hold their 24 bits.  With
+// bf16 queries P goes in as two, 16 bits: rounded to bf16 alone it is the larger part
+// of the result's error (32 requests of 8192 tokens in 4 bits, as a share of the
+// result: 0.0022, in two parts 0.0017, the result's own rounding), and all of a small
+// result where values cancel.  The second part costs 1 to 4 % of a call (there 24.2
+// and 25.1 us); where a step is one page, both go into one product of twice the depth.
 //
 // Bound by memory where there is enough of it: 64 requests, 189971 pages of 8-bit
 // rows (802 MB) 131 us, 6.1 TB/s; 95142 pages of 4-bit rows (207 MB, much of it in
@@ -222,7 +227,8 @@ __global__ void __launch_bounds__(kBlock, sizeof(T) == 2 && !(D == 128 && KB == 
                         const int32_t* __restrict__ bin_offsets_g) {
   using S = Shape<D, KB, VB>;
   constexpr int E = Row16<T>::kElems;
-  constexpr int NPART = sizeof(T) == 4 ? 3 : 1;   // bf16 parts of q and P
+  constexpr int NPART = sizeof(T) == 4 ? 3 : 1;   // bf16 parts of q
+  constexpr int PPART = sizeof(T) == 4 ? 3 : 2;   // of P
   constexpr int KP = S::kPages;
   constexpr int KW = D * KB / 128, VW = D * VB / 128;
   constexpr int NQ = D / 32, NV = D / 16;
@@ -536,12 +542,14 @@ __global__ void __launch_bounds__(kBlock, sizeof(T) == 2 && !(D == 128 && KB == 
         float sum = (sv[0] + sv[1]) + (sv[2] + sv[3]);
         if constexpr (KP == 2) sum += (sv[4] + sv[5]) + (sv[6] + sv[7]);
         l += sum;
-        uint32_t pb[NPART][2 * KP];
+        uint32_t pb[PPART][2 * KP];
 #pragma unroll
         for (int i = 0; i < 2 * KP; ++i) {
-          if constexpr (NPART == 1) {
-            // bf16 outputs: P rounded to bf16, half a step of the output's own
-            pb[0][i] = pack_bf16(sv[2 * i], sv[2 * i + 1]);
+          if constexpr (PPART == 2) {
+            // the first part cut, 2^-7 of P left at most, the second rounded: off by 2^-16 of P
+            const uint32_t x0 = __float_as_uint(sv[2 * i]), x1 = __float_as_uint(sv[2 * i + 1]);
+            pb[0][i] = join16(x0, x1);
+            pb[1][i] = pack_bf16(sv[2 * i] - __uint_as_float(x0 & 0xffff0000u), sv[2 * i + 1] - __uint_as_float(x1 & 0xffff0000u));
           } else {
             uint32_t a[3], b[3];
             split3(sv[2 * i], a);
@@ -555,9 +563,18 @@ __global__ void __launch_bounds__(kBlock, sizeof(T) == 2 && !(D == 128 && KB == 
           uint32_t a[2 * KP], b[2 * KP];
           if constexpr (!kEarly) v_operands(i, a, b);
 #pragma unroll
-          for (int part = 0; part < NPART; ++part) {
-            acc[2 * i] = mfma_pv<KP>(kEarly ? va[i] : a, pb[part], acc[2 * i]);
-            acc[2 * i + 1] = mfma_pv<KP>(kEarly ? vb[i] : b, pb[part], acc[2 * i + 1]);
+          for (int part = 0; part < PPART; ++part) {
+            if constexpr (KP == 1 && PPART == 2) {   // both parts in one product of twice the depth
+              if (part > 0) break;
+              const uint32_t a2[4] = {va[i][0], va[i][1], va[i][0], va[i][1]};
+              const uint32_t b2[4] = {vb[i][0], vb[i][1], vb[i][0], vb[i][1]};
+              const uint32_t w[4] = {pb[0][0], pb[0][1], pb[1][0], pb[1][1]};
+              acc[2 * i] = mfma_pv<2>(a2, w, acc[2 * i]);
+              acc[2 * i + 1] = mfma_pv<2>(b2, w, acc[2 * i + 1]);
+            } else {
+              acc[2 * i] = mfma_pv<KP>(kEarly ? va[i] : a, pb[part], acc[2 * i]);
+              acc[2 * i + 1] = mfma_pv<KP>(kEarly ? vb[i] : b, pb[part], acc[2 * i + 1]);
+            }
           }
         }
       }
