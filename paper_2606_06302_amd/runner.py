@@ -128,6 +128,13 @@ def random_mx_pool(geom, fmt, pages, device="cuda", seed=0):
     return pool.view(pages, geom.heads_per_group, slab)
 
 
+def check_mx_pool(pool, geom, fmt, pages):
+    """A quantised pool of at least that many pages of the format (a smaller one would be written past its end)."""
+    need = pages * tg.tg_mx_page_bytes(geom, fmt)
+    assert pool.dtype == torch.uint8 and pool.is_contiguous(), f"a quantised pool is dense bytes (got {pool.dtype})"
+    assert pool.numel() >= need, f"the quantised pool holds {pool.numel()} bytes, {pages} pages take {need}"
+
+
 class DecodeSession:
     """Pool, queries, outputs and per-layer plans of one decode workload.  softcap not 0: the scores are capped
     (tg_decode_capped).  mx: the tg_mx_format of a quantised cache; the pool is then bytes ([pages][H_p][slab], random
@@ -173,8 +180,7 @@ class DecodeSession:
             self.pool = torch.empty(self.t.pool_pages * page_elems(g), dtype=self.dtype, device=device)
             device_normal_(self.pool, wl, S_POOL, wl.kv_scale)
         if mx is not None:
-            assert self.pool.dtype == torch.uint8 and self.pool.is_contiguous() and \
-                self.pool.numel() >= self.t.pool_pages * tg.tg_mx_page_bytes(g, mx), "a quantised pool is bytes, tg_mx_page_bytes a page"
+            check_mx_pool(self.pool, g, mx, self.t.pool_pages)
         else:
             self.pool = self.pool.view(self.t.pool_pages, 2, g.heads_per_group, g.page_size, g.head_dim)
         if q is not None:
@@ -306,6 +312,7 @@ class DecodeSession:
         res = {}
         for l in self.layers:
             a = tg.tg_decode_args.from_buffer_copy(self.dplans[l].args)
+            a.pool = self.dplans[l].args.pool
             a.append_k, a.append_v = k[l].data_ptr(), v[l].data_ptr()
             a.append_full = self.full.data_ptr()
             res[l] = a
@@ -387,6 +394,7 @@ class DecodeSession:
         dp = self.dplans[l]
         ts = torch.zeros(2 * dp.host["num_bins"], dtype=torch.int64, device=self.device)
         args = tg.tg_decode_args.from_buffer_copy(dp.args)
+        args.pool = dp.args.pool
         args.timestamps = ts.data_ptr()
         self._decode(args, stream)
         torch.cuda.synchronize()
@@ -487,6 +495,7 @@ class PrefillSession:
         pages, pool_pages = self.t.d_pt_pages, self.t.pool_pages
         if mx is not None:
             assert mx_pool is not None, "a quantised history has a pool"
+            check_mx_pool(mx_pool, g, mx, self.t.pool_pages)
             ids, pool_pages = self._layer_pages()
             self.d_layer_pages = pages = to_device(ids, device)
             if pool is None:
@@ -589,6 +598,8 @@ class CompressSession:
         B, C, H = wl.batch, wl.chunk_len, g.num_kv_heads
         self.wl, self.t, self.layer, self.device = wl, tables, layer, device
         self.pool, self.mx = pool, mx
+        if mx is not None:
+            check_mx_pool(pool, g, mx, tables.pool_pages)
         self.dtype = TORCH_DTYPE[wl.dtype]
         self.chunk_start = np.asarray(chunk_start, dtype=np.int32)
         self.chunk_tokens = np.asarray(chunk_tokens, dtype=np.int32)

@@ -53,6 +53,7 @@ class tg_geometry(C.Structure):
 
 
 class tg_decode_args(C.Structure):
+    pool = None   # (address, quantised) of the tensor that kv_pool was packed from
     _fields_ = [("geom", tg_geometry), ("batch", C.c_int32), ("dtype", C.c_int32),
                 ("q", C.c_void_p), ("kv_pool", C.c_void_p), ("pt_pages", C.c_void_p),
                 ("items", C.c_void_p), ("bin_offsets", C.c_void_p), ("n_bins", C.c_int32),
@@ -65,6 +66,7 @@ class tg_decode_args(C.Structure):
 
 
 class tg_prefill_args(C.Structure):
+    pool = None   # (address, quantised) of the tensor that kv_pool was packed from
     _fields_ = [("geom", tg_geometry), ("batch", C.c_int32), ("chunk_len", C.c_int32), ("layer", C.c_int32),
                 ("dtype", C.c_int32), ("q", C.c_void_p), ("k_new", C.c_void_p), ("v_new", C.c_void_p),
                 ("kv_pool", C.c_void_p), ("pt_pages", C.c_void_p), ("pt_offsets", C.c_void_p),
@@ -74,6 +76,7 @@ class tg_prefill_args(C.Structure):
 
 
 class tg_append_args(C.Structure):
+    pool = None   # (address, quantised) of the tensor that kv_pool was packed from
     _fields_ = [("geom", tg_geometry), ("batch", C.c_int32), ("layer", C.c_int32), ("dtype", C.c_int32),
                 ("k_tok", C.c_void_p), ("v_tok", C.c_void_p), ("kv_pool", C.c_void_p), ("pt_pages", C.c_void_p),
                 ("pt_offsets", C.c_void_p), ("group_of", C.c_void_p), ("slot_of", C.c_void_p),
@@ -81,6 +84,7 @@ class tg_append_args(C.Structure):
 
 
 class tg_compress_args(C.Structure):
+    pool = None   # (address, quantised) of the tensor that kv_pool was packed from
     _fields_ = [("geom", tg_geometry), ("batch", C.c_int32), ("chunk_len", C.c_int32), ("dtype", C.c_int32),
                 ("k_new", C.c_void_p), ("v_new", C.c_void_p), ("scores", C.c_void_p), ("kv_pool", C.c_void_p),
                 ("pt_pages", C.c_void_p), ("items", C.c_void_p), ("num_items", C.c_int32),
@@ -345,6 +349,22 @@ def _dptr(t):
     return None if t is None else C.c_void_p(t.data_ptr())
 
 
+def _packed(args, kv_pool):
+    """args, which remember whether the pool holds rows or the bytes of a quantised cache, whose pages lie closer."""
+    if kv_pool is not None:
+        args.pool = kv_pool.data_ptr(), str(kv_pool.dtype) == "torch.uint8"
+    return args
+
+
+def _check_pool(where, args, quantised=False):
+    """The other kind's pool would be read and written past its end (not known of arguments that were packed otherwise,
+    or given another pool since)."""
+    pool = args.pool
+    if pool and pool[1] != quantised and pool[0] == args.kv_pool:
+        raise TangramError(TG_ERR_INVALID_ARG, where, "kv_pool is not a quantised pool (uint8)" if quantised else
+                           "kv_pool holds the bytes of a quantised cache, which the _mx calls take")
+
+
 def _stream(stream):
     if stream is None:
         return None
@@ -361,15 +381,17 @@ def make_decode_args(geom, batch, dtype, q, kv_pool, pt_pages, items, bin_offset
     zeros for the in-launch merge, or None for the two-launch merge; append_k / append_v the
     step's new token rows [B][H][d] for the in-launch append (with live_len), append_full an
     int32 flag the caller clears."""
-    return tg_decode_args(_geom(geom), int(batch), int(dtype), _dptr(q), _dptr(kv_pool), _dptr(pt_pages),
+    args = tg_decode_args(_geom(geom), int(batch), int(dtype), _dptr(q), _dptr(kv_pool), _dptr(pt_pages),
                           _dptr(items), _dptr(bin_offsets), int(n_bins), int(num_items), _dptr(unit_splits),
                           _dptr(unit_partial_base), int(num_partials), _dptr(out), _dptr(lse), float(sm_scale),
                           _dptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
                           _dptr(timestamps), _dptr(live_len), int(layer), _dptr(merge_counters),
                           _dptr(append_k), _dptr(append_v), _dptr(append_full))
+    return _packed(args, kv_pool)
 
 
 def tg_decode(args: tg_decode_args, stream=None):
+    _check_pool("tg_decode", args)
     _check(_lib.tg_decode(C.byref(args), _stream(stream)), "tg_decode")
 
 
@@ -378,6 +400,7 @@ TG_DECODE_NOALLOC_MAX_BYTES = 16 << 20
 
 def tg_decode_noalloc(args: tg_decode_args, stream=None):
     """tg_decode with the partials in the library's static per-device scratch (args.workspace ignored)."""
+    _check_pool("tg_decode_noalloc", args)
     _check(_lib.tg_decode_noalloc(C.byref(args), _stream(stream)), "tg_decode_noalloc")
 
 
@@ -386,11 +409,12 @@ def make_prefill_args(geom, batch, chunk_len, layer, dtype, q, k_new, v_new, kv_
                       block_order=None) -> tg_prefill_args:
     """Packs a tg_prefill_args from device tensors (kept alive by the caller); block_order is the
     device copy of a tg_prefill_schedule result, or None for the default block mapping."""
-    return tg_prefill_args(_geom(geom), int(batch), int(chunk_len), int(layer), int(dtype), _dptr(q),
+    args = tg_prefill_args(_geom(geom), int(batch), int(chunk_len), int(layer), int(dtype), _dptr(q),
                            _dptr(k_new), _dptr(v_new), _dptr(kv_pool), _dptr(pt_pages), _dptr(pt_offsets),
                            _dptr(kv_len), _dptr(group_of), _dptr(slot_of), _dptr(out), float(sm_scale),
                            _dptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
                            _dptr(block_order), 0 if block_order is None else int(block_order.numel()))
+    return _packed(args, kv_pool)
 
 
 def tg_prefill_schedule(geom, batch, chunk_len, layer, kv_len, n_xcd=8):
@@ -421,6 +445,7 @@ def tg_prefill_workspace_bytes(args: tg_prefill_args) -> int:
 
 
 def tg_prefill(args: tg_prefill_args, stream=None):
+    _check_pool("tg_prefill", args)
     _check(_lib.tg_prefill(C.byref(args), _stream(stream)), "tg_prefill")
 
 
@@ -452,12 +477,14 @@ def tg_compress_plan(geom, batch, layer, chunk_len, chunk_start, chunk_tokens, r
 def make_compress_args(geom, batch, chunk_len, dtype, k_new, v_new, scores, kv_pool, pt_pages, items, num_items,
                        chunk_tokens, keep_count, kept) -> tg_compress_args:
     """Packs a tg_compress_args from device tensors (kept alive by the caller)."""
-    return tg_compress_args(_geom(geom), int(batch), int(chunk_len), int(dtype), _dptr(k_new), _dptr(v_new),
+    args = tg_compress_args(_geom(geom), int(batch), int(chunk_len), int(dtype), _dptr(k_new), _dptr(v_new),
                             _dptr(scores), _dptr(kv_pool), _dptr(pt_pages), _dptr(items), int(num_items),
                             _dptr(chunk_tokens), _dptr(keep_count), _dptr(kept))
+    return _packed(args, kv_pool)
 
 
 def tg_compress(args: tg_compress_args, stream=None):
+    _check_pool("tg_compress", args)
     _check(_lib.tg_compress(C.byref(args), _stream(stream)), "tg_compress")
 
 
@@ -476,12 +503,14 @@ def tg_memory_footprint(geom, ctx_len, ratio, budget, group_of) -> dict:
 def make_append_args(geom, batch, layer, dtype, k_tok, v_tok, kv_pool, pt_pages, pt_offsets, group_of, slot_of,
                      live_len, full=None) -> tg_append_args:
     """Packs a tg_append_args from device tensors (kept alive by the caller)."""
-    return tg_append_args(_geom(geom), int(batch), int(layer), int(dtype), _dptr(k_tok), _dptr(v_tok),
+    args = tg_append_args(_geom(geom), int(batch), int(layer), int(dtype), _dptr(k_tok), _dptr(v_tok),
                           _dptr(kv_pool), _dptr(pt_pages), _dptr(pt_offsets), _dptr(group_of), _dptr(slot_of),
                           _dptr(live_len), _dptr(full))
+    return _packed(args, kv_pool)
 
 
 def tg_append(args: tg_append_args, stream=None):
+    _check_pool("tg_append", args)
     _check(_lib.tg_append(C.byref(args), _stream(stream)), "tg_append")
 
 
@@ -541,6 +570,8 @@ def tg_concat_tables(geom, offsets_a, pages_a, offsets_b, pages_b):
 def tg_read_probe(geom, dtype, kv_pool, page_ids, slots, n_workers, out, stream=None):
     """Streams the K and V slabs of every (page_ids[i], slots[i]) (device int32 tensors); out is a device
     uint32/int32 tensor of n_workers checksums."""
+    if str(kv_pool.dtype) == "torch.uint8":   # its pages lie closer: read as rows, past its end
+        raise TangramError(TG_ERR_INVALID_ARG, "tg_read_probe", "kv_pool holds the bytes of a quantised cache")
     _check(_lib.tg_read_probe(C.byref(_geom(geom)), int(dtype), _dptr(kv_pool), _dptr(page_ids), _dptr(slots),
                               int(page_ids.numel()), int(n_workers), _dptr(out), _stream(stream)), "tg_read_probe")
 
@@ -698,10 +729,12 @@ def make_score_mod(softcap=0.0, chunk_tokens=None, key_begin=None, key_end=None)
 
 
 def tg_prefill_mod(args: tg_prefill_args, mod: tg_score_mod, stream=None):
+    _check_pool("tg_prefill_mod", args)
     _check(_lib.tg_prefill_mod(C.byref(args), C.byref(mod), _stream(stream)), "tg_prefill_mod")
 
 
 def tg_decode_capped(args: tg_decode_args, softcap, stream=None):
+    _check_pool("tg_decode_capped", args)
     _check(_lib.tg_decode_capped(C.byref(args), float(softcap), _stream(stream)), "tg_decode_capped")
 
 
@@ -719,11 +752,13 @@ def tg_mx_page_bytes(geom, fmt: tg_mx_format) -> int:
 
 def tg_append_mx(args: tg_append_args, fmt: tg_mx_format, stream=None):
     """args as make_append_args packs them, kv_pool the quantised pool (uint8)."""
+    _check_pool("tg_append_mx", args, quantised=True)
     _check(_lib.tg_append_mx(C.byref(args), C.byref(fmt), _stream(stream)), "tg_append_mx")
 
 
 def tg_compress_mx(args: tg_compress_args, fmt: tg_mx_format, stream=None):
     """args as make_compress_args packs them, kv_pool the quantised pool (uint8)."""
+    _check_pool("tg_compress_mx", args, quantised=True)
     _check(_lib.tg_compress_mx(C.byref(args), C.byref(fmt), _stream(stream)), "tg_compress_mx")
 
 
@@ -755,4 +790,5 @@ def tg_decode_mx_bins(geom, dtype, fmt: tg_mx_format, device=0, batch=0, layer=0
 
 def tg_decode_mx(args: tg_decode_args, fmt: tg_mx_format, softcap=0.0, stream=None):
     """args as make_decode_args packs them, kv_pool the quantised pool (uint8)."""
+    _check_pool("tg_decode_mx", args, quantised=True)
     _check(_lib.tg_decode_mx(C.byref(args), C.byref(fmt), float(softcap), _stream(stream)), "tg_decode_mx")
