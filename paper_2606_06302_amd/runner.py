@@ -18,6 +18,14 @@ TORCH_DTYPE = {"f32": torch.float32, "bf16": torch.bfloat16}
 TG_DTYPE = {"f32": tg.TG_F32, "bf16": tg.TG_BF16}
 
 
+def entry_bytes(wl, mx=None):
+    """Bytes of one retained entry of a head, K and V: rows of the workload's type, or with mx its codes and scales."""
+    g = wl.geom
+    if mx is not None:
+        return tg.tg_mx_page_bytes(g, mx) // (g.heads_per_group * g.page_size)
+    return 2 * g.head_dim * (4 if wl.dtype == "f32" else 2)
+
+
 class Tables:
     """Clustering + reservation of one workload (host arrays and device copies)."""
 
@@ -47,12 +55,10 @@ class Tables:
         self.device = device
         self.d_pt_pages = to_device(self.pt_pages if len(self.pt_pages) else np.zeros(1, np.int32), device)
 
-    def kv_bytes(self, layer=None) -> int:
-        """Algorithmic bytes of retained K and V (what the method must read)."""
-        g = self.wl.geom
-        esz = 4 if self.wl.dtype == "f32" else 2
+    def kv_bytes(self, layer=None, mx=None) -> int:
+        """Algorithmic bytes of retained K and V (what the method must read); mx: the tg_mx_format of a quantised cache."""
         kv = self.kv_len if layer is None else self.kv_len[:, layer]
-        return int(kv.sum()) * 2 * g.head_dim * esz
+        return int(kv.sum()) * entry_bytes(self.wl, mx)
 
 
 def _torch_stream(stream, device):
@@ -138,7 +144,8 @@ def check_mx_pool(pool, geom, fmt, pages):
 class DecodeSession:
     """Pool, queries, outputs and per-layer plans of one decode workload.  softcap not 0: the scores are capped
     (tg_decode_capped).  mx: the tg_mx_format of a quantised cache; the pool is then bytes ([pages][H_p][slab], random
-    rows where none is given), attended to with tg_decode_mx and appended to with tg_append_mx."""
+    rows where none is given), attended to with tg_decode_mx and appended to with tg_append_mx; its merge is always a launch
+    of its own, whatever fused_merge says."""
 
     def __init__(self, wl, tables: Tables = None, mode=tg.TG_PLAN_AOT, n_bins=None, split_target=None,
                  fill="device", pool=None, q=None, want_lse=True, device="cuda", layers=None, open_end=False,
@@ -563,13 +570,13 @@ class PrefillSession:
             tg.tg_prefill(self.args, stream)
 
     def min_hbm_bytes(self) -> int:
-        """Bytes one launch must move at least: Q, each KV head's retained history and chunk K/V read once,
-        the output written once."""
+        """Bytes one run must move at least: Q, each KV head's retained history (as it is stored) and chunk K/V read
+        once, the output written once."""
         g, wl = self.wl.geom, self.wl
         esz = self.q.element_size()
         B, C, d = wl.batch, wl.chunk_len, g.head_dim
         hist = int(self.hist[:, self.layer, :].astype(np.int64).sum())
-        return int(esz * d * (2 * B * C * g.num_q_heads + 2 * B * C * g.num_kv_heads + 2 * hist))
+        return int(esz * d * (2 * B * C * g.num_q_heads + 2 * B * C * g.num_kv_heads)) + hist * entry_bytes(wl, self.mx)
 
     def flops(self) -> int:
         """Algorithmic flops: 4*d per (query row, visible key) for q.k and p.v."""
@@ -636,8 +643,7 @@ class CompressSession:
         written to the pages, the valid scores read once, and the kept indices written once
         (and read back by the copy)."""
         g = self.wl.geom
-        row = 2 * g.head_dim * (4 if self.wl.dtype == "f32" else 2)
-        stored = row if self.mx is None else tg.tg_mx_page_bytes(g, self.mx) // (g.heads_per_group * g.page_size)
+        row, stored = entry_bytes(self.wl), entry_bytes(self.wl, self.mx)
         kept = int(self.plan["keep_count"].sum())
         scores = int(self.chunk_tokens.astype(np.int64).sum()) * g.num_kv_heads * 4
         return kept * (row + stored) + scores + kept * 4 * 2
