@@ -7,7 +7,7 @@ import torch
 pytestmark = pytest.mark.gpu
 
 if torch.cuda.is_available():
-    from mx_helpers import TG, fmt
+    from mx_helpers import DTYPE, TG, Cache, fmt
     from paper_2606_06302_amd import tangram as tg
 
 
@@ -42,3 +42,24 @@ def test_bins_around_the_borders(dtype, d, gqa, bits, most):
     assert tg.tg_decode_mx_bins(one, TG[dtype], fmt(bits), 0, 1, 0, np.ones((1, 1, 1), np.int32)) == 1
     # lengths whose sum is past 32 bits
     assert tg.tg_decode_mx_bins(g, TG[dtype], fmt(bits), 0, 3, 1, np.full((3, 2, 4), 2 ** 31 - 1, np.int32)) == most * cus
+
+
+@pytest.mark.parametrize("dtype,d,gqa,bits", [("bf16", 128, 1, (8, 4)), ("bf16", 128, 2, (8, 4)), ("bf16", 128, 11, (4, 4)),
+                                              ("bf16", 128, 12, (4, 4)), ("bf16", 128, 12, (8, 8)), ("f32", 64, 16, (8, 8))])
+def test_the_workgroups_of_many_bins_run_together(dtype, d, gqa, bits):
+    """The last workgroup starts before the first ends: as many fit a CU as the rule says, also where it is a close fit in
+    LDS."""
+    c = Cache([1 << 14] * 16, H=8, gqa=gqa, d=d, Hp=8, bits=bits, headroom=0, fill=False)
+    c.kv_len[:] = 1 << 13                                  # what is attended to does not matter here, only how long
+    cus = torch.cuda.get_device_properties(0).multi_processor_count
+    assert int((c.kv_len // 16).sum()) >= 240 * cus
+    bins = tg.tg_decode_mx_bins(c.geom, TG[dtype], c.fmt, 0, c.B, 0, c.kv_len)
+    assert bins in (2 * cus, 3 * cus)
+    # every head's table holds its pages: the longest head of the one group reserved for all
+    assert np.all(np.diff(c.offsets) >= (1 << 13) // 16)
+    q = torch.zeros(c.B, 8 * gqa, d, dtype=DTYPE[dtype], device="cuda")
+    ts = torch.zeros(2 * bins, dtype=torch.int64, device="cuda")
+    for _ in range(3):                                     # the first call loads the code
+        c.decode(q, dtype, bins=bins, timestamps=ts)
+    start, end = ts.view(-1, 2).cpu().numpy().T
+    assert start.max() < end.min(), f"{bins} bins: the last starts {(start.max() - end.min()) / 100} us after the first ends"
