@@ -979,7 +979,7 @@ int32_t tg_unpack_mx(const tg_unpack_mx_args* args, void* hip_stream);
 
 /* 13d. Bins that a plan for these lengths should have (host): two workgroups a CU
  * of `device`, fewer where the layer's pages are too few to share, three for very
- * much work.  kv_len [B][L][H] (host), with batch and layer; NULL: two a CU.
+ * much work where they fit together.  The rule was measured on plans of TG_PLAN_AOT_FILL.  kv_len [B][L][H] (host), with batch and layer; NULL: two a CU.
  * n_bins out.  Errors: TG_ERR_INVALID_ARG, TG_ERR_UNSUPPORTED, TG_ERR_HIP. */
 int32_t tg_decode_mx_bins(const tg_geometry* geom, int32_t dtype, const tg_mx_format* format, int32_t device,
                           int32_t batch, int32_t layer, const int32_t* kv_len, int32_t* n_bins);

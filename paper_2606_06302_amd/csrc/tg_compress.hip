@@ -317,13 +317,14 @@ __global__ __launch_bounds__(kThreads) void tg_compress_copy_kernel(CopyParams p
   copy_rows<Row, kUnroll, false>(p, it, r0, r1 - r0, [&](int j) { return src_tok[j]; });
 }
 
-// Short chunks in one launch, one single-wave workgroup per work item and no
-// barrier: the wave holds its unit's whole chunk of keys in registers (lane
+// Short chunks in one launch, one workgroup per work item, of one wave (two where
+// the rows are quantised: each ranks the chunk for itself, in LDS of its own, and
+// copies half the item's ranks), and no barrier: a wave holds its unit's whole chunk of keys in registers (lane
 // l, slot i: token 64*i + l, so the score loads are coalesced and token order
 // is slot-major), finds the count-th largest key with the same
 // most-significant-digit radix select as the select launch, on 8-bit digits (the histogram in
 // the wave's LDS, whose operations a wave executes in order), ranks the kept
-// entries by ballots in token order, and copies its own ranks.  The unit's
+// entries by ballots in token order, and copies its ranks.  The unit's
 // first item also writes kept[].  KPL = keys per lane.  Single-wave
 // workgroups spread the items over every CU (measured at chunk 512: 7.9 us,
 // against 8.1, 9.3 and 12.1 us with 4, 8 and 16 items per workgroup).
@@ -430,7 +431,7 @@ __global__ __launch_bounds__(64 * kItemWaves<Row>) void tg_compress_wave_kernel(
   }
 }
 
-// One wave per item, or the two launches of longer chunks.
+// One workgroup per item, or the two launches of longer chunks.
 template <typename Row>
 int32_t launch(const tg_compress_args* a, const SelectParams& s, const CopyParams& c, hipStream_t stream) {
   if (a->chunk_len <= kFusedMaxChunk) {

@@ -4,9 +4,9 @@
 // a workgroup of four waves.  The pages of its items, laid end to end, are cut into
 // four equal ranges, and every wave runs its range by itself with an online softmax
 // of its own; the waves meet once, at the end, where the up to three items that a
-// cut goes through are joined through LDS.  What an item needs (page ids, lengths,
-// heads) is held a lane an item, so that no load stands between one item and the
-// next.
+// cut goes through are joined through LDS.  What an item says (length, head, place of
+// its page ids) is held a lane an item.  Page ids are a scalar load per step, made a
+// step ahead; an item's queries are loaded when it starts.
 //
 // Data movement.  A page's slab (tg_mx.h) goes as it lies into a stage of the
 // wave's ring in LDS with gfx950's global_load_lds (no registers, one wait counted
@@ -32,18 +32,26 @@
 // result where values cancel.  The second part costs 1 to 4 % of a call (there 24.2
 // and 25.1 us); where a step is one page, both go into one product of twice the depth.
 //
-// Bound by memory where there is enough of it: 64 requests, 189971 pages of 8-bit
-// rows (802 MB) 131 us, 6.1 TB/s; 95142 pages of 4-bit rows (207 MB, much of it in
-// the last-level cache) 47 us.  A step of two 4-bit pages (4352 bytes) takes a SIMD
-// about 1400 cycles with two waves on it (190 vector instructions and 16 matrix
-// products each), 7.5 TB/s over the chip, so the compute is not far behind.  A call
-// has about 3.5 us of latency in it (bin, items, page ids, rows, result, one after
-// the other) and 4 for the merge launch: 32 requests, 43233 pages (94 MB) 24.5 us.
-// Measured on the way there: two barriers an item and headers loaded item by item
-// 28 us, the waves' ranges 25.7, every read of a step ahead of its products 24.6;
-// a merge inside the launch (counters, device-scope stores) 2 to 5 us more than the
-// merge launch; 8 waves a workgroup and half the bins 27.  The block-scaled product
-// on the 4-bit codes themselves adds up to only 12 bits of the largest term.
+// Bound by memory where there is enough of it: 32 requests, gqa 4, 166568 pages in 8
+// bits (704 MB) 116 us, 6.1 TB/s.  In 4 bits (362 MB) 69 us, 5.3 TB/s: there the
+// compute is as near.  A step of two 4-bit pages of 128 dims (about 210 vector
+// instructions and 24 matrix products) takes a SIMD with two waves on it 1640 cycles
+// where the slabs stay in the caches, 6.5 TB/s over the chip; one 8-bit page 1025,
+// 10 TB/s.  A wave waits 0.3 us for its bin, 0.8 for the items, 0.5 to 0.8 for the
+// first page ids, 0.9 to 2.6 for the first slab; its results and the join take 0.5 to
+// 1.3; the merge launch 2.5 to 5: 32 requests, 43233 pages (94 MB) 25 us.
+// A step is two pages (one, of 8 + 8 bits and 128 dims) also where a wave has one: the
+// second is then the first again, thrown away by the mask.  In bins of three pages wave
+// 0 has none.
+// Registers: 135 to 168 vector registers in bf16 (183 for 4 + 8 bits at 128 dims, two
+// waves a SIMD), 155 to 168 in fp32 at 64 dims, 183 to 207 at 128; 27 to 36 scalar ones
+// are kept in vector registers, none in memory.
+// Measured on the way there, with P in one part: two barriers an item and headers
+// loaded item by item 28 us, the waves' ranges 25.7, every read of a step ahead of its
+// products 24.6; a merge inside the launch (counters, device-scope stores) 2 to 5 us
+// more than the merge launch; 8 waves a workgroup and half the bins 27.  The
+// block-scaled product on the 4-bit codes themselves adds up to only 12 bits of the
+// largest term.
 #include <hip/hip_runtime.h>
 
 #include <cfloat>
@@ -175,7 +183,9 @@ __device__ __forceinline__ void store4<uint16_t>(uint16_t* dst, const f32x4& v) 
 }
 
 // A wave's ring in LDS, by format: two steps of two pages, of one where two would
-// take a CU's third workgroup (8-bit rows of 128 dims).
+// take a CU's third workgroup (8-bit rows of 128 dims).  Two / three / four steps: 32
+// requests in 4 bits 25.1 / 25.3 / 25.8 us, one long request of 64 dims 15.5 / 15.5 /
+// 15.8; 64 requests in 8 bits, where three do not fit with three workgroups, 60.5 / 70.
 template <int D, int KB, int VB>
 struct Shape {
   static constexpr int kPages = KB + VB == 16 && D == 128 ? 1 : 2;   // of a step

@@ -88,7 +88,7 @@ __device__ __forceinline__ u4 row16(const u2& c, float s) {
 }
 
 constexpr int kUnits = 1024;    // (request, head) units shared out at once
-constexpr int kUnpackWgs = 256;
+constexpr int kUnpackWgs = 256; // the CUs of an MI355X; any number is right
 
 // The lengths are on the device and differ a lot between heads, so the pages are
 // shared out here: every workgroup lays the units' pages end to end (a sum over
@@ -98,7 +98,8 @@ constexpr int kUnpackWgs = 256;
 // a page's codes are requested before the page before it is stored.
 //
 // Bound by memory: 8 requests of up to 16384 tokens (4-bit rows to bf16, 214 MB)
-// 37 us, 5.8 TB/s; a few pages 4.6 us, the chain from tables to codes.  A
+// 37 us, 5.8 TB/s (three such calls in turn, more than the last-level cache holds,
+// 37.3); a few pages 4.6 us, the chain from tables to codes.  A
 // workgroup a unit with plain stores took 92 us there, stores past the caches 52,
 // equal ranges of pages 38.  One workgroup a CU: with two, three or four the same
 // 37.6, 37.9 and 39.3, small calls 5.2 / 5.3 / 5.5 / 6.0, of 14 others two
